@@ -1,0 +1,487 @@
+"""Performance cases of the FP8 products with a scale for each block of 128.
+
+The operators: quantizers to e4m3 codes with one scale per 128 values (along
+the rows after a rotation, along the columns for a weight gradient, per
+128 x 128 tile for weights), the product of such codes, and the product grouped
+by expert with its weight gradient.
+
+The ranges that the cases stand for: 1 to 16384 tokens, rows of 128 to 16384
+values with rotations of 1 to 16384 of them, 1 to 64 experts of any size
+including none, weights of 256 to 8192 rows; fp16 and bf16 inputs, outputs in
+16 or 32 bits.
+
+Keys of a case: "op" ("rows", "tiles", "columns", "matmul", "grouped",
+"gradient"), "dtype" (of the 16-bit input), "out" (of the product: "fp16",
+"bf16", "fp32"), "m" tokens, "n" weight rows (outputs), "k" columns, "rotate"
+(length of a rotation; 1: none), "experts", "empty" (experts without a token).
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+BLOCK = 128
+DTYPES = {"fp16": torch.float16, "bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+def _blocks(k):
+    return (k + BLOCK - 1) // BLOCK
+
+
+def _rows(name, dtype, m, k, rotate):
+    return {"name": name, "op": "rows", "dtype": dtype, "m": m, "k": k, "rotate": rotate}
+
+
+def _tiles(name, dtype, experts, n, k):
+    return {"name": name, "op": "tiles", "dtype": dtype, "experts": experts, "n": n, "k": k}
+
+
+def _columns(name, dtype, m, k, experts, empty):
+    return {"name": name, "op": "columns", "dtype": dtype, "m": m, "k": k, "experts": experts,
+            "empty": empty}
+
+
+def _matmul(name, out, m, n, k):
+    return {"name": name, "op": "matmul", "out": out, "m": m, "n": n, "k": k}
+
+
+def _grouped(name, op, out, m, n, k, experts, empty):
+    return {"name": name, "op": op, "out": out, "m": m, "n": n, "k": k, "experts": experts,
+            "empty": empty}
+
+
+def listed():
+    return [
+        # decode: the hidden states of 17 requests, rotated for the next product
+        _rows("rows_17x4096", "bf16", 17, 4096, 4096),
+        # prefill: hidden states of 16384 tokens, rotated over the whole row
+        _rows("rows_16384x4096", "fp16", 16384, 4096, 4096),
+        # prefill: a wide inner layer of 11 * 1024 columns, rotated block by block
+        _rows("rows_3001x11264", "bf16", 3001, 11264, 1024),
+        # a training step's (or a loader's) weights of eight experts, both orders of the codes
+        _tiles("tiles_8x2048x4096", "bf16", 8, 2048, 4096),
+        # a training step's tokens for the weight gradient, one expert without any
+        _columns("columns_8191x4096", "bf16", 8191, 4096, 8, 1),
+        # decode: one token through a square projection
+        _matmul("matmul_1x4096x4096", "bf16", 1, 4096, 4096),
+        # a batch of requests between decode and prefill, no size a multiple of anything
+        _matmul("matmul_173x5003x4100", "fp16", 173, 5003, 4100),
+        # prefill: the hidden states of 16384 tokens through a square projection
+        _matmul("matmul_16384x4096x4096", "bf16", 16384, 4096, 4096),
+        # decode: 32 requests with two experts each, over 32 experts
+        _grouped("grouped_64x2048x4096", "grouped", "bf16", 64, 2048, 4096, 32, 4),
+        # prefill: 8192 tokens with two experts each, over 16 experts
+        _grouped("grouped_16384x2048x4096", "grouped", "bf16", 16384, 2048, 4096, 16, 1),
+        # a training step's weight gradients of eight experts, in 32 bits for the optimizer
+        _grouped("gradient_8191x2048x4096", "gradient", "fp32", 8191, 2048, 4096, 8, 1),
+        # a dense layer's weight gradient: one group, a ragged number of tokens
+        _grouped("gradient_4001x4096x4096", "gradient", "bf16", 4001, 4096, 4096, 1, 0),
+    ]
+
+
+def _size(rng, low, high):
+    """A size between `low` and `high`, even over its logarithm; half of them odd."""
+    n = round(2.0 ** rng.uniform(math.log2(low), math.log2(high)))
+    return n | 1 if rng.random() < 0.5 else n
+
+
+def draw(rng):
+    op = rng.choice(["rows", "tiles", "columns", "matmul", "matmul", "grouped", "grouped", "gradient"])
+    dtype = rng.choice(["fp16", "bf16"])
+    out = rng.choice(["bf16", "fp16", "fp32"])
+    if op == "rows":
+        rotate = 1 << rng.choice([0, 4, 6, 7, 8, 9, 10, 11, 12, 13, 14])
+        k = _size(rng, 128, 16384) if rotate == 1 else rotate * rng.randint(
+            max(1, 128 // rotate), 16384 // rotate)
+        return {"op": op, "dtype": dtype, "m": _size(rng, 1, min(16384, (1 << 26) // k)), "k": k,
+                "rotate": rotate}
+    if op == "tiles":
+        experts, n = rng.randint(1, 8), _size(rng, 256, 4096)
+        return {"op": op, "dtype": dtype, "experts": experts, "n": n,
+                "k": _size(rng, 256, min(8192, (1 << 26) // (n * experts)))}
+    if op == "columns":
+        experts = rng.choice([1, 1, 4, 8, 33])
+        k = _size(rng, 256, 4096)
+        return {"op": op, "dtype": dtype, "m": _size(rng, 64, 8191), "k": k, "experts": experts,
+                "empty": rng.randint(0, experts // 4)}
+    if op == "matmul":
+        n, k = _size(rng, 256, 8192), _size(rng, 256, 8192)
+        return {"op": op, "out": out, "m": _size(rng, 1, min(16384, (1 << 37) // (n * k))), "n": n,
+                "k": k}
+    experts = rng.choice([4, 8, 16, 33, 64] if op == "grouped" else [1, 4, 8])
+    n, k = _size(rng, 256, 2048), _size(rng, 256, 4096)
+    return {"op": op, "out": out, "m": _size(rng, 1 if op == "grouped" else 64, 8191), "n": n,
+            "k": k, "experts": experts, "empty": rng.randint(0, experts // 4)}
+
+
+# ---- inputs -------------------------------------------------------------------
+
+
+def _values(gen, shape, dtype):
+    """N(0, 1) values with 16 columns x50, as hidden states have them."""
+    v = torch.randn(shape, generator=gen, device="cuda", dtype=torch.float32)
+    v[..., torch.randperm(shape[-1], generator=gen, device="cuda")[:16]] *= 50
+    return v.to(DTYPES[dtype])
+
+
+def _counts(case, gen):
+    """How many tokens each expert has: uneven, `empty` of them none, the others one at least
+    where there are enough tokens."""
+    experts, busy = case["experts"], case["experts"] - case["empty"]
+    share = torch.randn(busy, generator=gen, device="cuda").mul(0.5).exp().double().cpu()
+    counts = torch.zeros(experts, dtype=torch.int64)
+    where = torch.randperm(experts, generator=gen, device="cuda").cpu()[:busy]
+    least = min(1, case["m"] // busy)
+    free = case["m"] - least * busy
+    upto = (share.cumsum(0) / share.sum() * free).round().long()
+    upto[-1] = free
+    counts[where] = least + torch.diff(upto, prepend=torch.zeros(1, dtype=torch.int64))
+    return counts
+
+
+def _codes(gen, rows, k):
+    """e4m3 codes of N(0, 1) rows and a scale for each 128 of a row; the rows of the codes are
+    padded to 16 bytes, as the quantizers allocate them."""
+    codes = torch.zeros((rows, (k + 15) // 16 * 16), dtype=torch.uint8, device="cuda")
+    scales = torch.empty((rows, _blocks(k)), device="cuda")
+    step = max(1, (1 << 26) // k)
+    for r in range(0, rows, step):
+        x = torch.randn((min(step, rows - r), k), generator=gen, device="cuda")
+        x *= torch.rand((x.shape[0], 1), generator=gen, device="cuda") + 0.5
+        q, s = _quantize(x)
+        codes[r : r + step, :k] = q.view(torch.uint8)
+        scales[r : r + step] = s
+    return codes[:, :k], scales
+
+
+def _weights(gen, experts, n, k):
+    """Codes and scales per 128 x 128 tile of `experts` N(0, 1/k) weights."""
+    pitch = (k + 15) // 16 * 16
+    codes = torch.zeros((experts, n, pitch), dtype=torch.uint8, device="cuda")
+    scales = torch.empty((experts, _blocks(n), _blocks(k)), device="cuda")
+    for e in range(experts):
+        w = torch.randn((n, k), generator=gen, device="cuda") / math.sqrt(k)
+        q, s = _quantize_tiles(w)
+        codes[e, :, :k] = q.view(torch.uint8)
+        scales[e] = s
+    return codes[:, :, :k], scales
+
+
+def _transposed(case, gen, counts, width):
+    """What the column quantizer gives for N(0, 1) tokens: codes (width, capacity), one scale
+    for each 128 tokens of a group."""
+    x = torch.randn((case["m"], width), generator=gen, device="cuda")
+    x *= torch.rand((case["m"], 1), generator=gen, device="cuda") + 0.5
+    q, s = _quantize_columns(x, _padded_index(counts, case["m"]))
+    return q.view(torch.uint8), s
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(int(seed))
+    op = case["op"]
+    state = {"op": op, "case": case}
+    if op == "rows":
+        state["x"] = _values(gen, (case["m"], case["k"]), case["dtype"])
+    elif op == "tiles":
+        w = torch.randn((case["experts"], case["n"], case["k"]), generator=gen, device="cuda")
+        state["w"] = (w / math.sqrt(case["k"])).to(DTYPES[case["dtype"]])
+    elif op == "matmul":
+        state["a"], state["sa"] = _codes(gen, case["m"], case["k"])
+        b, sb = _weights(gen, 1, case["n"], case["k"])
+        state["b"], state["sb"] = b[0], sb[0]
+    else:
+        counts = _counts(case, gen)
+        state["ends"] = counts.cumsum(0).to(torch.int32).cuda()
+        if op == "columns":
+            state["x"] = _values(gen, (case["m"], case["k"]), case["dtype"])
+        elif op == "grouped":
+            state["a"], state["sa"] = _codes(gen, case["m"], case["k"])
+            state["b"], state["sb"] = _weights(gen, case["experts"], case["n"], case["k"])
+        else:
+            state["dy"], state["sdy"] = _transposed(case, gen, counts, case["n"])
+            state["x"], state["sx"] = _transposed(case, gen, counts, case["k"])
+        # what the plain form needs to know of the groups without asking the GPU
+        state["most"] = int(counts.max())
+        state["blocks"] = int(((counts + BLOCK - 1) // BLOCK).max())
+    return state
+
+
+# ---- plain forms --------------------------------------------------------------
+
+
+def _inverse(amax):
+    inv = 448.0 / amax
+    return torch.where(torch.isfinite(inv), inv, torch.zeros_like(inv))
+
+
+def _quantize(x):
+    """Codes and scales of the rows of `x` (32 bits), a scale for each 128."""
+    m, k = x.shape
+    blocks = torch.nn.functional.pad(x, (0, -k % BLOCK)).view(m, -1, BLOCK)
+    amax = blocks.abs().amax(dim=2)
+    q = (blocks * _inverse(amax)[..., None]).view(m, -1)[:, :k]
+    return q.to(torch.float8_e4m3fn), amax / 448.0
+
+
+def _quantize_tiles(w):
+    """The same with a scale for each 128 x 128 tile of the last two dimensions."""
+    n, k = w.shape[-2:]
+    v = torch.nn.functional.pad(w, (0, -k % BLOCK, 0, -n % BLOCK))
+    v = v.view(*w.shape[:-2], _blocks(n), BLOCK, _blocks(k), BLOCK)
+    amax = v.abs().amax(dim=(-3, -1))
+    q = v * _inverse(amax)[..., :, None, :, None]
+    q = q.reshape(*w.shape[:-2], _blocks(n) * BLOCK, _blocks(k) * BLOCK)[..., :n, :k]
+    return q.to(torch.float8_e4m3fn), amax / 448.0
+
+
+def _capacity(m, experts):
+    """Token places of the column quantizer: every group padded to 128, for any groups."""
+    return (m // BLOCK + min(m, experts)) * BLOCK
+
+
+def _padded_index(counts, m):
+    """The token at each of the padded places (m: none), from the groups' sizes."""
+    counts = counts.to("cuda")
+    padded = (counts + BLOCK - 1) // BLOCK * BLOCK
+    places = torch.arange(_capacity(m, len(counts)), device="cuda")
+    upto = padded.cumsum(0)
+    group = torch.searchsorted(upto, places, right=True).clamp(max=len(counts) - 1)
+    within = places - (upto - padded)[group]
+    token = (counts.cumsum(0) - counts)[group] + within
+    return torch.where(within < counts[group], token, m)
+
+
+def _quantize_columns(x, index):
+    """Transposed codes of the tokens of `x` (32 bits) at the padded places."""
+    v = torch.nn.functional.pad(x, (0, 0, 0, 1))[index]  # the token after the last is zero
+    v = v.view(-1, BLOCK, x.shape[1])
+    amax = v.abs().amax(dim=1)
+    q = (v * _inverse(amax)[:, None]).view(-1, x.shape[1])
+    return q.to(torch.float8_e4m3fn).t().contiguous(), (amax / 448.0).t().contiguous()
+
+
+def _hadamard(n):
+    i = torch.arange(n, device="cuda")
+    bits = i[:, None] & i[None, :]
+    bits = bits ^ (bits >> 8)
+    bits = bits ^ (bits >> 4)
+    bits = bits ^ (bits >> 2)
+    bits = bits ^ (bits >> 1)
+    return 1.0 - 2.0 * (bits & 1).float()
+
+
+def _rotate(x, n):
+    """Each n columns of `x` (32 bits) times H_n / sqrt(n), as H_a and H_b with a * b = n."""
+    a = 1 << (n.bit_length() - 1) // 2
+    b = n // a
+    v = (x * (1.0 / math.sqrt(n))).view(-1, b) @ _hadamard(b)
+    v = _hadamard(a) @ v.view(-1, a, b)
+    return v.view(x.shape)
+
+
+def _widen(codes, scales):
+    """The values of row codes in 32 bits."""
+    k = codes.shape[-1]
+    return codes.view(torch.float8_e4m3fn).float() * scales.repeat_interleave(BLOCK, -1)[..., :k]
+
+
+def _widen_tiles(codes, scales):
+    return _widen(codes, scales.repeat_interleave(BLOCK, -2)[..., : codes.shape[-2], :])
+
+
+def _counts_of(ends):
+    ends = ends.long()
+    return torch.diff(ends, prepend=ends.new_zeros(1))
+
+
+def _plain(state):
+    case, op = state["case"], state["op"]
+    if op == "rows":
+        return _quantize(_rotate(state["x"].float(), case["rotate"]))
+    if op == "tiles":
+        q, s = _quantize_tiles(state["w"].float())
+        return q, q.transpose(-1, -2).contiguous(), s
+    if op == "columns":
+        index = _padded_index(_counts_of(state["ends"]), case["m"])
+        return _quantize_columns(state["x"].float(), index)
+    out = DTYPES[case["out"]]
+    if op == "matmul":
+        return (_widen(state["a"], state["sa"]) @ _widen_tiles(state["b"], state["sb"]).t()).to(out)
+    counts = _counts_of(state["ends"])
+    if op == "grouped":
+        # every group padded to the largest, one product for all
+        within = torch.arange(state["most"], device="cuda")
+        token = (counts.cumsum(0) - counts)[:, None] + within
+        valid = within < counts[:, None]
+        a = _widen(state["a"], state["sa"])[torch.where(valid, token, 0)]
+        y = a @ _widen_tiles(state["b"], state["sb"]).transpose(-1, -2).contiguous()
+        return y.view(-1, case["n"])[_places(counts, state)].to(out)
+    # weight gradient: the padded tokens of each group, up to the longest group
+    blocks = (counts + BLOCK - 1) // BLOCK
+    within = torch.arange(state["blocks"] * BLOCK, device="cuda")
+    place = (blocks.cumsum(0) - blocks)[:, None] * BLOCK + within
+    valid = within < blocks[:, None] * BLOCK
+    place = torch.where(valid, place, 0)
+    dy = _widen(state["dy"], state["sdy"]).t()[place] * valid[..., None]
+    x = _widen(state["x"], state["sx"]).t()[place] * valid[..., None]
+    return (dy.transpose(1, 2).contiguous() @ x).to(out)
+
+
+def _places(counts, state):
+    """Where each token lies among the groups padded to the largest."""
+    token = torch.arange(state["case"]["m"], device="cuda")
+    upto = counts.cumsum(0)
+    group = torch.searchsorted(upto, token, right=True)
+    return group * state["most"] + token - (upto - counts)[group]
+
+
+def run(state):
+    if not own:
+        return _plain(state)
+    from paper_2412_08832_amd import hadacore
+
+    case, op = state["case"], state["op"]
+    e4m3 = torch.float8_e4m3fn
+    if op == "rows":
+        codes, scales = hadacore.transform_fp8_blocks(state["x"], n=case["rotate"])
+        return codes.view(e4m3), scales
+    if op == "tiles":
+        codes, scales, codes_t = hadacore.quantize_fp8_tiles(state["w"], transposed=True)
+        return codes.view(e4m3), codes_t.view(e4m3), scales
+    if op == "columns":
+        codes, scales = hadacore.quantize_fp8_columns(state["x"], ends=state["ends"])
+        return codes.view(e4m3), scales
+    out = DTYPES[case["out"]]
+    if op == "matmul":
+        return hadacore.matmul_fp8(state["a"], state["sa"], state["b"], state["sb"], dtype=out)
+    if op == "grouped":
+        return hadacore.grouped_matmul_fp8(state["a"], state["sa"], state["b"], state["sb"],
+                                           state["ends"], dtype=out)
+    return hadacore.grouped_weight_gradient_fp8(state["dy"], state["sdy"], state["x"], state["sx"],
+                                                state["ends"], dtype=out)
+
+
+def work(case):
+    op, k = case["op"], case["k"]
+    if op == "rows":
+        m = case["m"]
+        return {"bytes": 3 * m * k + 4 * m * _blocks(k),
+                "flops": m * k * (math.log2(case["rotate"]) + 3)}
+    if op == "tiles":
+        e, n = case["experts"], case["n"]
+        return {"bytes": 4 * e * n * k + 4 * e * _blocks(n) * _blocks(k), "flops": 3 * e * n * k}
+    if op == "columns":
+        m = case["m"]
+        places = _capacity(m, case["experts"])
+        return {"bytes": 2 * m * k + places * k + 4 * places // BLOCK * k, "flops": 3 * m * k}
+    m, n = case["m"], case["n"]
+    wide = 4 if case["out"] == "fp32" else 2
+    flops = 2 * m * n * k
+    if op == "matmul":
+        return {"bytes": m * k + n * k + 4 * (m + _blocks(n)) * _blocks(k) + wide * m * n,
+                "flops": flops}
+    e = case["experts"]
+    if op == "grouped":
+        hit = min(m, e - case["empty"])
+        return {"bytes": m * k + hit * n * k + 4 * (m + hit * _blocks(n)) * _blocks(k) + wide * m * n,
+                "flops": flops}
+    return {"bytes": m * (n + k) + 4 * _blocks(m) * (n + k) + wide * e * n * k, "flops": flops}
+
+
+# ---- 64 bits --------------------------------------------------------------------
+
+
+def _transform64(x, n):
+    y = x.double().view(-1, n) * float(torch.tensor(1.0 / math.sqrt(n), dtype=torch.float32))
+    h = 1
+    while h < n:
+        v = y.view(-1, n // (2 * h), 2, h)
+        y = torch.stack((v[:, :, 0] + v[:, :, 1], v[:, :, 0] - v[:, :, 1]), dim=2).view(-1, n)
+        h *= 2
+    return y.view(x.shape)
+
+
+def _split64(v):
+    """What e4m3 rounds, and the scales, of (..., 128) blocks in 64 bits."""
+    amax = v.abs().amax(dim=-1)
+    factor = torch.where(amax > 0, 448 / amax, torch.zeros_like(amax))
+    return v * factor[..., None], amax / 448
+
+
+def _value64(codes):
+    """The values of e4m3 codes: sign, exponent of bias 7, three bits of fraction."""
+    c = codes.view(torch.uint8).to(torch.int32)
+    exponent, fraction = (c >> 3) & 15, (c & 7).double()
+    value = torch.where(exponent == 0, fraction * 2.0 ** -9,
+                        (1 + fraction / 8) * torch.exp2(exponent.double() - 7))
+    return torch.where(c >= 128, -value, value)
+
+
+def _matrix64(codes, scales, tall):
+    """codes * scales, where a scale covers `tall` rows and 128 columns."""
+    r = torch.arange(codes.shape[0], device="cuda") // tall
+    c = torch.arange(codes.shape[1], device="cuda") // BLOCK
+    return _value64(codes) * scales.double()[r][:, c]
+
+
+def exact(case, seed):
+    state = prepare(case, seed)
+    op, k = case["op"], case["k"]
+    if op == "rows":
+        m = case["m"]
+        y = torch.zeros((m, _blocks(k) * BLOCK), dtype=torch.float64, device="cuda")
+        step = max(1, (1 << 25) // k)
+        for r in range(0, m, step):
+            y[r : r + step, :k] = _transform64(state["x"][r : r + step], case["rotate"])
+        q, s = _split64(y.view(m, -1, BLOCK))
+        return q.view(m, -1)[:, :k], s
+    if op == "tiles":
+        e, n = case["experts"], case["n"]
+        q = torch.empty((e, n, k), dtype=torch.float64, device="cuda")
+        s = torch.empty((e, _blocks(n), _blocks(k)), dtype=torch.float64, device="cuda")
+        for i in range(e):
+            w = torch.zeros((_blocks(n) * BLOCK, _blocks(k) * BLOCK), dtype=torch.float64,
+                            device="cuda")
+            w[:n, :k] = state["w"][i]
+            t = w.view(_blocks(n), BLOCK, _blocks(k), BLOCK).permute(0, 2, 1, 3)
+            v, s[i] = _split64(t.reshape(_blocks(n), _blocks(k), BLOCK * BLOCK))
+            v = v.view(_blocks(n), _blocks(k), BLOCK, BLOCK).permute(0, 2, 1, 3)
+            q[i] = v.reshape(w.shape)[:n, :k]
+        return q, q.transpose(1, 2), s
+    if op == "matmul":
+        return _matrix64(state["a"], state["sa"], 1) @ _matrix64(state["b"], state["sb"], BLOCK).t()
+    ends = [0] + state["ends"].tolist()
+    groups = list(zip(ends[:-1], ends[1:]))
+    if op == "columns":
+        places = _capacity(case["m"], case["experts"])
+        q = torch.zeros((k, places), dtype=torch.float64, device="cuda")
+        s = torch.zeros((k, places // BLOCK), dtype=torch.float64, device="cuda")
+        at = 0
+        for low, high in groups:
+            wide = _blocks(high - low)
+            v = torch.zeros((k, wide * BLOCK), dtype=torch.float64, device="cuda")
+            v[:, : high - low] = state["x"][low:high].t()
+            v, s[:, at : at + wide] = _split64(v.view(k, wide, BLOCK))
+            q[:, at * BLOCK : (at + wide) * BLOCK] = v.reshape(k, -1)
+            at += wide
+        return q, s
+    if op == "grouped":
+        y = torch.empty((case["m"], case["n"]), dtype=torch.float64, device="cuda")
+        for e, (low, high) in enumerate(groups):
+            if low < high:
+                y[low:high] = (_matrix64(state["a"][low:high], state["sa"][low:high], 1)
+                               @ _matrix64(state["b"][e], state["sb"][e], BLOCK).t())
+        return y
+    g = torch.zeros((case["experts"], case["n"], k), dtype=torch.float64, device="cuda")
+    at = 0
+    for e, (low, high) in enumerate(groups):
+        wide = _blocks(high - low)
+        cut, cuts = slice(at * BLOCK, (at + wide) * BLOCK), slice(at, at + wide)
+        if wide:
+            g[e] = (_matrix64(state["dy"][:, cut], state["sdy"][:, cuts], 1)
+                    @ _matrix64(state["x"][:, cut], state["sx"][:, cuts], 1).t())
+        at += wide
+    return g
