@@ -239,7 +239,7 @@ def _quantize_tiles(w):
 
 def _capacity(m, experts):
     """Token places of the column quantizer: every group padded to 128, for any groups."""
-    return (m // BLOCK + min(m, experts)) * BLOCK
+    return (m + (BLOCK - 1) * min(m, experts)) // BLOCK * BLOCK
 
 
 def _padded_index(counts, m):
