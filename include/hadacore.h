@@ -81,11 +81,12 @@
 extern "C" {
 #endif
 
-#define HADACORE_VERSION 10200 /* 1.2.0: hadamard_transform_ws_noalloc */
+#define HADACORE_VERSION 10300 /* 1.3.0: codes with a scale per block of 128, their products */
 
 typedef int32_t hadacore_dtype;
 #define HADACORE_FP16 0 /* IEEE binary16 */
 #define HADACORE_BF16 1 /* bfloat16 */
+#define HADACORE_FP32 2 /* IEEE binary32: output of the FP8 products only */
 
 typedef int32_t hadacore_status;
 #define HADACORE_SUCCESS 0
@@ -237,6 +238,157 @@ hadacore_status hadamard_transform_fp8(const void *in, int64_t in_row_stride, vo
 hadacore_status hadamard_transform_int8(const void *in, int64_t in_row_stride, void *out_codes,
                                         int64_t out_row_stride, float *out_scales, int64_t m,
                                         int64_t n, hadacore_dtype dtype, float scale, void *stream);
+
+/*
+ * FP8 codes with a scale for each block of 128, and their products.
+ *
+ * A block of 128 values y is stored as e4m3 codes and one fp32 scale, as a row is by
+ * hadamard_transform_fp8:
+ *     amax = max |y| (NaN ignored unless the block is all NaN),
+ *     scale = amax / 448, code = e4m3 of y * (448 / amax), 448 / amax taken as 0 where
+ *     it is not finite.
+ * A block lies along a row (activations), down a column (the operands of a weight
+ * gradient, transposed), or is a tile of 128 x 128 (weights).  The last block of a row, column
+ * or tile may be shorter.  The products take the codes as they are: a NaN code, or an Inf
+ * or NaN scale, reaches the outputs of its own row and column as IEEE arithmetic dictates.
+ *
+ * Rows of codes start every `row_stride` bytes, a multiple of 16 and at most 2^22 for
+ * the products (2^26 for hadamard_transform_fp8_blocks), from a 16-byte aligned
+ * address.  The products read codes in 16-byte pieces: every row of codes must be
+ * readable up to the next multiple of 16 bytes; what lies there is ignored.  Rows of
+ * scales start every `scales_row_stride` floats.
+ *
+ * Groups: `ends` is a device array of `groups` int32, the end of each group of rows (or
+ * tokens), in order: group g is [ends[g - 1], ends[g]), the first starts at 0, and a
+ * group may be empty.  Values outside [0, rows] are taken as the nearest inside; ends that
+ * go down give unspecified outputs, but no access out of bounds.  The host does not read
+ * them: no call waits for the GPU.
+ *
+ * Streams, ownership, errors and graph capture are as for the transforms.  Sizes are below
+ * 2^30 (HADACORE_ERROR_TOO_LARGE), batches and groups too.
+ */
+
+/*
+ * hadamard_transform_fp8_blocks -- each row of k values rotated in blocks of n, and
+ * quantized with a scale for each 128 of the row.  With y = scale * H_n applied to
+ * each n consecutive values (n = 1: the values times `scale`), code row i holds the codes
+ * of y[i], and out_scales[i * scales_row_stride + b] the scale of columns 128 b .. 128 b + 127.
+ *   in              m rows of k 16-bit values, in_row_stride elements apart (>= k, <= 2^26).
+ *                   n >= 128: 16-byte aligned and the stride a multiple of 8; n <= 64: any
+ *                   stride, 2-byte aligned
+ *   out_codes       m rows of k bytes, out_row_stride (>= k, multiple of 16, <= 2^26) apart
+ *   out_scales      m rows of ceil(k / 128) floats
+ *   k               a multiple of n, >= 0
+ *   n               a power of two in [1, 32768]
+ * Rows without gaps take one launch; others one for each n columns if n >= 128.  The
+ * three ranges must not overlap.
+ */
+hadacore_status hadamard_transform_fp8_blocks(const void *in, int64_t in_row_stride,
+                                              void *out_codes, int64_t out_row_stride,
+                                              float *out_scales, int64_t scales_row_stride,
+                                              int64_t m, int64_t k, int64_t n,
+                                              hadacore_dtype dtype, float scale, void *stream);
+
+/*
+ * hadacore_padded_tokens -- the places that `tokens` tokens in `groups` groups may
+ * take when each group is padded to a multiple of 128, whatever the groups:
+ * floor((tokens + 127 min(groups, tokens)) / 128) * 128.  0 for negative arguments.
+ */
+int64_t hadacore_padded_tokens(int64_t tokens, int64_t groups);
+
+/*
+ * hadacore_quantize_fp8_columns -- codes of a tall matrix, transposed, with a scale for
+ * each 128 rows of a column: the operands of a weight gradient, which sums over rows
+ * (tokens).  Each group of rows is padded with zeros to a multiple of 128, and the groups
+ * follow each other; out_codes[c][p] is the code of column c at padded place p, and
+ * out_scales[c][p / 128] its scale.  Places after the last group, up to
+ * hadacore_padded_tokens(m, groups), get zero codes and scales.  Rows after the last end
+ * are left out.
+ *   in          m rows of k 16-bit values, any stride >= k (<= 2^26), 2-byte aligned
+ *   ends        the groups' ends; NULL with groups = 1: one group of all rows
+ *   out_codes   k rows of hadacore_padded_tokens(m, groups) bytes
+ *   out_scales  k rows of a 128th of that
+ * Ranges must not overlap.  m is at most 2^22 by the stride of the codes.
+ */
+hadacore_status hadacore_quantize_fp8_columns(const void *in, int64_t in_row_stride,
+                                              const int32_t *ends, int64_t groups,
+                                              void *out_codes, int64_t out_row_stride,
+                                              float *out_scales, int64_t scales_row_stride,
+                                              int64_t m, int64_t k, hadacore_dtype dtype,
+                                              void *stream);
+
+/*
+ * hadacore_quantize_fp8_tiles -- codes of `batch` m x k matrices with a scale for each
+ * tile of 128 x 128: weights.  out_codes_t, unless NULL, gets the codes transposed (k
+ * rows of m bytes), for the product with the transposed weights; their scales are
+ * out_scales transposed.
+ *   in                   m rows of k 16-bit values, any stride >= k (<= 2^26), 2-byte aligned
+ *   out_scales           ceil(m / 128) rows of ceil(k / 128) floats
+ *   *_batch_stride       elements (bytes, floats) from one matrix to the next; not used for
+ *                        batch <= 1.  Output matrices must not interleave.
+ * Ranges must not overlap.
+ */
+hadacore_status hadacore_quantize_fp8_tiles(const void *in, int64_t in_row_stride,
+                                            int64_t in_batch_stride, void *out_codes,
+                                            int64_t out_row_stride, int64_t out_batch_stride,
+                                            void *out_codes_t, int64_t out_t_row_stride,
+                                            int64_t out_t_batch_stride, float *out_scales,
+                                            int64_t scales_row_stride,
+                                            int64_t scales_batch_stride, int64_t batch,
+                                            int64_t m, int64_t k, hadacore_dtype dtype,
+                                            void *stream);
+
+/*
+ * hadacore_matmul_fp8 -- out = A B^T for codes A (m x k) and B (n x k):
+ *     out[i][j] = sum_b a_scales[i][b] * b_scales[j'][b] * sum_{c in block b} A[i][c] B[j][c],
+ * j' = j for b_scale_rows = 1 and j / 128 for b_scale_rows = 128 (weights in tiles).
+ * Products are exact, sums are fp32, and the result is rounded once, to nearest even.
+ *   a, b            codes; a_scales m rows of ceil(k / 128) floats, b_scales n (or
+ *                   ceil(n / 128)) rows
+ *   out             m rows of n values of out_dtype (HADACORE_FP16, _BF16 or _FP32),
+ *                   out_row_stride elements apart (>= n, <= 2^26), aligned to its values
+ *   k               >= 0; k = 0 gives zeros
+ * The output must not overlap the inputs.
+ */
+hadacore_status hadacore_matmul_fp8(const void *a, int64_t a_row_stride, const float *a_scales,
+                                    int64_t a_scales_row_stride, const void *b,
+                                    int64_t b_row_stride, const float *b_scales,
+                                    int64_t b_scales_row_stride, int32_t b_scale_rows, void *out,
+                                    int64_t out_row_stride, hadacore_dtype out_dtype, int64_t m,
+                                    int64_t n, int64_t k, void *stream);
+
+/*
+ * hadacore_matmul_fp8_grouped -- hadacore_matmul_fp8 with rows of A sorted by group (expert)
+ * and a B of its own for each group: out[i] = A[i] B[g]^T for the rows i of group g.  B
+ * is `groups` matrices of n x k codes with a scale per tile of 128 x 128,
+ * b_batch_stride bytes (a multiple of 16) and b_scales_batch_stride floats apart.  Rows
+ * after the last end get zeros.
+ */
+hadacore_status hadacore_matmul_fp8_grouped(const void *a, int64_t a_row_stride,
+                                            const float *a_scales, int64_t a_scales_row_stride,
+                                            const void *b, int64_t b_row_stride,
+                                            int64_t b_batch_stride, const float *b_scales,
+                                            int64_t b_scales_row_stride,
+                                            int64_t b_scales_batch_stride, const int32_t *ends,
+                                            int64_t groups, void *out, int64_t out_row_stride,
+                                            hadacore_dtype out_dtype, int64_t m, int64_t n,
+                                            int64_t k, void *stream);
+
+/*
+ * hadacore_weight_gradient_fp8_grouped -- the weight gradients of such a product: for each
+ * group g, out[g] (n x k) = sum over the group's tokens t of A[:, t] B[:, t]^T, where A
+ * (n rows: output gradients) and B (k rows: inputs) are what
+ * hadacore_quantize_fp8_columns gives for the same tokens and `ends`: rows of `places` =
+ * hadacore_padded_tokens(tokens, groups) codes, a multiple of 128 (INVALID_SIZE).  A group
+ * without tokens gets zeros.  ends = NULL with groups = 1: one group of all tokens.  The
+ * outputs are out_batch_stride elements apart.
+ */
+hadacore_status hadacore_weight_gradient_fp8_grouped(
+    const void *a, int64_t a_row_stride, const float *a_scales, int64_t a_scales_row_stride,
+    const void *b, int64_t b_row_stride, const float *b_scales, int64_t b_scales_row_stride,
+    const int32_t *ends, int64_t groups, void *out, int64_t out_row_stride,
+    int64_t out_batch_stride, hadacore_dtype out_dtype, int64_t places, int64_t n, int64_t k,
+    void *stream);
 
 /*
  * hadacore_stream_copy -- copies `bytes` bytes from device pointer `src` to

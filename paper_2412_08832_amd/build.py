@@ -12,7 +12,7 @@ from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
 ROOT = PKG.parent
-SOURCES = [PKG / "csrc" / "hadacore.hip"]
+SOURCES = [PKG / "csrc" / "hadacore.hip", PKG / "csrc" / "fp8_blocks.hip"]
 INCLUDE = ROOT / "include"
 LIBRARY = PKG / "libhadacore.so"
 ARCH = "gfx950"

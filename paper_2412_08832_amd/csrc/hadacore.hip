@@ -70,6 +70,7 @@
 #include <type_traits>
 
 #include "hadacore.h"
+#include "internal.h"
 
 namespace hadacore {
 namespace {
@@ -577,11 +578,13 @@ struct ScaleArgs {
 constexpr int kStore16 = 0;  // 16-bit output in the input dtype
 constexpr int kFp8 = 1;      // e4m3 codes + one fp32 scale per row
 constexpr int kInt8 = 2;     // int8 codes + one fp32 scale per row
+constexpr int kFp8Blocks = 3;  // e4m3 codes + one fp32 scale per 128 values of a row (n >= 128)
 
 struct QuantOut {
   uint8_t *codes;
-  int64_t stride;  // bytes between rows of codes
-  float *scales;   // one per row
+  int64_t stride;        // bytes between rows of codes
+  float *scales;         // one per row; kFp8Blocks: n / 128 per row
+  int64_t scale_stride;  // kFp8Blocks: floats between the scales of two rows
 };
 
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
@@ -741,6 +744,59 @@ struct RowQuant {
   }
 };
 
+// kFp8Blocks: amax, scale and codes are those of kFp8 for each 128 consecutive
+// outputs of a row instead of the whole row.  A chunk of the matrix-core front
+// holds four such blocks, told apart by the outputs' tile bits 7 and 8 (lane_field
+// >> 4).  With n = 128 and 256 these sit on lane bits 2 and 3; from n = 512 the
+// change of basis (lane_frequency) makes them the parity of lane bits 0-2, and lane
+// bit 3.  So the lanes of one block are l ^ b for every b that the values 1, 2, 16,
+// 32, or 3, 6, 16, 32, span.  All steps stay in the VALU: quad permutations, xor 6 as
+// row_half_mirror (xor 7) then xor 1, and the row swaps, which given the same
+// register twice leave a lane's own row in one result and its partner's in the other.
+template <int L>
+__device__ __forceinline__ float block_lane_max(float x) {
+  static_assert(L >= 7, "a block of 128 lies inside a row");
+  const auto dpp = [](float v, auto ctrl) {
+    return __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(ctrl)::value, 0xF, 0xF,
+                                    true);
+  };
+  using Xor1 = std::integral_constant<int, 0xB1>;   // quad_perm [1, 0, 3, 2]
+  using Xor2 = std::integral_constant<int, 0x4E>;   // quad_perm [2, 3, 0, 1]
+  using Xor3 = std::integral_constant<int, 0x1B>;   // quad_perm [3, 2, 1, 0]
+  using Xor7 = std::integral_constant<int, 0x141>;  // row_half_mirror
+  if constexpr (L <= 8) {
+    x = max_with(x, dpp(x, Xor1{}));
+    x = max_with(x, dpp(x, Xor2{}));
+  } else {
+    x = max_with(x, dpp(x, Xor3{}));
+    x = max_with(x, dpp(__builtin_bit_cast(float, dpp(x, Xor7{})), Xor1{}));
+  }
+  const uint32_t b = __builtin_bit_cast(uint32_t, x);
+  const auto s16 = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  x = max_with(__builtin_bit_cast(float, s16[0]), (int)s16[1]);
+  const uint32_t c = __builtin_bit_cast(uint32_t, x);
+  const auto s32 = __builtin_amdgcn_permlane32_swap(c, c, false, false);
+  return max_with(__builtin_bit_cast(float, s32[0]), (int)s32[1]);
+}
+
+// Scale and codes of a lane's 8 values of a block (matrix-core front), given the
+// largest |register| of the block.  As in RowQuant one division serves two lanes; the
+// pair is l and l ^ 3, which are in one block at every n.
+struct BlockQuant {
+  float scale;  // amax / 448
+  float mul;    // (twist sign) * post * 448 / amax, 0 where 448 / amax is not finite
+  __device__ __forceinline__ BlockQuant(float reg_amax, bool tw, float post, int lane) {
+    const float amax = reg_amax * fabsf(post);
+    const bool odd = (lane & 1) != 0;
+    const float q = (odd ? amax : 448.0f) / (odd ? 448.0f : amax);
+    const float qp = __builtin_bit_cast(
+        float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, q), 0x1B, 0xF, 0xF, true));
+    scale = odd ? q : qp;
+    const float inv = odd ? qp : q;
+    mul = (tw ? -post : post) * (inv < __builtin_inff() ? inv : 0.0f);
+  }
+};
+
 // ---- kernels ------------------------------------------------------------------
 
 // n <= 512*C: a tile of 512*C elements is 512*C/n whole rows and every stage
@@ -789,7 +845,8 @@ __global__ __launch_bounds__(kWave *WPB) void fwht_wave_kernel(
   const char *src = reinterpret_cast<const char *>(in) + row0 * in_stride * 2;
   char *dst = EPI == kStore16 ? reinterpret_cast<char *>(out) + row0 * out_pitch
                               : reinterpret_cast<char *>(qo.codes) + row0 * out_pitch;
-  float *scales = EPI == kStore16 ? nullptr : qo.scales + row0;
+  const int64_t scale_pitch = EPI == kFp8Blocks ? qo.scale_stride : 1;
+  float *scales = EPI == kStore16 ? nullptr : qo.scales + row0 * scale_pitch;
   auto rows_in_tile = [&](int64_t r0) { return (int)(m - r0 < kRows ? m - r0 : kRows); };
   auto load_tile = [&](const char *base, int valid, u4(&raw)[C]) {
 #pragma unroll
@@ -832,6 +889,18 @@ __global__ __launch_bounds__(kWave *WPB) void fwht_wave_kernel(
       for (int k = 0; k < C; ++k) {
         if (kRows == 1 || st_row[k] < cur_valid) gstore_u<NT, SC1>(dst, st_off[k], fin(&v[k * 8]));
       }
+    } else if constexpr (EPI == kFp8Blocks) {
+      const bool tw = twisted<FRONT, L>(lane);
+#pragma unroll
+      for (int k = 0; k < C; ++k) {
+        const BlockQuant qz(block_lane_max<L>(abs_max8(&v[k * 8])), tw, sc.post, lane);
+        if (kRows == 1 || st_row[k] < cur_valid) {
+          gstore8_u<NT, SC1>(dst, st_off[k], to_e4m3x8(&v[k * 8], qz.mul));
+          if ((lf & 15) == 0)
+            scales[st_row[k] * qo.scale_stride + ((((k * kWave + lf) * 8) & kMask) >> 7)] =
+                qz.scale;
+        }
+      }
     } else {
       // row maxima: within each chunk, across the chunks of one row (chunk
       // bits that are element bits), then across the row's lanes
@@ -870,7 +939,7 @@ __global__ __launch_bounds__(kWave *WPB) void fwht_wave_kernel(
     if (!more) break;
     row0 += kRows;
     dst += (int64_t)kRows * out_pitch;
-    if constexpr (EPI != kStore16) scales += kRows;
+    if constexpr (EPI != kStore16) scales += kRows * scale_pitch;
   }
 }
 
@@ -1037,6 +1106,17 @@ __global__ __launch_bounds__((1 << L) / (8 * C)) void fwht_block_kernel(
     for (int k = 0; k < C; ++k) {
       const int W = (k % NW) * C + (k / NW) * NW + w;
       gstore_u<NT, kSc1>(dst, (uint32_t)((W * kWave + lf) * 16), fin(&v[k * 8]));
+    }
+  } else if constexpr (EPI == kFp8Blocks) {
+    const bool tw = twisted<FRONT, L>(lane);
+    uint8_t *codes = qo.codes + row * qo.stride;
+    float *scales = qo.scales + row * qo.scale_stride;
+#pragma unroll
+    for (int k = 0; k < C; ++k) {
+      const int W = (k % NW) * C + (k / NW) * NW + w;
+      const BlockQuant qz(block_lane_max<L>(abs_max8(&v[k * 8])), tw, sc.post, lane);
+      gstore8_u<NT, kSc1>(codes, (uint32_t)((W * kWave + lf) * 8), to_e4m3x8(&v[k * 8], qz.mul));
+      if ((lf & 15) == 0) scales[W * 4 + (lf >> 4)] = qz.scale;
     }
   } else {
     // the row spans the workgroup: registers, then lanes, then waves (through LDS)
@@ -1810,8 +1890,6 @@ ScaleArgs split_scale(float scale, int dtype) {
   return a;
 }
 
-int device_cus();
-
 // Whether rows of `row_bytes` at `pitch_bytes` from `p` lie in whole 128-byte
 // lines: p is aligned to 128 and either the rows are contiguous or both the
 // row and the pitch are multiples of 128 bytes.  Row bytes 0 checks p only.
@@ -2349,6 +2427,8 @@ constexpr int kMaxDevices = 64;
 std::atomic<int> g_arch_state[kMaxDevices];
 std::atomic<int> g_cus[kMaxDevices];
 
+}  // namespace
+
 hadacore_status check_device() {
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0) return HADACORE_ERROR_UNSUPPORTED_DEVICE;
@@ -2380,6 +2460,8 @@ int device_cus() {
     return c;
   return 256;
 }
+
+namespace {
 
 // Largest row stride (elements, or bytes for FP8 codes): keeps every offset
 // inside a wave tile (at most 32 rows) below 2^32 bytes.
@@ -2652,6 +2734,114 @@ extern "C" hadacore_status hadamard_transform_int8(const void *in, int64_t in_ro
                                                    hadacore_dtype dtype, float scale, void *stream) {
   return transform_quantized<kInt8>(in, in_row_stride, out_codes, out_row_stride, out_scales, m,
                                     n, dtype, scale, stream);
+}
+
+namespace hadacore {
+namespace {
+
+// Rotated rows of n = 2^L >= 128 values with a scale per 128, `m` rows: the matrix-core
+// front end at every size, as for the other quantized outputs.
+template <int DT>
+hipError_t launch_blocks_one(int L, const uint16_t *in, int64_t in_stride, int64_t m,
+                             const ScaleArgs &sc, hipStream_t stream, const QuantOut &qo) {
+  switch (L) {
+#define HC_BLOCKS(N)                                                                             \
+  case N:                                                                                        \
+    return launch_front<DT, N, kFp8Blocks, kMfma>(in, in_stride, nullptr, 0, m, sc, stream, qo)
+    HC_BLOCKS(7);
+    HC_BLOCKS(8);
+    HC_BLOCKS(9);
+    HC_BLOCKS(10);
+    HC_BLOCKS(11);
+    HC_BLOCKS(12);
+    HC_BLOCKS(13);
+    HC_BLOCKS(14);
+    HC_BLOCKS(15);
+#undef HC_BLOCKS
+    default: return hipErrorInvalidValue;
+  }
+}
+
+template <int DT>
+hipError_t launch_blocks(int L, const uint16_t *in, int64_t in_stride, int64_t m,
+                         const ScaleArgs &sc, hipStream_t stream, const QuantOut &qo) {
+  const int64_t chunk = rows_per_launch(L);
+  for (int64_t r0 = 0; r0 < m; r0 += chunk) {
+    QuantOut q = qo;
+    q.codes += r0 * qo.stride;
+    q.scales += r0 * qo.scale_stride;
+    const hipError_t e = launch_blocks_one<DT>(L, in + r0 * in_stride, in_stride,
+                                               m - r0 < chunk ? m - r0 : chunk, sc, stream, q);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+constexpr int kMaxBlocksL = 15;
+
+}  // namespace
+}  // namespace hadacore
+
+extern "C" hadacore_status hadamard_transform_fp8_blocks(
+    const void *in, int64_t in_row_stride, void *out_codes, int64_t out_row_stride,
+    float *out_scales, int64_t scales_row_stride, int64_t m, int64_t k, int64_t n,
+    hadacore_dtype dtype, float scale, void *stream) {
+  if (m < 0 || k < 0) return HADACORE_ERROR_INVALID_VALUE;
+  const int L = log2_exact(n);
+  if (L < 0 || L > kMaxBlocksL || k % n != 0) return HADACORE_ERROR_INVALID_SIZE;
+  if (dtype != HADACORE_FP16 && dtype != HADACORE_BF16) return HADACORE_ERROR_INVALID_DTYPE;
+  if (!isfinite(scale)) return HADACORE_ERROR_INVALID_VALUE;
+  const bool wide = n >= 128;  // the transform's kernels, with their rules for the input
+  const int64_t blocks = (k + 127) / 128;
+  if (in_row_stride < k || (wide && in_row_stride % 8 != 0) || out_row_stride < k ||
+      out_row_stride % 16 != 0 || scales_row_stride < blocks || in_row_stride > kMaxStride ||
+      out_row_stride > kMaxStride || scales_row_stride > kMaxStride)
+    return HADACORE_ERROR_INVALID_STRIDE;
+  if (m == 0 || k == 0) return HADACORE_SUCCESS;
+  if (in == nullptr || out_codes == nullptr || out_scales == nullptr)
+    return HADACORE_ERROR_INVALID_VALUE;
+  if ((reinterpret_cast<uintptr_t>(in) & (wide ? 15 : 1)) != 0 ||
+      (reinterpret_cast<uintptr_t>(out_codes) & 15) != 0 ||
+      (reinterpret_cast<uintptr_t>(out_scales) & 3) != 0)
+    return HADACORE_ERROR_MISALIGNED;
+  if (m >= (int64_t(1) << 31)) return HADACORE_ERROR_TOO_LARGE;
+  const int64_t most = (int64_t(1) << 40) / m;
+  if (in_row_stride > most || out_row_stride > most || scales_row_stride > most)
+    return HADACORE_ERROR_TOO_LARGE;
+  if (spans_overlap(span(in, m, in_row_stride, k, 2), span(out_codes, m, out_row_stride, k, 1)) ||
+      spans_overlap(span(in, m, in_row_stride, k, 2),
+                    span(out_scales, m, scales_row_stride, blocks, 4)) ||
+      spans_overlap(span(out_codes, m, out_row_stride, k, 1),
+                    span(out_scales, m, scales_row_stride, blocks, 4)))
+    return HADACORE_ERROR_OVERLAP;
+  const hadacore_status dev = check_device();
+  if (dev != HADACORE_SUCCESS) return dev;
+
+  const uint16_t *src = static_cast<const uint16_t *>(in);
+  uint8_t *codes = static_cast<uint8_t *>(out_codes);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t err = hipSuccess;
+  if (!wide) {
+    err = launch_short_rotations(src, in_row_stride, codes, out_row_stride, out_scales,
+                                 scales_row_stride, m, (int)k, L, dtype, scale, s);
+  } else {
+    const ScaleArgs sc = split_scale(scale, dtype);
+    const auto rows = [&](int64_t at, int64_t in_stride, int64_t out_stride, int64_t scale_stride,
+                          int64_t count) {
+      const QuantOut qo{codes + at, out_stride, out_scales + at / 128, scale_stride};
+      return dtype == HADACORE_FP16
+                 ? launch_blocks<HADACORE_FP16>(L, src + at, in_stride, count, sc, s, qo)
+                 : launch_blocks<HADACORE_BF16>(L, src + at, in_stride, count, sc, s, qo);
+    };
+    if (in_row_stride == k && out_row_stride == k && scales_row_stride == blocks) {
+      // dense: every n values are a row of their own, in one launch
+      err = rows(0, n, n, n / 128, m * (k / n));
+    } else {
+      for (int64_t at = 0; at < k && err == hipSuccess; at += n)
+        err = rows(at, in_row_stride, out_row_stride, scales_row_stride, m);
+    }
+  }
+  return err == hipSuccess ? HADACORE_SUCCESS : HADACORE_ERROR_LAUNCH;
 }
 
 extern "C" hadacore_status hadacore_stream_copy(const void *src, void *dst, int64_t bytes,

@@ -7,9 +7,14 @@ directory; if it is missing, every call raises (there is no fallback).
 The raw entry points take device addresses as integers and keep the C names:
 ``hadamard_transform``, ``hadamard_transform_strided``, ``hadamard_transform_ws``,
 ``hadamard_transform_ws_noalloc``, ``hadamard_transform_workspace_size``, ``hadamard_transform_fp8``,
-``hadamard_transform_int8``, ``hadacore_stream_copy``, ``hadacore_status_string``,
-``hadacore_version``.  ``transform``, ``transform_fp8`` and ``transform_int8`` are
-convenience wrappers for 2-D torch tensors on a ROCm device.
+``hadamard_transform_int8``, ``hadamard_transform_fp8_blocks``, ``hadacore_padded_tokens``,
+``hadacore_quantize_fp8_columns``, ``hadacore_quantize_fp8_tiles``, ``hadacore_matmul_fp8``,
+``hadacore_matmul_fp8_grouped``, ``hadacore_weight_gradient_fp8_grouped``,
+``hadacore_stream_copy``, ``hadacore_status_string``, ``hadacore_version``.  ``transform``,
+``transform_fp8`` and ``transform_int8`` are convenience wrappers for 2-D torch tensors on a
+ROCm device, and so are, for codes with a scale per block of 128, ``transform_fp8_blocks``,
+``quantize_fp8_columns``, ``quantize_fp8_tiles``, ``matmul_fp8``, ``grouped_matmul_fp8`` and
+``grouped_weight_gradient_fp8``.
 """
 from __future__ import annotations
 
@@ -21,6 +26,8 @@ LIBRARY = Path(__file__).resolve().parent / "libhadacore.so"
 
 FP16 = 0
 BF16 = 1
+FP32 = 2  # output of the FP8 products only
+BLOCK = 128  # values that share a scale in the block quantizers and the products
 SUCCESS = 0
 STATUS_NAMES = {
     0: "SUCCESS", 1: "INVALID_VALUE", 2: "INVALID_SIZE", 3: "INVALID_DTYPE",
@@ -30,8 +37,10 @@ STATUS_NAMES = {
 NOALLOC_SCRATCH_BYTES = 32 << 20  # HADACORE_NOALLOC_SCRATCH_BYTES
 EXPORTS = ("hadamard_transform", "hadamard_transform_strided", "hadamard_transform_ws",
            "hadamard_transform_ws_noalloc", "hadamard_transform_workspace_size", "hadamard_transform_fp8",
-           "hadamard_transform_int8", "hadacore_stream_copy", "hadacore_status_string",
-           "hadacore_version")
+           "hadamard_transform_int8", "hadamard_transform_fp8_blocks", "hadacore_padded_tokens",
+           "hadacore_quantize_fp8_columns", "hadacore_quantize_fp8_tiles", "hadacore_matmul_fp8",
+           "hadacore_matmul_fp8_grouped", "hadacore_weight_gradient_fp8_grouped",
+           "hadacore_stream_copy", "hadacore_status_string", "hadacore_version")
 
 
 class HadacoreError(RuntimeError):
@@ -84,6 +93,27 @@ def library() -> ctypes.CDLL:
         lib.hadamard_transform_fp8.restype = i32
         lib.hadamard_transform_int8.argtypes = [vp, i64, vp, i64, vp, i64, i64, i32, f32, vp]
         lib.hadamard_transform_int8.restype = i32
+        lib.hadamard_transform_fp8_blocks.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i64, i32,
+                                                      f32, vp]
+        lib.hadamard_transform_fp8_blocks.restype = i32
+        lib.hadacore_padded_tokens.argtypes = [i64, i64]
+        lib.hadacore_padded_tokens.restype = i64
+        lib.hadacore_quantize_fp8_columns.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, i64,
+                                                      i32, vp]
+        lib.hadacore_quantize_fp8_columns.restype = i32
+        lib.hadacore_quantize_fp8_tiles.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, vp,
+                                                    i64, i64, i64, i64, i64, i32, vp]
+        lib.hadacore_quantize_fp8_tiles.restype = i32
+        lib.hadacore_matmul_fp8.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, i64, i32,
+                                            i64, i64, i64, vp]
+        lib.hadacore_matmul_fp8.restype = i32
+        lib.hadacore_matmul_fp8_grouped.argtypes = [vp, i64, vp, i64, vp, i64, i64, vp, i64, i64, vp,
+                                                    i64, vp, i64, i32, i64, i64, i64, vp]
+        lib.hadacore_matmul_fp8_grouped.restype = i32
+        lib.hadacore_weight_gradient_fp8_grouped.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp,
+                                                             i64, vp, i64, i64, i32, i64, i64, i64,
+                                                             vp]
+        lib.hadacore_weight_gradient_fp8_grouped.restype = i32
         lib.hadacore_stream_copy.argtypes = [vp, vp, i64, vp]
         lib.hadacore_stream_copy.restype = i32
         lib.hadacore_status_string.argtypes = [i32]
@@ -161,6 +191,94 @@ def hadamard_transform_int8(in_ptr: int, in_row_stride: int, codes_ptr: int,
     return st
 
 
+def hadamard_transform_fp8_blocks(in_ptr: int, in_row_stride: int, codes_ptr: int,
+                                  codes_row_stride: int, scales_ptr: int, scales_row_stride: int,
+                                  m: int, k: int, n: int, dtype: int, scale: float,
+                                  stream: int = 0, check: bool = True) -> int:
+    st = library().hadamard_transform_fp8_blocks(in_ptr, in_row_stride, codes_ptr,
+                                                 codes_row_stride, scales_ptr, scales_row_stride,
+                                                 m, k, n, dtype, scale, stream)
+    if check:
+        _check(st, "hadamard_transform_fp8_blocks")
+    return st
+
+
+def hadacore_padded_tokens(tokens: int, groups: int) -> int:
+    return int(library().hadacore_padded_tokens(tokens, groups))
+
+
+def hadacore_quantize_fp8_columns(in_ptr: int, in_row_stride: int, ends_ptr: int, groups: int,
+                                  codes_ptr: int, codes_row_stride: int, scales_ptr: int,
+                                  scales_row_stride: int, m: int, k: int, dtype: int,
+                                  stream: int = 0, check: bool = True) -> int:
+    st = library().hadacore_quantize_fp8_columns(in_ptr, in_row_stride, ends_ptr, groups, codes_ptr,
+                                                 codes_row_stride, scales_ptr, scales_row_stride,
+                                                 m, k, dtype, stream)
+    if check:
+        _check(st, "hadacore_quantize_fp8_columns")
+    return st
+
+
+def hadacore_quantize_fp8_tiles(in_ptr: int, in_row_stride: int, in_batch_stride: int,
+                                codes_ptr: int, codes_row_stride: int, codes_batch_stride: int,
+                                codes_t_ptr: int, codes_t_row_stride: int,
+                                codes_t_batch_stride: int, scales_ptr: int,
+                                scales_row_stride: int, scales_batch_stride: int, batch: int,
+                                m: int, k: int, dtype: int, stream: int = 0,
+                                check: bool = True) -> int:
+    st = library().hadacore_quantize_fp8_tiles(
+        in_ptr, in_row_stride, in_batch_stride, codes_ptr, codes_row_stride, codes_batch_stride,
+        codes_t_ptr, codes_t_row_stride, codes_t_batch_stride, scales_ptr, scales_row_stride,
+        scales_batch_stride, batch, m, k, dtype, stream)
+    if check:
+        _check(st, "hadacore_quantize_fp8_tiles")
+    return st
+
+
+def hadacore_matmul_fp8(a_ptr: int, a_row_stride: int, a_scales_ptr: int, a_scales_row_stride: int,
+                        b_ptr: int, b_row_stride: int, b_scales_ptr: int, b_scales_row_stride: int,
+                        b_scale_rows: int, out_ptr: int, out_row_stride: int, out_dtype: int,
+                        m: int, n: int, k: int, stream: int = 0, check: bool = True) -> int:
+    st = library().hadacore_matmul_fp8(a_ptr, a_row_stride, a_scales_ptr, a_scales_row_stride,
+                                       b_ptr, b_row_stride, b_scales_ptr, b_scales_row_stride,
+                                       b_scale_rows, out_ptr, out_row_stride, out_dtype, m, n, k,
+                                       stream)
+    if check:
+        _check(st, "hadacore_matmul_fp8")
+    return st
+
+
+def hadacore_matmul_fp8_grouped(a_ptr: int, a_row_stride: int, a_scales_ptr: int,
+                                a_scales_row_stride: int, b_ptr: int, b_row_stride: int,
+                                b_batch_stride: int, b_scales_ptr: int, b_scales_row_stride: int,
+                                b_scales_batch_stride: int, ends_ptr: int, groups: int,
+                                out_ptr: int, out_row_stride: int, out_dtype: int, m: int, n: int,
+                                k: int, stream: int = 0, check: bool = True) -> int:
+    st = library().hadacore_matmul_fp8_grouped(
+        a_ptr, a_row_stride, a_scales_ptr, a_scales_row_stride, b_ptr, b_row_stride,
+        b_batch_stride, b_scales_ptr, b_scales_row_stride, b_scales_batch_stride, ends_ptr, groups,
+        out_ptr, out_row_stride, out_dtype, m, n, k, stream)
+    if check:
+        _check(st, "hadacore_matmul_fp8_grouped")
+    return st
+
+
+def hadacore_weight_gradient_fp8_grouped(a_ptr: int, a_row_stride: int, a_scales_ptr: int,
+                                         a_scales_row_stride: int, b_ptr: int, b_row_stride: int,
+                                         b_scales_ptr: int, b_scales_row_stride: int,
+                                         ends_ptr: int, groups: int, out_ptr: int,
+                                         out_row_stride: int, out_batch_stride: int,
+                                         out_dtype: int, places: int, n: int, k: int,
+                                         stream: int = 0, check: bool = True) -> int:
+    st = library().hadacore_weight_gradient_fp8_grouped(
+        a_ptr, a_row_stride, a_scales_ptr, a_scales_row_stride, b_ptr, b_row_stride, b_scales_ptr,
+        b_scales_row_stride, ends_ptr, groups, out_ptr, out_row_stride, out_batch_stride,
+        out_dtype, places, n, k, stream)
+    if check:
+        _check(st, "hadacore_weight_gradient_fp8_grouped")
+    return st
+
+
 def hadacore_stream_copy(src_ptr: int, dst_ptr: int, nbytes: int, stream: int = 0,
                          check: bool = True) -> int:
     st = library().hadacore_stream_copy(src_ptr, dst_ptr, nbytes, stream)
@@ -182,6 +300,8 @@ def hadacore_version() -> int:
 # device contexts were half.
 _torch = None
 _dtype_codes: dict = {}
+_out_codes: dict = {}
+_code_types: tuple = ()
 _raw_stream = None
 _current_device = None
 _one_device = False
@@ -190,9 +310,11 @@ _SCALES = {1 << k: float(ctypes.c_float(1.0 / math.sqrt(1 << k)).value) for k in
 
 
 def _init_torch() -> None:
-    global _torch, _raw_stream, _current_device, _one_device
+    global _torch, _raw_stream, _current_device, _one_device, _code_types
     import torch
     _dtype_codes.update({torch.float16: FP16, torch.bfloat16: BF16})
+    _out_codes.update({torch.float16: FP16, torch.bfloat16: BF16, torch.float32: FP32})
+    _code_types = (torch.uint8, torch.float8_e4m3fn)
     _current_device = torch.cuda.current_device
     _one_device = torch.cuda.device_count() == 1
     # the current stream's handle without building a Stream object
@@ -327,3 +449,288 @@ def transform_int8(x, codes=None, scales=None, scale: float | None = None, strea
     tensor, so that x @ H_n * scale ~ codes.float() * scales[:, None].
     """
     return _transform_quantized(x, codes, scales, scale, stream, "hadamard_transform_int8", True)
+
+
+# ---- e4m3 codes with a scale for each block of 128, and their products ----------
+
+
+def _stream_of(stream, device: int):
+    if stream is None:
+        return _raw_stream(device)
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
+
+
+def _padded_rows(shape: tuple, device):
+    """A uint8 tensor whose rows start on 16-byte boundaries and are readable, as zeros,
+    up to the next one: what the quantizers write and the products read."""
+    k = shape[-1]
+    if k % 16 == 0:
+        return _torch.empty(shape, dtype=_torch.uint8, device=device)
+    # whole rows are cleared, a copy of 1/3 of the quantizer's bytes, for odd sizes only
+    return _torch.zeros((*shape[:-1], -(-k // 16) * 16), dtype=_torch.uint8,
+                        device=device)[..., :k]
+
+
+def _check_codes(name: str, codes, scales, dim: int, rows: int, device: int):
+    """Codes and scales of a product's operand: types, devices, unit column strides, the
+    shape of the scales (``rows`` of them) and that every row of codes is readable up to
+    the next multiple of 16 bytes."""
+    if codes.dtype not in _code_types:
+        raise TypeError(f"{name}: codes must be uint8 or float8_e4m3fn, got {codes.dtype}")
+    if scales.dtype != _torch.float32:
+        raise TypeError(f"{name}: scales must be float32, got {scales.dtype}")
+    if codes.dim() != dim or scales.dim() != dim:
+        raise ValueError(f"{name}: expected {dim}-D codes and scales")
+    if codes.get_device() != device or scales.get_device() != device:
+        raise ValueError(f"{name}: all tensors must be on the same ROCm device")
+    k = codes.shape[-1]
+    want = (*codes.shape[:-2], rows, (k + 127) // 128)
+    if tuple(scales.shape) != want:
+        raise ValueError(f"{name}: expected scales of shape {want}, got {tuple(scales.shape)}")
+    if (k > 1 and codes.stride(-1) != 1) or (want[-1] > 1 and scales.stride(-1) != 1):
+        raise ValueError(f"{name}: rows must be contiguous (column stride 1)")
+    if k % 16 and codes.numel():
+        last = sum((n - 1) * s for n, s in zip(codes.shape[:-1], codes.stride()))
+        if codes.storage_offset() + last + (k + 15) // 16 * 16 > codes.untyped_storage().nbytes():
+            raise ValueError(f"{name}: the last row of codes must be readable up to a multiple of "
+                             "16 bytes (as the quantizers allocate it)")
+
+
+def _row_stride(t, least: int) -> int:
+    """The row stride; of a single row, whose stride is never used, one that passes."""
+    return t.stride(-2) if t.shape[-2] > 1 else least
+
+
+def _pitch(codes) -> int:
+    """The row stride of codes (of a single row: its padded length; of empty rows 0)."""
+    if codes.shape[-1] == 0:
+        return 0
+    return codes.stride(-2) if codes.shape[-2] > 1 else -(-codes.shape[-1] // 16) * 16
+
+
+def _new_scales(scales, shape: tuple, device):
+    if scales is None:
+        return _torch.empty(shape, dtype=_torch.float32, device=device)
+    if scales.dtype != _torch.float32 or tuple(scales.shape) != shape or scales.device != device \
+            or (shape[-1] > 1 and scales.stride(-1) != 1):
+        raise ValueError(f"scales must be a {shape} float32 tensor with contiguous rows")
+    return scales
+
+
+def _new_codes(codes, shape: tuple, device):
+    if codes is None:
+        return _padded_rows(shape, device)
+    if codes.dtype not in _code_types or tuple(codes.shape) != shape or codes.device != device \
+            or (shape[-1] > 1 and codes.stride(-1) != 1):
+        raise ValueError(f"codes must be a {shape} uint8 tensor with contiguous rows")
+    return codes
+
+
+def transform_fp8_blocks(x, n: int | None = None, codes=None, scales=None,
+                         scale: float | None = None, stream=None):
+    """Rotate each row of a 2-D float16/bfloat16 tensor in blocks of ``n`` and quantize it to
+    e4m3 with one scale for every 128 columns.
+
+    ``n`` is a power of two up to 32768 that divides the columns (default: all of them; 1:
+    no rotation) and ``scale`` defaults to fp32(1/sqrt(n)).  Returns (codes, scales): (m, k)
+    uint8 and (m, ceil(k / 128)) float32, the operand that ``matmul_fp8`` takes:
+    (x.view(m, -1, n) @ H_n * scale).view(m, k) ~ codes * scales, a scale per 128 columns.
+    """
+    if _torch is None:
+        _init_torch()
+    if x.dim() != 2 or not x.is_cuda:
+        raise ValueError("expected a 2-D tensor on a ROCm device")
+    m, k = x.shape
+    if k > 1 and x.stride(1) != 1:
+        raise ValueError("rows must be contiguous (column stride 1)")
+    code = _dtype_code(x)
+    n = max(k, 1) if n is None else int(n)
+    codes = _new_codes(codes, (m, k), x.device)
+    scales = _new_scales(scales, (m, (k + 127) // 128), x.device)
+    if scale is None:
+        scale = _default_scale(n)
+    device = x.get_device()
+    _call("hadamard_transform_fp8_blocks", device, x.data_ptr(), x.stride(0) if m > 1 else k,
+          codes.data_ptr(), _pitch(codes), scales.data_ptr(), _row_stride(scales, scales.shape[1]),
+          m, k, n, code, scale, _stream_of(stream, device))
+    return codes, scales
+
+
+def _check_ends(ends, device: int) -> None:
+    if ends.dtype != _torch.int32 or ends.dim() != 1 or not ends.is_contiguous():
+        raise ValueError("ends must be a contiguous 1-D int32 tensor: the end of each group")
+    if ends.get_device() != device:
+        raise ValueError("ends must be on the same ROCm device")
+
+
+def quantize_fp8_columns(x, ends=None, codes=None, scales=None, stream=None):
+    """Quantize the columns of a 2-D float16/bfloat16 tensor (tokens x features) to
+    transposed e4m3 codes with one scale for every 128 tokens: the operands of
+    ``grouped_weight_gradient_fp8``.
+
+    ``ends`` (int32, on the device) holds the end of each group of tokens; None is one
+    group.  Each group is padded with zeros to a multiple of 128 places.  Returns (codes,
+    scales): (k, p) uint8 and (k, p / 128) float32 with p =
+    hadacore_padded_tokens(tokens, groups).
+    """
+    if _torch is None:
+        _init_torch()
+    if x.dim() != 2 or not x.is_cuda:
+        raise ValueError("expected a 2-D tensor on a ROCm device")
+    m, k = x.shape
+    if k > 1 and x.stride(1) != 1:
+        raise ValueError("rows must be contiguous (column stride 1)")
+    code = _dtype_code(x)
+    device = x.get_device()
+    if ends is not None:
+        _check_ends(ends, device)
+    groups = 1 if ends is None else ends.numel()
+    places = hadacore_padded_tokens(m, groups)
+    codes = _new_codes(codes, (k, places), x.device)
+    scales = _new_scales(scales, (k, places // 128), x.device)
+    _call("hadacore_quantize_fp8_columns", device, x.data_ptr(), x.stride(0) if m > 1 else k,
+          None if ends is None else ends.data_ptr(), groups, codes.data_ptr(), _pitch(codes),
+          scales.data_ptr(), _row_stride(scales, scales.shape[1]), m, k, code,
+          _stream_of(stream, device))
+    return codes, scales
+
+
+def quantize_fp8_tiles(w, transposed: bool = False, stream=None):
+    """Quantize float16/bfloat16 weights (n x k, or experts x n x k) to e4m3 with one scale
+    for every tile of 128 x 128.
+
+    Returns (codes, scales), codes of w's shape and scales ceil(n / 128) x ceil(k / 128) for
+    each matrix; with ``transposed`` (codes, scales, codes_t), where codes_t holds the same
+    codes as k x n matrices, whose scales are ``scales.transpose(-1, -2).contiguous()``.
+    """
+    if _torch is None:
+        _init_torch()
+    if w.dim() not in (2, 3) or not w.is_cuda:
+        raise ValueError("expected a 2-D or 3-D tensor on a ROCm device")
+    n, k = w.shape[-2:]
+    if k > 1 and w.stride(-1) != 1:
+        raise ValueError("rows must be contiguous (column stride 1)")
+    code = _dtype_code(w)
+    lead = tuple(w.shape[:-2])
+    batch = lead[0] if lead else 1
+    codes = _padded_rows((*lead, n, k), w.device)
+    codes_t = _padded_rows((*lead, k, n), w.device) if transposed else None
+    scales = _torch.empty((*lead, (n + 127) // 128, (k + 127) // 128), dtype=_torch.float32,
+                          device=w.device)
+    device = w.get_device()
+
+    def step(t):
+        return t.stride(0) if lead else 0
+
+    _call("hadacore_quantize_fp8_tiles", device, w.data_ptr(), w.stride(-2) if n > 1 else k,
+          step(w), codes.data_ptr(), _pitch(codes), step(codes),
+          codes_t.data_ptr() if transposed else None, _pitch(codes_t) if transposed else 0,
+          step(codes_t) if transposed else 0, scales.data_ptr(), scales.stride(-2), step(scales),
+          batch, n, k, code, _stream_of(stream, device))
+    return (codes, scales, codes_t) if transposed else (codes, scales)
+
+
+def _product_out(out, shape: tuple, dtype, like):
+    """The output of a product and its type's code."""
+    if out is None:
+        out = _torch.empty(shape, dtype=dtype or _torch.bfloat16, device=like.device)
+    elif tuple(out.shape) != shape or out.device != like.device or \
+            (shape[-1] > 1 and out.stride(-1) != 1) or (dtype is not None and out.dtype != dtype):
+        raise ValueError(f"out must be a {shape} tensor of the output type with contiguous rows")
+    code = _out_codes.get(out.dtype)
+    if code is None:
+        raise TypeError(f"expected an output of float16, bfloat16 or float32, got {out.dtype}")
+    return out, code
+
+
+def matmul_fp8(a, a_scales, b, b_scales, out=None, dtype=None, stream=None):
+    """out = A @ B^T for e4m3 codes with a scale for each block of 128.
+
+    ``a`` (m x k) and ``a_scales`` (m x ceil(k / 128)) are as ``transform_fp8_blocks`` gives
+    them.  ``b`` (n x k) has a scale per tile of 128 x 128 (``quantize_fp8_tiles``) or one per
+    row and 128 columns, told apart by the rows of ``b_scales``.  ``dtype`` is the output's:
+    bfloat16 (default), float16 or float32.  Sums are in 32 bits, rounded once.
+    """
+    if _torch is None:
+        _init_torch()
+    if not a.is_cuda or a.dim() != 2 or b.dim() != 2:
+        raise ValueError("expected 2-D tensors on a ROCm device")
+    device = a.get_device()
+    m, k = a.shape
+    n = b.shape[0]
+    if b.shape[1] != k:
+        raise ValueError(f"a has {k} columns and b {b.shape[1]}")
+    tiles = (n + 127) // 128
+    by_row = b_scales.dim() == 2 and b_scales.shape[0] == n and n != tiles
+    _check_codes("a", a, a_scales, 2, m, device)
+    _check_codes("b", b, b_scales, 2, n if by_row else tiles, device)
+    out, code = _product_out(out, (m, n), dtype, a)
+    blocks = (k + 127) // 128
+    _call("hadacore_matmul_fp8", device, a.data_ptr(), _pitch(a), a_scales.data_ptr(),
+          _row_stride(a_scales, blocks), b.data_ptr(), _pitch(b), b_scales.data_ptr(),
+          _row_stride(b_scales, blocks), 1 if by_row else 128, out.data_ptr(),
+          _row_stride(out, n), code, m, n, k, _stream_of(stream, device))
+    return out
+
+
+def grouped_matmul_fp8(a, a_scales, b, b_scales, ends, out=None, dtype=None, stream=None):
+    """``matmul_fp8`` with a weight of its own for each group of rows (tokens by expert).
+
+    The rows of ``a`` (m x k) are sorted by group and ``ends`` (int32, on the device) holds
+    the end of each group, which may be empty; ``b`` is groups x n x k with a scale per tile
+    of 128 x 128.  Row i of group g gets a[i] @ b[g]^T; rows after the last end get zeros.
+    """
+    if _torch is None:
+        _init_torch()
+    if not a.is_cuda or a.dim() != 2 or b.dim() != 3:
+        raise ValueError("expected a 2-D and a 3-D tensor on a ROCm device")
+    device = a.get_device()
+    m, k = a.shape
+    groups, n = b.shape[:2]
+    if b.shape[2] != k:
+        raise ValueError(f"a has {k} columns and b {b.shape[2]}")
+    _check_ends(ends, device)
+    if ends.numel() != groups:
+        raise ValueError(f"{ends.numel()} ends for {groups} groups")
+    _check_codes("a", a, a_scales, 2, m, device)
+    _check_codes("b", b, b_scales, 3, (n + 127) // 128, device)
+    out, code = _product_out(out, (m, n), dtype, a)
+    blocks = (k + 127) // 128
+    _call("hadacore_matmul_fp8_grouped", device, a.data_ptr(), _pitch(a), a_scales.data_ptr(),
+          _row_stride(a_scales, blocks), b.data_ptr(), _pitch(b), b.stride(0), b_scales.data_ptr(),
+          _row_stride(b_scales, blocks), b_scales.stride(0), ends.data_ptr(), groups,
+          out.data_ptr(), _row_stride(out, n), code, m, n, k, _stream_of(stream, device))
+    return out
+
+
+def grouped_weight_gradient_fp8(dy, dy_scales, x, x_scales, ends=None, out=None, dtype=None,
+                                stream=None):
+    """The weight gradients of ``grouped_matmul_fp8``: for each group, dy^T x over its tokens.
+
+    ``dy`` (n x places) and ``x`` (k x places) are the transposed codes that
+    ``quantize_fp8_columns`` gives for the output's gradient and the input, with the same
+    ``ends``; a group without tokens gets zeros.  ``ends=None`` is one group of all places.
+    Returns groups x n x k, or n x k without ends.
+    """
+    if _torch is None:
+        _init_torch()
+    if not dy.is_cuda or dy.dim() != 2 or x.dim() != 2:
+        raise ValueError("expected 2-D tensors on a ROCm device")
+    device = dy.get_device()
+    n, places = dy.shape
+    k = x.shape[0]
+    if x.shape[1] != places:
+        raise ValueError(f"dy has {places} places and x {x.shape[1]}")
+    _check_codes("dy", dy, dy_scales, 2, n, device)
+    _check_codes("x", x, x_scales, 2, k, device)
+    if ends is not None:
+        _check_ends(ends, device)
+    groups = 1 if ends is None else ends.numel()
+    out, code = _product_out(out, (n, k) if ends is None else (groups, n, k), dtype, dy)
+    blocks = places // 128
+    _call("hadacore_weight_gradient_fp8_grouped", device, dy.data_ptr(), _pitch(dy),
+          dy_scales.data_ptr(), _row_stride(dy_scales, blocks), x.data_ptr(), _pitch(x),
+          x_scales.data_ptr(), _row_stride(x_scales, blocks),
+          None if ends is None else ends.data_ptr(), groups, out.data_ptr(), _row_stride(out, k),
+          0 if ends is None else out.stride(0), code, places, n, k, _stream_of(stream, device))
+    return out

@@ -1,0 +1,484 @@
+"""Codes with a scale per block of 128, and their products, on the GPU against 64 bits."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+import blocks_reference as R
+from paper_2412_08832_amd import hadacore as H
+from paper_2412_08832_amd import workloads as W
+from gpu_util import to_device
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = ["fp16", "bf16"]
+OUTS = ["bf16", "fp16", "fp32"]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _device():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a ROCm device"
+    H.library()
+    yield
+    torch.cuda.synchronize()
+
+
+def _torch_type(out):
+    import torch
+    return {"fp16": torch.float16, "bf16": torch.bfloat16, "fp32": torch.float32}[out]
+
+
+def _host(t):
+    return t.float().cpu().numpy() if t.is_floating_point() else t.cpu().numpy()
+
+
+def _decode(bits, dtype):
+    if dtype == "fp16":
+        return bits.view(np.float16).astype(np.float64)
+    return (bits.astype(np.uint32) << 16).view(np.float32).astype(np.float64)
+
+
+def _hadamard_rows(y, n):
+    """Each n columns of y (64 bits) times H_n, by butterflies."""
+    m, k = y.shape
+    y = y.reshape(-1, n)
+    h = 1
+    while h < n:
+        v = y.reshape(-1, n // (2 * h), 2, h)
+        y = np.stack((v[:, :, 0] + v[:, :, 1], v[:, :, 0] - v[:, :, 1]), axis=2).reshape(-1, n)
+        h *= 2
+    return y.reshape(m, k)
+
+
+# ---- rows -------------------------------------------------------------------------
+
+
+def _rows_case(dtype, m, k, n, gap=0, codes_gap=0, scales_gap=0, bits=None, scale=None):
+    import torch
+    if bits is None:
+        bits = W.random_rows(m, k, dtype, seed=k + m, stride=k + gap)
+        bits[:, 5 % k] = W.round_to_bits(np.full(m, 60.0, np.float32), dtype)
+    x = to_device(bits, dtype)[:, :k]
+    blocks = -(-k // 128)
+    pitch = -(-(k + codes_gap) // 16) * 16
+    codes = torch.full((m, pitch), 0xA5, dtype=torch.uint8, device="cuda")
+    scales = torch.full((m, blocks + scales_gap), -7.0, device="cuda")
+    H.transform_fp8_blocks(x, n=n, codes=codes[:, :k], scales=scales[:, :blocks], scale=scale)
+    torch.cuda.synchronize()
+    codes, scales = codes.cpu().numpy(), scales.cpu().numpy()
+    assert (codes[:, k:] == 0xA5).all() and (scales[:, blocks:] == -7.0).all()
+    s = W.default_scale(n) if scale is None else scale
+    values = _decode(bits[:, :k], dtype) * s
+    y = _hadamard_rows(values, n)
+    # rows whose sums pass the largest fp32 from finite values: the sums that overflow on
+    # the way depend on their order, so only the scales of the blocks that do are known
+    over = np.isfinite(values).all(axis=1) & (np.abs(y) > np.finfo(np.float32).max).any(axis=1)
+    for row in np.nonzero(over)[0]:
+        hit = (R.pad_to(np.abs(y[row:row + 1]), 1, 128) > np.finfo(np.float32).max)
+        assert np.isinf(scales[row, :blocks][hit.reshape(-1, 128).any(axis=1)]).all()
+    R.check_rows(y[~over], codes[~over, :k], scales[~over, :blocks], f"{dtype} {m}x{k} n={n}")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,k,m", [
+    (1, 1, 1), (1, 127, 3), (1, 128, 2), (1, 129, 5), (1, 1001, 17), (1, 4096, 3), (2, 130, 7),
+    (4, 252, 3), (8, 136, 9), (16, 400, 5), (32, 32, 33), (64, 64, 1), (64, 192, 70), (64, 4160, 3)])
+def test_rows_short_rotations(dtype, n, k, m):
+    _rows_case(dtype, m, k, n)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("L", range(7, 16))
+@pytest.mark.parametrize("m,per", [(1, 1), (5, 1), (3, 3), (17, 2)])
+def test_rows_every_rotation(dtype, L, m, per):
+    _rows_case(dtype, m, per << L, 1 << L)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,k", [(1, 301), (32, 288), (128, 384), (256, 512), (1024, 5120),
+                                 (8192, 8192)])
+def test_rows_strided(dtype, n, k):
+    """Rows with gaps on either side, codes and scales inside wider buffers."""
+    _rows_case(dtype, 9, k, n, gap=8, codes_gap=16, scales_gap=3)
+    _rows_case(dtype, 4, k, n, gap=0, codes_gap=0, scales_gap=1)
+    if n < 128:
+        _rows_case(dtype, 6, k, n, gap=3)  # rows at odd addresses
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [1, 64, 128, 512, 4096])
+def test_rows_special_values(dtype, n):
+    """Zero blocks, Inf and NaN, values near the end of the type; a negative scale."""
+    k, m = max(n, 256), 6
+    bits = W.random_rows(m, k, dtype, seed=n)
+    bits[0] = 0
+    bits[1, :128] = 0
+    inf, nan = (0x7C00, 0x7E00) if dtype == "fp16" else (0x7F80, 0x7FC0)
+    bits[2, 3] = inf
+    bits[3, 130] = nan
+    bits[4] = W.round_to_bits(np.full(k, 6e4 if dtype == "fp16" else 3e38, np.float32), dtype)
+    bits[4, ::2] ^= 0x8000
+    bits[5] = 1  # the smallest subnormal
+    _rows_case(dtype, m, k, n, bits=bits)
+    _rows_case(dtype, 1, k, n, bits=bits[:1].copy(), scale=-0.5)
+    _rows_case(dtype, 1, k, n, bits=W.random_rows(1, k, dtype, seed=3), scale=-0.37)
+
+
+def test_rows_no_rows_and_defaults():
+    import torch
+    codes, scales = H.transform_fp8_blocks(torch.empty((0, 256), dtype=torch.float16, device="cuda"))
+    assert codes.shape == (0, 256) and scales.shape == (0, 2)
+    x = torch.randn(3, 4096, device="cuda").to(torch.bfloat16)
+    one, two = H.transform_fp8_blocks(x), H.transform_fp8_blocks(x, n=4096)
+    assert all(torch.equal(p, q) for p, q in zip(one, two))  # the whole row; repeatable
+    odd, _ = H.transform_fp8_blocks(x[:, :4001].contiguous(), n=1)
+    # what the products read past a row's end lies in the tensor's storage
+    assert odd.stride(0) % 16 == 0 and odd.untyped_storage().nbytes() >= 3 * odd.stride(0)
+
+
+def test_rows_agree_with_one_block_rows():
+    """n = 128 with one block to a row is the per-row quantizer's result, bit for bit."""
+    import torch
+    x = torch.randn(1000, 128, device="cuda").to(torch.float16)
+    codes, scales = H.transform_fp8_blocks(x)
+    want, want_scales = H.transform_fp8(x)
+    assert torch.equal(codes, want) and torch.equal(scales[:, 0], want_scales)
+
+
+# ---- columns and tiles -----------------------------------------------------------
+
+
+def _ends(ends):
+    import torch
+    return torch.tensor(ends, dtype=torch.int32, device="cuda")
+
+
+GROUPS = [
+    (1, [1]), (300, [300]), (300, [0, 300]), (257, [128, 128, 256, 257]), (500, [1, 2, 131, 131, 500]),
+    (40, [3, 10, 10, 10]),  # tokens after the last end
+    (200, [0] * 70 + [100] * 30 + [200] * 30),  # more groups than lanes
+    (7, [0, 0, 0])]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("k,gap", [(1, 0), (77, 0), (128, 8), (264, 3)])
+@pytest.mark.parametrize("tokens,ends", GROUPS)
+def test_columns(dtype, k, gap, tokens, ends):
+    import torch
+    bits = W.random_rows(tokens, k, dtype, seed=tokens + k, stride=k + gap)
+    bits[:, k // 2] = 0
+    codes, scales = H.quantize_fp8_columns(to_device(bits, dtype)[:, :k], _ends(ends))
+    torch.cuda.synchronize()
+    groups, places = R.padded_places(ends, tokens)
+    assert codes.shape == (k, places) and scales.shape == (k, places // 128)
+    x = _decode(bits[:, :k], dtype)
+    y = np.zeros((k, places))
+    for _, low, n, at, _ in groups:
+        y[:, at:at + n] = x[low:low + n].T
+    R.check_rows(y, codes.cpu().numpy(), scales.cpu().numpy(), f"{tokens} {ends}")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_columns_without_groups_and_special_values(dtype):
+    import torch
+    bits = W.random_rows(200, 40, dtype, seed=5)
+    inf, nan = (0x7C00, 0x7E00) if dtype == "fp16" else (0x7F80, 0x7FC0)
+    bits[3, 0], bits[150, 1], bits[:, 2] = inf, nan, nan
+    codes, scales = H.quantize_fp8_columns(to_device(bits, dtype))
+    assert codes.shape == (40, 256)
+    y = np.zeros((40, 256))
+    y[:, :200] = _decode(bits, dtype).T
+    y[2, 200:] = np.nan  # a block of NaN and padding: amax is 0, and the padding's codes 0
+    got, s = codes.cpu().numpy(), scales.cpu().numpy()
+    assert s[2, 1] == 0 and (got[2, 200:] == 0).all() and np.isnan(s[2, 0])
+    keep = np.arange(40) != 2
+    R.check_rows(y[keep], got[keep], s[keep])
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape,gap", [((1, 1), 0), ((128, 128), 0), ((100, 300), 0), ((257, 129), 5),
+                                       ((3, 130, 65), 0), ((2, 64, 1000), 8), ((5, 384, 256), 0)])
+def test_tiles(dtype, shape, gap):
+    import torch
+    *lead, n, k = shape
+    batch = lead[0] if lead else 1
+    bits = W.random_rows(batch * n, k, dtype, seed=n + k, stride=k + gap)
+    bits[0, :] = 0
+    w = to_device(bits, dtype).view(*lead, n, k + gap)[..., :k]
+    codes, scales, codes_t = H.quantize_fp8_tiles(w, transposed=True)
+    again, again_scales = H.quantize_fp8_tiles(w)
+    assert torch.equal(codes, again) and torch.equal(scales, again_scales)
+    assert torch.equal(codes.transpose(-1, -2), codes_t)
+    x = _decode(bits[:, :k], dtype).reshape(batch, n, k)
+    c = codes.cpu().numpy().reshape(batch, n, k)
+    s = scales.cpu().numpy().reshape(batch, -1, scales.shape[-1])
+    for e in range(batch):
+        R.check_tiles(x[e], c[e], s[e], f"{shape} matrix {e}")
+
+
+def test_tiles_zero_and_padding():
+    import torch
+    w = torch.zeros((130, 200), dtype=torch.bfloat16, device="cuda")
+    codes, scales = H.quantize_fp8_tiles(w)
+    assert int(codes.sum()) == 0 and float(scales.sum()) == 0
+    assert H.quantize_fp8_tiles(w[:0])[0].shape == (0, 200)
+
+
+# ---- products --------------------------------------------------------------------
+
+
+def _codes(rng, rows, k, pad=0, fill=0x7F, scale_rows=None, spread=1.0):
+    """Codes (padded with NaN codes up to the pitch) and scales on the GPU, and on the host."""
+    import torch
+    pitch = -(-k // 16) * 16 + pad
+    buf = np.full((rows, pitch), fill, np.uint8)
+    v = rng.standard_normal((rows, k)) * 120 * spread
+    buf[:, :k] = _encode(v)
+    scales = np.exp2(rng.uniform(-6, 2, (rows if scale_rows is None else scale_rows,
+                                         -(-k // 128)))).astype(np.float32)
+    return (torch.from_numpy(buf).cuda()[:, :k], torch.from_numpy(scales).cuda(), buf[:, :k], scales)
+
+
+def _encode(v):
+    """Nearest e4m3 code (ties as they come: these are inputs)."""
+    order = np.argsort(R.VALUES[np.r_[0:127]])
+    pos = R.VALUES[order]
+    at = np.searchsorted((pos[1:] + pos[:-1]) / 2, np.minimum(np.abs(v), 448))
+    return (order[at] | np.where(v < 0, 128, 0)).astype(np.uint8)
+
+
+SIZES = [(1, 1, 1), (1, 64, 128), (2, 5, 15), (3, 130, 16), (15, 33, 127), (16, 64, 129), (17, 257, 300),
+         (33, 128, 512), (64, 96, 640), (65, 64, 256), (100, 300, 1000), (128, 128, 128),
+         (129, 129, 257), (200, 513, 384), (300, 260, 1155), (1, 1000, 4096), (7, 515, 2049),
+         (513, 640, 200), (1, 17, 16000), (40, 48, 9000), (800, 1030, 144)]
+
+
+@pytest.mark.parametrize("out", OUTS)
+@pytest.mark.parametrize("tall", [128, 1])
+@pytest.mark.parametrize("m,n,k", SIZES)
+def test_matmul(m, n, k, tall, out):
+    import torch
+    rng = np.random.default_rng(m * 7 + n * 3 + k)
+    a, sa, ha, hsa = _codes(rng, m, k)
+    b, sb, hb, hsb = _codes(rng, n, k, pad=32, scale_rows=-(-n // tall), spread=0.05 / k ** 0.5)
+    y = H.matmul_fp8(a, sa, b, sb, dtype=_torch_type(out))
+    torch.cuda.synchronize()
+    R.check_product(ha, hsa, hb, hsb, _host(y), out, tall if n != -(-n // 128) else 128,
+                    f"{m}x{n}x{k} {out} {tall}")
+
+
+@pytest.mark.parametrize("out", OUTS)
+@pytest.mark.parametrize("m,n,gap,first", [(5, 100, 28, 0), (70, 130, 5, 0), (130, 200, 8, 8), (33, 64, 0, 1)])
+def test_matmul_into_a_wider_buffer(m, n, gap, first, out):
+    """Row gaps, and starts and pitches off 16 bytes, are left alone and change nothing."""
+    import torch
+    rng = np.random.default_rng(m + n)
+    a, sa, ha, hsa = _codes(rng, m, 260)
+    b, sb, hb, hsb = _codes(rng, n, 260, scale_rows=-(-n // 128), spread=0.01)
+    buf = torch.full((m * (n + gap) + first,), 7.0, dtype=_torch_type(out), device="cuda")
+    view = buf[first:].view(m, n + gap)
+    y = H.matmul_fp8(a, sa, b, sb, out=view[:, :n])
+    assert y.data_ptr() == view.data_ptr()
+    R.check_product(ha, hsa, hb, hsb, _host(y), out)
+    assert (_host(view[:, n:]) == 7).all() and (_host(buf[:first]) == 7).all()
+
+
+def test_matmul_nothing_to_add():
+    import torch
+    z = torch.zeros
+    a, b = z((5, 0), dtype=torch.uint8, device="cuda"), z((9, 0), dtype=torch.uint8, device="cuda")
+    sa, sb = z((5, 0), device="cuda"), z((1, 0), device="cuda")
+    y = H.matmul_fp8(a, sa, b, sb, out=torch.full((5, 9), 3.0, dtype=torch.bfloat16, device="cuda"))
+    assert (y == 0).all()
+    a, sa = z((0, 64), dtype=torch.uint8, device="cuda"), z((0, 1), device="cuda")
+    b, sb = z((9, 64), dtype=torch.uint8, device="cuda"), z((1, 1), device="cuda")
+    assert H.matmul_fp8(a, sa, b, sb).shape == (0, 9)
+    assert H.matmul_fp8(b, z((9, 1), device="cuda"), a, z((0, 1), device="cuda")).shape == (9, 0)
+
+
+@pytest.mark.parametrize("m", [1, 20, 200])
+@pytest.mark.parametrize("out", OUTS)
+def test_matmul_nan_and_inf_stay_in_their_row(m, out):
+    """A NaN code or scale reaches the outputs of its row or column only."""
+    import torch
+    rng = np.random.default_rng(11)
+    a, sa, _, _ = _codes(rng, m, 300)
+    b, sb, _, _ = _codes(rng, 150, 300, scale_rows=2, spread=0.01)
+    clean = H.matmul_fp8(a, sa, b, sb, dtype=_torch_type(out))
+    b[7, 299] = 0x7F
+    sb[1, 0] = float("nan")
+    got = H.matmul_fp8(a, sa, b, sb, dtype=_torch_type(out))
+    bad = torch.zeros(150, dtype=torch.bool, device="cuda")
+    bad[7] = True
+    bad[128:] = True
+    assert torch.isnan(got[:, bad]).all() and torch.equal(got[:, ~bad], clean[:, ~bad])
+    sb[1, 0] = 1.0
+    sa[m - 1, 1] = float("inf")
+    got = H.matmul_fp8(a, sa, b, sb, dtype=_torch_type(out))
+    assert not torch.isfinite(got[m - 1]).any()
+    ok = torch.arange(150, device="cuda") < 128
+    ok[7] = False
+    assert torch.equal(got[: m - 1, ok], clean[: m - 1, ok])
+
+
+@pytest.mark.parametrize("out", OUTS)
+@pytest.mark.parametrize("n,k", [(64, 128), (130, 300), (257, 1030)])
+@pytest.mark.parametrize("tokens,ends", GROUPS + [(1000, [500, 500, 990, 1000])])
+def test_grouped(tokens, ends, n, k, out):
+    import torch
+    rng = np.random.default_rng(tokens + n + k)
+    groups = len(ends)
+    a, sa, ha, hsa = _codes(rng, tokens, k, pad=16)
+    parts = [_codes(rng, n, k, scale_rows=-(-n // 128), spread=0.05 / k ** 0.5)
+             for _ in range(min(groups, 5))]
+    pick = [g % len(parts) for g in range(groups)]
+    pitch = parts[0][0].stride(0)
+    b = torch.stack([parts[i][0] for i in pick])
+    if pitch != k:
+        wide = torch.full((groups, n, pitch), 0x7F, dtype=torch.uint8, device="cuda")
+        wide[:, :, :k] = b
+        b = wide[:, :, :k]
+    sb = torch.stack([parts[i][1] for i in pick])
+    y = H.grouped_matmul_fp8(a, sa, b, sb, _ends(ends), dtype=_torch_type(out),
+                             out=torch.full((tokens, n), 5.0, dtype=_torch_type(out), device="cuda"))
+    torch.cuda.synchronize()
+    y = _host(y)
+    low = 0
+    for g, high in enumerate(ends):
+        if high > low:
+            _, _, hb, hsb = parts[pick[g]]
+            R.check_product(ha[low:high], hsa[low:high], hb, hsb, y[low:high], out, 128, f"group {g}")
+        low = high
+    assert (y[low:] == 0).all()
+
+
+@pytest.mark.parametrize("out", OUTS)
+@pytest.mark.parametrize("n,k", [(1, 128), (130, 77), (257, 300)])
+@pytest.mark.parametrize("tokens,ends", GROUPS + [(0, [0, 0]), (700, [650, 650, 700])])
+def test_weight_gradient(tokens, ends, n, k, out):
+    """From the column quantizers' codes, against 64 bits of the same codes; empty groups."""
+    import torch
+    dy = to_device(W.random_rows(max(tokens, 1), n, "bf16", seed=n), "bf16")[:tokens]
+    x = to_device(W.random_rows(max(tokens, 1), k, "fp16", seed=k + 1), "fp16")[:tokens]
+    qd, sd = H.quantize_fp8_columns(dy, _ends(ends))
+    qx, sx = H.quantize_fp8_columns(x, _ends(ends))
+    shape = (len(ends), n, k)
+    g = H.grouped_weight_gradient_fp8(
+        qd, sd, qx, sx, _ends(ends),
+        out=torch.full(shape, 9.0, dtype=_torch_type(out), device="cuda"))
+    torch.cuda.synchronize()
+    g = _host(g)
+    hd, hsd, hx, hsx = (t.cpu().numpy() for t in (qd, sd, qx, sx))
+    for e, low, count, at, blocks in R.padded_places(ends, tokens)[0]:
+        if count == 0:
+            assert (g[e] == 0).all()
+            continue
+        cut, cuts = slice(at, at + blocks * 128), slice(at // 128, at // 128 + blocks)
+        R.check_product(hd[:, cut], hsd[:, cuts], hx[:, cut], hsx[:, cuts], g[e], out, 1, f"group {e}")
+
+
+def test_weight_gradient_of_one_group():
+    import torch
+    dy = torch.randn(300, 140, device="cuda").to(torch.float16)
+    x = torch.randn(300, 70, device="cuda").to(torch.float16)
+    qd, sd, qx, sx = *H.quantize_fp8_columns(dy), *H.quantize_fp8_columns(x)
+    g = H.grouped_weight_gradient_fp8(qd, sd, qx, sx, dtype=torch.float32)
+    assert torch.equal(g, H.grouped_weight_gradient_fp8(qd, sd, qx, sx, _ends([300]),
+                                                        dtype=torch.float32)[0])
+    assert torch.equal(g, H.matmul_fp8(qd, sd, qx, sx, dtype=torch.float32))
+
+
+def test_ends_out_of_range_stay_in_bounds():
+    """Ends below 0, past the rows or going down: wrong rows at most, neighbours untouched."""
+    import torch
+    rng = np.random.default_rng(2)
+    a, sa, _, _ = _codes(rng, 100, 128)
+    b, sb, _, _ = _codes(rng, 64, 128, scale_rows=1)
+    b3, sb3 = b[None].expand(4, -1, -1), sb[None].expand(4, -1, -1)
+    for ends in ([-5, 50, 1000, 2000], [90, 10, 95, 20], [2 ** 31 - 1, -2 ** 31, 0, 100]):
+        buf = torch.full((102, 64), 3.0, device="cuda")
+        H.grouped_matmul_fp8(a, sa, b3, sb3, _ends(ends), out=buf[1:101])
+        x = torch.randn(100, 40, device="cuda").to(torch.float16)
+        codes, scales = H.quantize_fp8_columns(x, _ends(ends))
+        H.grouped_weight_gradient_fp8(codes, scales, codes, scales, _ends(ends))
+        torch.cuda.synchronize()
+        assert (buf[0] == 3).all() and (buf[101] == 3).all()
+
+
+def test_broadcast_weights():
+    """One weight for every group, by a stride of 0."""
+    import torch
+    rng = np.random.default_rng(4)
+    a, sa, ha, hsa = _codes(rng, 150, 200)
+    b, sb, hb, hsb = _codes(rng, 70, 200, scale_rows=1, spread=0.01)
+    y = H.grouped_matmul_fp8(a, sa, b[None].expand(3, -1, -1), sb[None].expand(3, -1, -1),
+                             _ends([10, 20, 150]), dtype=torch.float32)
+    R.check_product(ha, hsa, hb, hsb, _host(y), "fp32")
+
+
+# ---- offsets beyond 32 bits ----------------------------------------------------------
+
+
+def test_outputs_beyond_4_gib():
+    import torch
+    m, n, k = 70001, 32768, 16
+    rng = np.random.default_rng(8)
+    a, sa, ha, hsa = _codes(rng, m, k)
+    b, sb, hb, hsb = _codes(rng, n, k, scale_rows=n // 128, spread=0.1)
+    y = H.matmul_fp8(a, sa, b, sb)
+    rows = [0, 32767, 65535, 65536, 65537, 70000]
+    R.check_product(ha[rows], hsa[rows], hb, hsb, _host(y[rows]), "bf16")
+
+
+def test_weights_beyond_4_gib():
+    import torch
+    groups, n, k = 40, 8192, 16384
+    codes = torch.zeros((groups, n, k), dtype=torch.uint8, device="cuda")
+    scales = torch.zeros((groups, n // 128, k // 128), device="cuda")
+    rng = np.random.default_rng(9)
+    a, sa, ha, hsa = _codes(rng, 3, k)
+    b, sb, hb, hsb = _codes(rng, n, k, scale_rows=n // 128, spread=0.001)
+    codes[39], scales[39] = b, sb
+    y = H.grouped_matmul_fp8(a, sa, codes, scales, _ends([1] * 39 + [3]))
+    assert (y[0] == 0).all()
+    R.check_product(ha[1:], hsa[1:], hb, hsb, _host(y[1:]), "bf16")
+
+
+# ---- streams and graphs -----------------------------------------------------------------
+
+
+def test_another_stream_and_captured_graph():
+    """The whole path on a side stream, and captured: replays follow new inputs and ends."""
+    import torch
+    tokens, k, n, groups = 200, 512, 192, 3
+    x = torch.randn(tokens, k, device="cuda").to(torch.bfloat16)
+    w = (torch.randn(groups, n, k, device="cuda") / 20).to(torch.bfloat16)
+    ends = _ends([50, 50, 200])
+    b, sb, bt = H.quantize_fp8_tiles(w, transposed=True)
+
+    def path():
+        a, sa = H.transform_fp8_blocks(x, n=128)
+        y = H.grouped_matmul_fp8(a, sa, b, sb, ends)
+        q, sq = H.quantize_fp8_columns(x, ends)
+        d, sd = H.quantize_fp8_columns(y, ends)
+        return y, H.grouped_weight_gradient_fp8(d, sd, q, sq, ends, dtype=torch.float32)
+
+    want = path()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = path()
+    side.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(want, got))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = path()
+    for step in range(4):
+        x.copy_(torch.randn(tokens, k, device="cuda"))
+        ends.copy_(_ends([[50, 50, 200], [0, 199, 200], [200, 200, 200], [1, 2, 3]][step]))
+        graph.replay()
+        want = path()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(want, held)), step
