@@ -20,6 +20,8 @@
 
 #include <math.h>
 #include <stdint.h>
+#include <stdlib.h>
+#include <string.h>
 
 #include <type_traits>
 
@@ -57,29 +59,32 @@ __device__ __forceinline__ int clamp_end(int e, int rows) {
   return e < 0 ? 0 : e > rows ? rows : e;
 }
 
+// Sum over the lanes up to this one, of the whole wave (row shifts, then row broadcasts).
+__device__ __forceinline__ int prefix_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);  // row_shr:2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);  // row_shr:4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);  // row_shr:8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // row_bcast:15
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // row_bcast:31
+  return x;
+}
+
 // Piece `id` of the groups cut into pieces of `unit` rows: group 0's first, then group
 // 1's, ...  With `rest` the rows after the last end are one more group.  Called by
 // whole waves; 64 groups at a time by a prefix sum over the lanes.
 __device__ __forceinline__ Piece find_piece(const int32_t *ends, int groups, int rows, int unit,
                                             int id, bool rest) {
   const int lane = threadIdx.x & (kWave - 1);
-  int base = 0;
+  int base = 0, start = 0;  // pieces and rows before these 64 groups
   const int all = groups + (rest ? 1 : 0);
   for (int g0 = 0; g0 < all; g0 += kWave) {
     const int g = g0 + lane;
-    int low = 0, high = 0;
-    if (g < all) {
-      low = g > 0 ? clamp_end(ends[g - 1], rows) : 0;
-      high = g < groups ? clamp_end(ends[g], rows) : rows;
-    }
-    const int count = high > low ? high - low : 0;
-    const int pieces = (count + unit - 1) / unit;
-    int sum = pieces;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const int other = __shfl_up(sum, d);
-      if (lane >= d) sum += other;
-    }
+    const int high = g < groups ? clamp_end(ends[g], rows) : rows;
+    // wave_shr:1, the first lane's from the groups before
+    const int low = __builtin_amdgcn_update_dpp(start, high, 0x138, 0xF, 0xF, false);
+    const int pieces = g < all && high > low ? (high - low + unit - 1) / unit : 0;
+    const int sum = prefix_sum(pieces);
     const uint64_t hit = __ballot(pieces > 0 && id >= base + sum - pieces && id < base + sum);
     if (hit != 0) {
       const int at = __builtin_ctzll(hit);
@@ -88,6 +93,7 @@ __device__ __forceinline__ Piece find_piece(const int32_t *ends, int groups, int
       return {g0 + at, lo + (id - first) * unit, __builtin_amdgcn_readlane(high, at)};
     }
     base += __builtin_amdgcn_readlane(sum, kWave - 1);
+    start = __builtin_amdgcn_readlane(high, kWave - 1);
   }
   return {-1, 0, 0};
 }
@@ -393,7 +399,7 @@ __global__ __launch_bounds__(256) void tile_kernel(TileArgs p) {
 
 // ---- products ------------------------------------------------------------------
 
-constexpr int kTiles = 0;     // all rows of A with one B
+constexpr int kDense = 0;     // all rows of A with one B
 constexpr int kGroups = 1;    // groups of rows of A, each with its own B
 constexpr int kGradient = 2;  // groups of blocks of k, each with its own output
 
@@ -411,23 +417,63 @@ struct ProductArgs {
   const int32_t *ends;
   int groups;
   int m, n, k;
-  int tiles_m, tiles_n;  // the grid (kGradient: of each group)
+  int tiles_m, tiles_n;  // the grid (kGradient: of each group; kGroups: at most)
   int kind, out_type;
 };
 
-// 16 bytes of LDS per lane at `lds` + 16 * lane from base + offset, asynchronously.
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t base, void *lds, int offset,
-                                            int uniform_offset) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(
-      base, (__attribute__((address_space(3))) void *)lds, 16, offset, uniform_offset, 0, 0);
+// Asynchronous loads into LDS: lane l's 16 bytes from base + offset + uniform_offset go to
+// `lds` + 16 l.  In asm, because the compiler waits for all outstanding loads of this kind
+// before any LDS read, which would undo the loading ahead: the kernel waits itself
+// (wait_stages) before the barrier that publishes the data.  The instruction writes no
+// register; the wait state is the one that it needs after a write of M0 (which no other
+// instruction of these kernels uses, and which may not be named as clobbered).
+// NT: with the streaming cache policy, for data that nobody reads again.
+template <bool NT = false>
+__device__ __forceinline__ void load_to_lds(u4 base, uint32_t lds, int offset, int uniform_offset) {
+  if constexpr (NT)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds"
+                 :
+                 : "s"(lds), "v"(offset), "s"(base), "s"(uniform_offset)
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :
+                 : "s"(lds), "v"(offset), "s"(base), "s"(uniform_offset)
+                 : "memory");
 }
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_rsrc(const void *base) {
+// The same for one 4-byte word of each lane's own address.
+__device__ __forceinline__ void load_word_to_lds(const float *from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+               :
+               : "s"(lds), "v"(from)
+               : "memory");
+}
+
+// Waits until at most the loads of `ahead` later stages of `LOADS` loads are in flight,
+// `ahead` being at most MOST.
+template <int MOST, int LOADS>
+__device__ __forceinline__ void wait_stages(int ahead) {
+  if constexpr (MOST > 0) {
+    if (ahead < MOST) {
+      wait_stages<MOST - 1, LOADS>(ahead);
+      return;
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(MOST * LOADS) : "memory");
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
+}
+
+// A buffer over everything from `base`, which is the same in every lane: the range check
+// is off, the rows that a kernel reads are clamped instead.
+__device__ __forceinline__ u4 buffer_words(const void *base) {
   const uint64_t b = reinterpret_cast<uint64_t>(base);
-  const uint64_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
-  const uint64_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
-  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>((hi << 32) | lo), (short)0,
-                                           -1, 0x00020000);
+  return u4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b),
+            (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) & 0xFFFFu, 0xFFFFFFFFu,
+            0x00020000u};
 }
 
 // The first `valid` of 16 bytes.
@@ -521,8 +567,34 @@ struct Operand<true> {
   }
 };
 
-// A tile of BM x BN outputs by WM x WN waves, from LDS tiles of 128 bytes of k that are
-// loaded one step ahead.
+// Which tile a workgroup takes.  Workgroups go to the 8 XCDs in turn, each with an L2 of
+// its own: of 256 that run together (one to a CU), each XCD takes 32 consecutive tiles, and
+// tiles are numbered in bands of kBand rows, down the band first, so that 32 tiles read
+// 4 strips of A and 8 of B.
+struct TileAt {
+  int matrix, m, n;
+};
+
+__device__ __forceinline__ TileAt tile_at(uint32_t id, uint32_t total, int tiles_m, int tiles_n) {
+  constexpr uint32_t kXcds = 8, kTogether = 256;
+  constexpr int kBand = 4;
+  const uint32_t first = id & ~(kTogether - 1);
+  const uint32_t count = total - first < kTogether ? total - first : kTogether;
+  const uint32_t xcd = id & (kXcds - 1), turn = (id - first) / kXcds;
+  const uint32_t each = count / kXcds, more = count % kXcds;
+  const uint32_t tile = first + xcd * each + (xcd < more ? xcd : more) + turn;
+  const uint32_t per = (uint32_t)tiles_m * (uint32_t)tiles_n;
+  const int matrix = (int)(tile / per), rest = (int)(tile % per);
+  const int band = rest / (kBand * tiles_n), in_band = rest % (kBand * tiles_n);
+  const int high = tiles_m - band * kBand < kBand ? tiles_m - band * kBand : kBand;
+  return {matrix, band * kBand + in_band % high, in_band / high};
+}
+
+// The whole tiles' kernel: BM x BN outputs by WM x WN waves, in steps of a block of k.
+//
+// The rows of A and B and their scales go through D stages of LDS, loaded D - 1 steps
+// ahead; one barrier a step.  All loads are of the kind that goes to LDS, the same number
+// in every wave, so that a wait counts stages.
 //
 // B is the MFMA's first operand and A its second, so a lane's four results are four
 // columns n of one row m: its A scale is one value, and its stores are along the row.
@@ -533,32 +605,39 @@ struct Operand<true> {
 //
 // LDS rows are 128 bytes; chunk c of row r lies at c ^ ((r >> 1) & 7), which the loads
 // obey by choosing their global chunk, since LDS addresses of a load run with the lane.
-template <int BM, int BN, int WM, int WN, bool BROWS, bool FULL>
-__global__ __launch_bounds__(WM *WN *kWave) void product_kernel(ProductArgs p) {
-  constexpr int kThreads = WM * WN * kWave;
+template <int BM, int BN, int WM, int WN, int D, int KS, bool BROWS, bool FULL>
+__global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs p) {
+  constexpr int kThreads = WM * WN * kWave;  // of one share of k
   constexpr int TM = BM / WM / 16, TN = BN / WN / 16;  // MFMA tiles of a wave
-  static_assert(TN % 4 == 0 && (BN / WN) <= kBlock, "a wave's columns are in one block of B");
+  static_assert(TN % 4 == 0 && kBlock % (BN / WN) == 0, "a wave's columns are in one block of B");
   constexpr int kLoadsA = BM * 8 / kThreads, kLoadsB = BN * 8 / kThreads;
+  constexpr int kTiles = kLoadsA + kLoadsB;  // loads of 16 bytes a thread
+  // scales of A's rows, then of B's columns or blocks of columns
   constexpr int SB = BROWS ? BN : BN / kBlock > 0 ? BN / kBlock : 1;
-  __shared__ __align__(16) uint8_t tile_a[2][BM * kBlock];
-  __shared__ __align__(16) uint8_t tile_b[2][BN * kBlock];
-  __shared__ __align__(16) float scale_a[2][BM];
-  __shared__ __align__(16) float scale_b[2][SB];
+  constexpr int kScales = (BM + SB + kThreads - 1) / kThreads;
+  constexpr int kLoads = kTiles + kScales;
+  static_assert(kLoads * (D - 2) < 64, "loads in flight that one wait can count");
+  constexpr int kStageBytes = (BM + BN) * kBlock;
+  __shared__ __align__(16) uint8_t tiles[KS * D * kStageBytes];
+  __shared__ __align__(16) float scales_of[KS][D][kScales * kThreads];
 
-  const int t = threadIdx.x, lane = t & (kWave - 1);
+  const int share = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+  const int t = threadIdx.x - share * kThreads, lane = t & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(t / kWave);
   const int wm = wave / WN, wn = wave % WN;
+  uint8_t *const ring = tiles + share * D * kStageBytes;
+  float (*const scales)[kScales * kThreads] = scales_of[share];
   const int g = lane >> 4, li = lane & 15;
 
   // which tile
-  int tile = blockIdx.x, m0, n0, m_end = p.m, kb0 = 0, kb1 = (p.k + kBlock - 1) / kBlock;
+  int m0, n0, m_end = p.m, kb0 = 0, kb1 = (p.k + kBlock - 1) / kBlock;
   const uint8_t *b = p.b;
   const float *sb = p.sb;
   int64_t out_at = 0;
-  n0 = (tile % p.tiles_n) * BN;
-  tile /= p.tiles_n;
+  const TileAt tile = tile_at(blockIdx.x, gridDim.x, p.tiles_m, p.tiles_n);
+  n0 = tile.n * BN;
   if (p.kind == kGroups) {
-    const Piece piece = find_piece(p.ends, p.groups, p.m, BM, tile, true);
+    const Piece piece = find_piece(p.ends, p.groups, p.m, BM, tile.m, true);
     if (piece.group < 0) return;
     m0 = piece.low;
     m_end = piece.high;
@@ -570,79 +649,64 @@ __global__ __launch_bounds__(WM *WN *kWave) void product_kernel(ProductArgs p) {
       sb += piece.group * p.sb_batch;
     }
   } else {
-    m0 = (tile % p.tiles_m) * BM;
+    m0 = tile.m * BM;
     if (p.kind == kGradient) {
-      const int group = tile / p.tiles_m;
-      out_at = group * p.out_batch;
+      out_at = tile.matrix * p.out_batch;
       if (p.ends != nullptr) {
         int before, count;
-        group_blocks(p.ends, p.groups, p.k, group, before, count);
+        group_blocks(p.ends, p.groups, p.k, tile.matrix, before, count);
         kb0 = before < kb1 ? before : kb1;
         kb1 = before + count < kb1 ? before + count : kb1;
       }
     }
   }
-  const __amdgpu_buffer_rsrc_t ra = uniform_rsrc(p.a + (int64_t)m0 * p.a_pitch);
-  const __amdgpu_buffer_rsrc_t rb = uniform_rsrc(b + (int64_t)n0 * p.b_pitch);
-
+  // this share of the blocks of k, and the steps that all shares take
+  const int steps = KS == 1 ? kb1 - kb0 : (kb1 - kb0 + KS - 1) / KS;
+  if constexpr (KS > 1) {
+    kb0 = kb0 + share * steps < kb1 ? kb0 + share * steps : kb1;
+    kb1 = kb0 + steps < kb1 ? kb0 + steps : kb1;
+  }
   // the rows past the end repeat the last one; their results are not stored
-  int off_a[kLoadsA], off_b[kLoadsB];
+  const int rows = m_end - m0, columns = p.n - n0;
+  const u4 ra = buffer_words(p.a + (int64_t)m0 * p.a_pitch);
+  const u4 rb = buffer_words(b + (int64_t)n0 * p.b_pitch);
+  int off[kTiles];
 #pragma unroll
-  for (int i = 0; i < kLoadsA; ++i) {
-    const int s = i * kThreads + t, r = s >> 3;
-    const int row = r < m_end - m0 ? r : m_end - m0 - 1;
-    off_a[i] = row * (int)p.a_pitch + (((s & 7) ^ ((r >> 1) & 7)) << 4);
-  }
-#pragma unroll
-  for (int i = 0; i < kLoadsB; ++i) {
-    const int s = i * kThreads + t, r = s >> 3;
+  for (int i = 0; i < kTiles; ++i) {
+    const int s = (i < kLoadsA ? i : i - kLoadsA) * kThreads + t, r = s >> 3;
     const int c = (r & ~63) + 16 * ((r & 15) >> 2) + 4 * ((r >> 4) & 3) + (r & 3);
-    const int row = c < p.n - n0 ? c : p.n - n0 - 1;
-    off_b[i] = row * (int)p.b_pitch + (((s & 7) ^ ((r >> 1) & 7)) << 4);
+    const int row = i < kLoadsA ? (r < rows ? r : rows - 1) : (c < columns ? c : columns - 1);
+    off[i] = row * (int)(i < kLoadsA ? p.a_pitch : p.b_pitch) + (((s & 7) ^ ((s >> 4) & 7)) << 4);
   }
-  const int tail = p.k & (kBlock - 1);
-  const int kb_tail = tail != 0 ? p.k / kBlock : -1;
-  // thread t brings the A scale of row t and the B scale of column (or block) t
-  const int srow = t < m_end - m0 ? t : m_end - m0 - 1;
-  const float *sa_at = p.sa + (int64_t)(m0 + srow) * p.sa_pitch;
-  const int scol = BROWS ? (n0 + t < p.n ? n0 + t : p.n - 1)
-                         : (n0 / kBlock + t <= (p.n - 1) / kBlock ? n0 / kBlock + t
-                                                                  : (p.n - 1) / kBlock);
-  const float *sb_at = sb + (int64_t)scol * p.sb_pitch;
-  float next_sa = 0.0f, next_sb = 0.0f;
+  // the threads past the scales bring the last one again
+  const float *scale_at[kScales];
+#pragma unroll
+  for (int i = 0; i < kScales; ++i) {
+    const int r = i * kThreads + t, last = BROWS ? p.n - 1 : (p.n - 1) / kBlock;
+    const int c = (BROWS ? n0 : n0 / kBlock) + r - BM;
+    scale_at[i] = r < BM ? p.sa + (int64_t)(m0 + (r < rows ? r : rows - 1)) * p.sa_pitch
+                         : sb + (int64_t)(c < last ? c : last) * p.sb_pitch;
+  }
+  const int tail = p.k & (kBlock - 1), kb_tail = tail != 0 ? p.k / kBlock : -1;
 
-  const auto load = [&](int kb) {
-    uint8_t *la = tile_a[kb & 1], *lb = tile_b[kb & 1];
-    if (kb != kb_tail) {
-#pragma unroll
-      for (int i = 0; i < kLoadsA; ++i)
-        load_to_lds(ra, la + (i * kThreads + wave * kWave) * 16, off_a[i], kb * kBlock);
-#pragma unroll
-      for (int i = 0; i < kLoadsB; ++i)
-        load_to_lds(rb, lb + (i * kThreads + wave * kWave) * 16, off_b[i], kb * kBlock);
-    } else {
-      // the last, partial block of k: codes past it are 0
-#pragma unroll
-      for (int i = 0; i < kLoadsA; ++i) {
-        const int s = i * kThreads + t, valid = tail - (((s & 7) ^ ((s >> 4) & 7)) << 4);
-        u4 v = {0, 0, 0, 0};
-        if (valid > 0)
-          v = first_bytes(__builtin_amdgcn_raw_buffer_load_b128(ra, off_a[i], kb * kBlock, 0),
-                          valid);
-        *reinterpret_cast<u4 *>(la + s * 16) = v;
-      }
-#pragma unroll
-      for (int i = 0; i < kLoadsB; ++i) {
-        const int s = i * kThreads + t, valid = tail - (((s & 7) ^ ((s >> 4) & 7)) << 4);
-        u4 v = {0, 0, 0, 0};
-        if (valid > 0)
-          v = first_bytes(__builtin_amdgcn_raw_buffer_load_b128(rb, off_b[i], kb * kBlock, 0),
-                          valid);
-        *reinterpret_cast<u4 *>(lb + s * 16) = v;
-      }
+  // One of a thread's kLoads loads of block kb.  In the last, partial block (TAIL) chunks
+  // wholly past k may lie past the matrix: the row's first one is loaded instead.
+  const auto load_piece = [&](int kb, int stage, int i, auto is_tail) {
+    if (i >= kTiles) {
+      load_word_to_lds(scale_at[i - kTiles] + kb,
+                       lds_address(&scales[stage][(i - kTiles) * kThreads + wave * kWave]));
+      return;
     }
-    if (t < BM) next_sa = sa_at[kb];
-    if (t < SB) next_sb = sb_at[kb];
+    int from = off[i];
+    if constexpr (decltype(is_tail)::value) {
+      const int s = (i < kLoadsA ? i : i - kLoadsA) * kThreads + t;
+      const int c = ((s & 7) ^ ((s >> 4) & 7)) << 4;
+      if (c >= tail) from -= c + kb * kBlock;
+    }
+    // A's rows and then B's
+    load_to_lds(i < kLoadsA ? ra : rb,
+                lds_address(ring + stage * kStageBytes) + (i * kThreads + wave * kWave) * 16, from,
+                kb * kBlock);
   };
 
   f4 acc[TM][TN];
@@ -652,52 +716,134 @@ __global__ __launch_bounds__(WM *WN *kWave) void product_kernel(ProductArgs p) {
     for (int j = 0; j < TN; ++j) acc[i][j] = f4{0, 0, 0, 0};
 
   const int key = (li >> 1) & 7;
-  const int chunk0 = ((g ^ key) << 4), chunk1 = (((g + 4) ^ key) << 4);
-  const auto fragment = [&](const uint8_t *tile_rows) {
-    const uint8_t *row = tile_rows + li * kBlock;
-    const u4 lo = *reinterpret_cast<const u4 *>(row + chunk0);
-    const u4 hi = *reinterpret_cast<const u4 *>(row + chunk1);
+  const int chunk0 = li * kBlock + ((g ^ key) << 4), chunk1 = li * kBlock + (((g + 4) ^ key) << 4);
+  const auto fragment = [&](const uint8_t *tile_rows, auto is_tail) {
+    u4 lo = *reinterpret_cast<const u4 *>(tile_rows + chunk0);
+    u4 hi = *reinterpret_cast<const u4 *>(tile_rows + chunk1);
+    if constexpr (decltype(is_tail)::value) {
+      lo = first_bytes(lo, tail - g * 16);
+      hi = first_bytes(hi, tail - g * 16 - 64);
+    }
     return i8v{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3],
                (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
   };
 
-  if (kb0 < kb1) load(kb0);
-  for (int kb = kb0; kb < kb1; ++kb) {
-    // this step's tiles and scales have come; the barrier also ends the last step's reads
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if (t < BM) scale_a[kb & 1][t] = next_sa;
-    if (t < SB) scale_b[kb & 1][t] = next_sb;
+  using No = std::false_type;
+  using Yes = std::true_type;
+  // One step: the products of block kb, in `stage`, and in between the loads of block
+  // kb + D - 1 (LOAD: 0 none, 1 a whole block, 2 the tail) into the stage that the last step
+  // has read.  Issuing them all first would hold up the wave, which takes its turn at the
+  // address unit, 16 cycles a load; the first half of the step leaves them time to arrive.
+  const auto step = [&](int kb, int stage, auto what, auto is_tail) {
+    constexpr int LOAD = decltype(what)::value;
+    // this block has come; the barrier also ends the last step's reads
+    wait_stages<D - 2, kLoads>(kb1 - 1 - kb);
     __syncthreads();
-    if (kb + 1 < kb1) load(kb + 1);
-    const uint8_t *la = tile_a[kb & 1] + wm * (BM / WM) * kBlock;
-    const uint8_t *lb = tile_b[kb & 1] + wn * (BN / WN) * kBlock;
-    Operand<FULL> fb[TN];
+    const uint8_t *la = ring + stage * kStageBytes + wm * (BM / WM) * kBlock;
+    const uint8_t *lb = ring + stage * kStageBytes + (BM + wn * (BN / WN)) * kBlock;
+    const int into = stage == 0 ? D - 1 : stage - 1;
+    // The scaling of a product waits for its MFMA, so it is done kAhead products later;
+    // the operand of the next row of products is read during this one's.  The barriers of
+    // the scheduler keep that order, which the compiler would undo.
+    constexpr int kAhead = 3;
+    f4 r[kAhead + 1];
+    Operand<FULL> fa[2], fb[TN];
+    fa[0].set(fragment(la, is_tail));
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int j = 0; j < TN; ++j) fb[j].set(fragment(lb + j * 16 * kBlock));
+    for (int j = 0; j < TN; ++j) {
+      fb[j].set(fragment(lb + j * 16 * kBlock, is_tail));
+      __builtin_amdgcn_sched_barrier(0);
+    }
     f4 col[TN];
     float uniform_b = 0.0f;
     if constexpr (BROWS) {
 #pragma unroll
       for (int j = 0; j < TN; ++j)
         col[j] = *reinterpret_cast<const f4 *>(
-            &scale_b[kb & 1][wn * (BN / WN) + (j & ~3) * 16 + 16 * g + 4 * (j & 3)]);
+            &scales[stage][BM + wn * (BN / WN) + (j & ~3) * 16 + 16 * g + 4 * (j & 3)]);
     } else {
-      uniform_b = scale_b[kb & 1][wn * (BN / WN) / kBlock];
+      uniform_b = scales[stage][BM + wn * (BN / WN) / kBlock];
     }
+    float s[TM];
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      Operand<FULL> fa;
-      fa.set(fragment(la + i * 16 * kBlock));
-      float s = scale_a[kb & 1][wm * (BM / WM) + i * 16 + li];
-      if constexpr (!BROWS) s *= uniform_b;
+    for (int i = 0; i < TM; ++i) s[i] = scales[stage][wm * (BM / WM) + i * 16 + li];
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const f4 r = Operand<FULL>::product(fb[j], fa);
+    for (int c = 0; c < TM * TN + kAhead; ++c) {
+      if (c < TM * TN) {
+        const int i = c / TN, j = c % TN;
+        if (j == 0 && i + 1 < TM) fa[(i + 1) & 1].set(fragment(la + (i + 1) * 16 * kBlock, is_tail));
+        r[c % (kAhead + 1)] = Operand<FULL>::product(fb[j], fa[i & 1]);
+      }
+      if (c >= kAhead) {
+        const int d = c - kAhead, i = d / TN, j = d % TN;
+        if (!BROWS && j == 0) s[i] *= uniform_b;
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          acc[i][j][q] = __builtin_fmaf(r[q], BROWS ? s * col[j][q] : s, acc[i][j][q]);
+          acc[i][j][q] = __builtin_fmaf(r[d % (kAhead + 1)][q], BROWS ? s[i] * col[j][q] : s[i],
+                                        acc[i][j][q]);
+        // keeps the sums here: the compiler would move them past the next barrier
+        asm volatile("" : "+v"(acc[i][j]));
+      }
+      if constexpr (LOAD != 0) {
+        constexpr int kOver = TM * TN / 2;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+          if (i * kOver / kLoads == c)
+            load_piece(kb + D - 1, into, i, std::bool_constant<LOAD == 2>{});
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  if (kb0 < kb1) {
+#pragma unroll
+    for (int d = 0; d < D - 1; ++d) {
+      if (kb0 + d >= kb1) continue;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        if (kb0 + d == kb_tail)
+          load_piece(kb0 + d, d, i, Yes{});
+        else
+          load_piece(kb0 + d, d, i, No{});
       }
     }
+    const int whole = kb1 - 1 == kb_tail ? kb1 - 1 : kb1;  // end of the whole blocks
+    int kb = kb0, stage = 0;
+    const auto after = [](int s) { return s == D - 1 ? 0 : s + 1; };
+    for (; kb + D - 1 < whole; ++kb, stage = after(stage))
+      step(kb, stage, std::integral_constant<int, 1>{}, No{});
+    if (kb + D - 1 < kb1) {
+      step(kb, stage, std::integral_constant<int, 2>{}, No{});
+      ++kb;
+      stage = after(stage);
+    }
+    for (; kb < whole; ++kb, stage = after(stage))
+      step(kb, stage, std::integral_constant<int, 0>{}, No{});
+    if (kb < kb1) step(kb, stage, std::integral_constant<int, 0>{}, Yes{});
+  }
+  if constexpr (KS > 1) {
+    // the other shares' barriers, then the sums of the shares, added in their order
+    for (int i = kb1 - kb0; i < steps; ++i) __syncthreads();
+    static_assert((KS - 1) * BM * BN * 4 <= sizeof(tiles), "the sums fit the stages");
+    f4 *sums = reinterpret_cast<f4 *>(tiles);
+    __syncthreads();
+    if (share > 0) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          sums[(((share - 1) * TM + i) * TN + j) * kThreads + t] = acc[i][j];
+    }
+    __syncthreads();
+    if (share > 0) return;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int q = 0; q < KS - 1; ++q) acc[i][j] += sums[((q * TM + i) * TN + j) * kThreads + t];
   }
 
   const int wide = FULL ? 4 : 2;
@@ -724,30 +870,271 @@ __global__ __launch_bounds__(WM *WN *kWave) void product_kernel(ProductArgs p) {
   }
 }
 
-template <int BM, int BN, int WM, int WN>
-hipError_t launch_product(ProductArgs p, bool b_rows, hipStream_t stream) {
+// Few rows of A: the product is a reading of B at HBM speed.  A workgroup takes 16 MT rows
+// of A and 16 RB rows of B; its W waves share the blocks of k, each summing its own, and
+// add their sums in LDS in the order of the waves.  Every wave streams its blocks through
+// D stages of LDS of its own, so there is no barrier before the sums: with its loads D - 1
+// stages ahead it waits for the oldest only.  Loads of 16 bytes a lane straight to
+// registers in the MFMA's order would touch 64 cache lines an instruction, in LDS order 8.
+template <int MT, int RB, int W, int D, bool NT, bool FULL>
+__global__ __launch_bounds__(W *kWave) void few_rows_kernel(ProductArgs p) {
+  constexpr int kRowsA = 16 * MT, kRowsB = 16 * RB;
+  constexpr int kStage = (kRowsA + kRowsB) * kBlock;
+  constexpr int kScaleLoads = kRowsA < kWave ? 1 : 2;  // A's rows and then B's block, a lane each
+  constexpr int kLoads = 2 * (MT + RB) + kScaleLoads;
+  static_assert(kLoads * (D - 1) < 64, "loads in flight that one wait can count");
+  constexpr int kSums = kRowsA * kRowsB;
+  constexpr int kRing = W * D * kStage, kSumBytes = W * kSums * 4;
+  __shared__ __align__(16) uint8_t memory[kRing > kSumBytes ? kRing : kSumBytes];
+  __shared__ float scales[W][D][kScaleLoads * kWave];
+
+  const int t = threadIdx.x, lane = t & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(t / kWave);
+  const int g = lane >> 4, li = lane & 15;
+  const int n0 = (int)(blockIdx.x % p.tiles_n) * kRowsB, tile = blockIdx.x / p.tiles_n;
+  int m0 = tile * kRowsA, m_end = p.m, blocks = (p.k + kBlock - 1) / kBlock;
+  const uint8_t *b = p.b;
+  const float *sb = p.sb;
+  if (p.kind == kGroups) {
+    const Piece piece = find_piece(p.ends, p.groups, p.m, kRowsA, tile, true);
+    if (piece.group < 0) return;
+    m0 = piece.low;
+    m_end = piece.high;
+    if (m0 < 0 || m0 >= m_end) return;
+    if (piece.group == p.groups) {
+      blocks = 0;  // rows after the last group: zeros
+    } else {
+      b += piece.group * p.b_batch;
+      sb += piece.group * p.sb_batch;
+    }
+  }
+  const int rows = m_end - m0, columns = p.n - n0;
+  const int kb0 = (int)((int64_t)blocks * wave / W), kb1 = (int)((int64_t)blocks * (wave + 1) / W);
+  const u4 ra = buffer_words(p.a + (int64_t)m0 * p.a_pitch);
+  const u4 rb = buffer_words(b + (int64_t)n0 * p.b_pitch);
+  // slot s of 16 bytes of a stage is row s / 8; rows past the end repeat the last one
+  const int tail = p.k & (kBlock - 1), kb_tail = tail != 0 ? p.k / kBlock : -1;
+  const auto row_offset = [&](int s, int count, int64_t pitch) {
+    const int r = s >> 3;
+    return (r < count ? r : count - 1) * (int)pitch;
+  };
+  const auto chunk = [&](int s) { return ((s & 7) ^ ((s >> 4) & 7)) << 4; };
+  int off_a[2 * MT], off_b[2 * RB];
+#pragma unroll
+  for (int i = 0; i < 2 * MT; ++i)
+    off_a[i] = row_offset(i * kWave + lane, rows, p.a_pitch) + chunk(i * kWave + lane);
+#pragma unroll
+  for (int i = 0; i < 2 * RB; ++i)
+    off_b[i] = row_offset(i * kWave + lane, columns, p.b_pitch) + chunk(i * kWave + lane);
+  const float *scale_at[kScaleLoads];
+#pragma unroll
+  for (int i = 0; i < kScaleLoads; ++i) {
+    const int r = i * kWave + lane;
+    scale_at[i] = r < kRowsA ? p.sa + (int64_t)(m0 + (r < rows ? r : rows - 1)) * p.sa_pitch
+                             : sb + (int64_t)(n0 / kBlock) * p.sb_pitch;
+  }
+  uint8_t *ring = memory + wave * D * kStage;
+  const auto load = [&](int kb, int stage) {
+    const uint32_t to = lds_address(ring + stage * kStage);
+#pragma unroll
+    for (int i = 0; i < 2 * (MT + RB); ++i) {
+      const bool of_b = i >= 2 * MT;
+      int off = of_b ? off_b[of_b ? i - 2 * MT : 0] : off_a[of_b ? 0 : i];
+      // chunks wholly past k may lie past the matrix: the row's first one instead
+      const int c = chunk((of_b ? i - 2 * MT : i) * kWave + lane);
+      if (kb == kb_tail && c >= tail) off -= c + kb * kBlock;
+      if (of_b)
+        load_to_lds<NT>(rb, to + i * kWave * 16, off, kb * kBlock);
+      else
+        load_to_lds(ra, to + i * kWave * 16, off, kb * kBlock);
+    }
+#pragma unroll
+    for (int i = 0; i < kScaleLoads; ++i)
+      load_word_to_lds(scale_at[i] + kb, lds_address(&scales[wave][stage][i * kWave]));
+  };
+
+  f4 acc[MT][RB];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < RB; ++j) acc[i][j] = f4{0, 0, 0, 0};
+  const int key = (li >> 1) & 7;
+  const int at0 = li * kBlock + ((g ^ key) << 4), at1 = li * kBlock + (((g + 4) ^ key) << 4);
+  const auto fragment = [&](const uint8_t *tile_rows, int kb) {
+    u4 lo = *reinterpret_cast<const u4 *>(tile_rows + at0);
+    u4 hi = *reinterpret_cast<const u4 *>(tile_rows + at1);
+    if (kb == kb_tail) {
+      lo = first_bytes(lo, tail - g * 16);
+      hi = first_bytes(hi, tail - g * 16 - 64);
+    }
+    return i8v{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3],
+               (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+  };
+
+#pragma unroll
+  for (int d = 0; d < D - 1; ++d)
+    if (kb0 + d < kb1) load(kb0 + d, d);
+  int stage = 0;
+#pragma unroll 1
+  for (int kb = kb0; kb < kb1; ++kb) {
+    // this stage's last reads (D steps ago) are done: its loads may overwrite it
+    const int ahead = kb + D - 1;
+    if (ahead < kb1) load(ahead, stage == 0 ? D - 1 : stage - 1);
+    wait_stages<D - 1, kLoads>(kb1 - 1 - kb);
+    const uint8_t *la = ring + stage * kStage, *lb = la + kRowsA * kBlock;
+    const float scale_b = scales[wave][stage][kRowsA];
+    Operand<FULL> fb[RB];
+#pragma unroll
+    for (int j = 0; j < RB; ++j) fb[j].set(fragment(lb + j * 16 * kBlock, kb));
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      Operand<FULL> fa;
+      fa.set(fragment(la + i * 16 * kBlock, kb));
+      const float s = scales[wave][stage][i * 16 + li] * scale_b;
+#pragma unroll
+      for (int j = 0; j < RB; ++j) {
+        const f4 r = Operand<FULL>::product(fb[j], fa);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[i][j][q] = __builtin_fmaf(r[q], s, acc[i][j][q]);
+      }
+    }
+    // the reads have returned before the next loads go to this stage
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    stage = stage == D - 1 ? 0 : stage + 1;
+  }
+
+  __syncthreads();
+  float *sums = reinterpret_cast<float *>(memory);
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < RB; ++j)
+      *reinterpret_cast<f4 *>(
+          &sums[wave * kSums + (i * 16 + li) * kRowsB + j * 16 + 4 * g]) = acc[i][j];
+  __syncthreads();
+#pragma unroll
+  for (int e = t; e < kSums; e += W * kWave) {
+    const int row = e / kRowsB, column = e % kRowsB;
+    if (row >= rows || column >= columns) continue;
+    float v = sums[e];
+#pragma unroll
+    for (int w = 1; w < W; ++w) v += sums[w * kSums + e];
+    const int64_t at = (int64_t)(m0 + row) * p.out_pitch + n0 + column;
+    if constexpr (FULL)
+      store_out<HADACORE_FP32>(p.out, at, v);
+    else if (p.out_type == HADACORE_FP16)
+      store_out<HADACORE_FP16>(p.out, at, v);
+    else
+      store_out<HADACORE_BF16>(p.out, at, v);
+  }
+}
+
+// Pieces of `unit` rows, at most: of ragged groups each has one that is not full at most,
+// the rows after them too.
+int most_pieces(const ProductArgs &p, int unit) {
+  if (p.kind != kGroups) return (p.m + unit - 1) / unit;
+  return p.m / unit + (p.groups + 1 < p.m ? p.groups + 1 : p.m);
+}
+
+template <int BM, int BN, int WM, int WN, int D, int KS>
+hipError_t launch_tiles(ProductArgs p, bool b_rows, hipStream_t stream) {
   p.tiles_n = (p.n + BN - 1) / BN;
-  p.tiles_m = (p.m + BM - 1) / BM;
+  p.tiles_m = most_pieces(p, BM);
   int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
-  // ragged groups: each has at most one tile that is not full, the rows after them too
-  if (p.kind == kGroups)
-    tiles = ((int64_t)(p.m / BM) + (p.groups + 1 < p.m ? p.groups + 1 : p.m)) * p.tiles_n;
   if (p.kind == kGradient) tiles *= p.groups;
-  if (tiles * (WM * WN * kWave) >= (int64_t(1) << 32)) return hipErrorInvalidValue;
-  const dim3 grid((uint32_t)tiles), block(WM * WN * kWave);
+  if (tiles * (KS * WM * WN * kWave) >= (int64_t(1) << 32)) return hipErrorInvalidValue;
+  const dim3 grid((uint32_t)tiles), block(KS * WM * WN * kWave);
   const auto go = [&](auto rows, auto full) {
-    hipLaunchKernelGGL(
-        (product_kernel<BM, BN, WM, WN, decltype(rows)::value, decltype(full)::value>), grid,
-        block, 0, stream, p);
+    hipLaunchKernelGGL((product_kernel<BM, BN, WM, WN, D, KS, decltype(rows)::value,
+                                       decltype(full)::value>),
+                       grid, block, 0, stream, p);
     return hipGetLastError();
   };
-  if (p.out_type == HADACORE_FP32)
-    return b_rows ? go(std::true_type{}, std::true_type{}) : go(std::false_type{}, std::true_type{});
+  if (p.out_type == HADACORE_FP32) {
+    if constexpr (BM <= 128)
+      return b_rows ? go(std::true_type{}, std::true_type{})
+                    : go(std::false_type{}, std::true_type{});
+    return hipErrorInvalidValue;  // not chosen
+  }
   return b_rows ? go(std::true_type{}, std::false_type{}) : go(std::false_type{}, std::false_type{});
 }
 
+template <int MT, int RB, int W, int D>
+hipError_t launch_few(ProductArgs p, bool stream_b, hipStream_t stream) {
+  p.tiles_n = (p.n + 16 * RB - 1) / (16 * RB);
+  p.tiles_m = most_pieces(p, 16 * MT);
+  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
+  if (tiles * (W * kWave) >= (int64_t(1) << 32)) return hipErrorInvalidValue;
+  const dim3 grid((uint32_t)tiles), block(W * kWave);
+  const auto go = [&](auto nt, auto full) {
+    hipLaunchKernelGGL(
+        (few_rows_kernel<MT, RB, W, D, decltype(nt)::value, decltype(full)::value>), grid, block,
+        0, stream, p);
+    return hipGetLastError();
+  };
+  if (p.out_type == HADACORE_FP32)
+    return stream_b ? go(std::true_type{}, std::true_type{}) : go(std::false_type{}, std::true_type{});
+  return stream_b ? go(std::true_type{}, std::false_type{}) : go(std::false_type{}, std::false_type{});
+}
+
+// Which kernel.  Few rows (for groups: on average) are a reading of B; else the tile
+// with the least estimated time: turns of the CUs times blocks of k times the time of a
+// step, measured with at most one workgroup to a CU and with all slots taken.
+struct TileTime {
+  int bm, bn, slots;  // workgroups that run together on 256 CUs
+  float alone, full;  // us of a step
+};
+
+// HADACORE_VARIANT=tiles-64|tiles-64x128|tiles-128|tiles-256 forces a tile for every
+// product (testing and tuning; tiles-256 not for 32-bit outputs, which keep the choice).
+int tile_override() {
+  const char *v = getenv("HADACORE_VARIANT");
+  if (v == nullptr || strncmp(v, "tiles-", 6) != 0) return -1;
+  static constexpr const char *kNames[] = {"64", "64x128", "128", "256"};
+  for (int i = 0; i < 4; ++i)
+    if (strcmp(v + 6, kNames[i]) == 0) return i;
+  return -1;
+}
+
 hipError_t launch_product(const ProductArgs &p, bool b_rows, hipStream_t stream) {
-  return launch_product<128, 128, 2, 2>(p, b_rows, stream);
+  const int64_t groups = p.kind == kGroups ? (p.groups < p.m ? p.groups : p.m) : 1;
+  int forced = tile_override();
+  if (forced == 3 && p.out_type == HADACORE_FP32) forced = -1;
+  if (forced < 0 && !b_rows && p.m <= 64 * groups) {
+    // weights of this size do not stay in the last-level cache beside others: streamed, 64
+    // tokens over 32 experts of 2048 x 4096 take 40.6 us instead of 46.8 and 16 rows by
+    // 8192 x 8192 13.9 instead of 14.8; 4096 x 4096 6.3 instead of 5.8
+    const bool stream_b = groups * p.n * p.k >= (int64_t(1) << 26);
+    if (p.m > 16 * groups) return launch_few<2, 2, 4, 2>(p, stream_b, stream);
+    if (groups * p.n < 16 * 512) return launch_few<1, 1, 8, 2>(p, stream_b, stream);
+    return launch_few<1, 2, 4, 2>(p, stream_b, stream);
+  }
+  static constexpr TileTime kTimes[] = {{64, 64, 256, 0.32f, 0.36f},
+                                        {64, 128, 512, 0.48f, 0.81f},
+                                        {128, 128, 512, 0.80f, 1.32f},
+                                        {256, 256, 256, 1.45f, 1.87f}};
+  int best = 0;
+  float least = 0.0f;
+  for (int i = 0; i < 4; ++i) {
+    // 32-bit outputs widen both operands in registers, which the largest tile has not got
+    if (i == 3 && p.out_type == HADACORE_FP32) continue;
+    const TileTime &c = kTimes[i];
+    const float pieces =
+        p.kind == kGroups ? (float)p.m / c.bm + 0.5f * groups : ceilf((float)p.m / c.bm);
+    const float tiles = pieces * ceilf((float)p.n / c.bn) * (p.kind == kGradient ? p.groups : 1);
+    const float time = ceilf(tiles / c.slots) * (tiles <= 256 ? c.alone : c.full);
+    if (i == 0 || time < least) {
+      best = i;
+      least = time;
+    }
+  }
+  if (forced >= 0) best = forced;
+  switch (best) {
+    case 0: return launch_tiles<64, 64, 2, 1, 3, 2>(p, b_rows, stream);
+    case 1: return launch_tiles<64, 128, 2, 2, 3, 1>(p, b_rows, stream);
+    case 2: return launch_tiles<128, 128, 2, 2, 2, 1>(p, b_rows, stream);
+    default: return launch_tiles<256, 256, 2, 4, 2, 1>(p, b_rows, stream);
+  }
 }
 
 // ---- arguments -------------------------------------------------------------------
@@ -1010,7 +1397,7 @@ extern "C" hadacore_status hadacore_matmul_fp8(
   p.n = (int)n;
   p.k = (int)k;
   p.groups = 1;
-  p.kind = kTiles;
+  p.kind = kDense;
   p.out_type = out_dtype;
   const hadacore_status st =
       check_product(p, m, n, k, 1, b_scale_rows == 1 ? n : blocks_of(n));

@@ -249,6 +249,15 @@ def _encode(v):
     return (order[at] | np.where(v < 0, 128, 0)).astype(np.uint8)
 
 
+@pytest.fixture(params=["auto", "tiles-64", "tiles-64x128", "tiles-128", "tiles-256"])
+def variant(request, monkeypatch):
+    if request.param == "auto":
+        monkeypatch.delenv("HADACORE_VARIANT", raising=False)
+    else:
+        monkeypatch.setenv("HADACORE_VARIANT", request.param)
+    return request.param
+
+
 SIZES = [(1, 1, 1), (1, 64, 128), (2, 5, 15), (3, 130, 16), (15, 33, 127), (16, 64, 129), (17, 257, 300),
          (33, 128, 512), (64, 96, 640), (65, 64, 256), (100, 300, 1000), (128, 128, 128),
          (129, 129, 257), (200, 513, 384), (300, 260, 1155), (1, 1000, 4096), (7, 515, 2049),
@@ -258,7 +267,7 @@ SIZES = [(1, 1, 1), (1, 64, 128), (2, 5, 15), (3, 130, 16), (15, 33, 127), (16, 
 @pytest.mark.parametrize("out", OUTS)
 @pytest.mark.parametrize("tall", [128, 1])
 @pytest.mark.parametrize("m,n,k", SIZES)
-def test_matmul(m, n, k, tall, out):
+def test_matmul(m, n, k, tall, out, variant):
     import torch
     rng = np.random.default_rng(m * 7 + n * 3 + k)
     a, sa, ha, hsa = _codes(rng, m, k)
@@ -271,7 +280,7 @@ def test_matmul(m, n, k, tall, out):
 
 @pytest.mark.parametrize("out", OUTS)
 @pytest.mark.parametrize("m,n,gap,first", [(5, 100, 28, 0), (70, 130, 5, 0), (130, 200, 8, 8), (33, 64, 0, 1)])
-def test_matmul_into_a_wider_buffer(m, n, gap, first, out):
+def test_matmul_into_a_wider_buffer(m, n, gap, first, out, variant):
     """Row gaps, and starts and pitches off 16 bytes, are left alone and change nothing."""
     import torch
     rng = np.random.default_rng(m + n)
@@ -285,7 +294,7 @@ def test_matmul_into_a_wider_buffer(m, n, gap, first, out):
     assert (_host(view[:, n:]) == 7).all() and (_host(buf[:first]) == 7).all()
 
 
-def test_matmul_nothing_to_add():
+def test_matmul_nothing_to_add(variant):
     import torch
     z = torch.zeros
     a, b = z((5, 0), dtype=torch.uint8, device="cuda"), z((9, 0), dtype=torch.uint8, device="cuda")
@@ -300,7 +309,7 @@ def test_matmul_nothing_to_add():
 
 @pytest.mark.parametrize("m", [1, 20, 200])
 @pytest.mark.parametrize("out", OUTS)
-def test_matmul_nan_and_inf_stay_in_their_row(m, out):
+def test_matmul_nan_and_inf_stay_in_their_row(m, out, variant):
     """A NaN code or scale reaches the outputs of its row or column only."""
     import torch
     rng = np.random.default_rng(11)
@@ -326,7 +335,7 @@ def test_matmul_nan_and_inf_stay_in_their_row(m, out):
 @pytest.mark.parametrize("out", OUTS)
 @pytest.mark.parametrize("n,k", [(64, 128), (130, 300), (257, 1030)])
 @pytest.mark.parametrize("tokens,ends", GROUPS + [(1000, [500, 500, 990, 1000])])
-def test_grouped(tokens, ends, n, k, out):
+def test_grouped(tokens, ends, n, k, out, variant):
     import torch
     rng = np.random.default_rng(tokens + n + k)
     groups = len(ends)
@@ -357,7 +366,7 @@ def test_grouped(tokens, ends, n, k, out):
 @pytest.mark.parametrize("out", OUTS)
 @pytest.mark.parametrize("n,k", [(1, 128), (130, 77), (257, 300)])
 @pytest.mark.parametrize("tokens,ends", GROUPS + [(0, [0, 0]), (700, [650, 650, 700])])
-def test_weight_gradient(tokens, ends, n, k, out):
+def test_weight_gradient(tokens, ends, n, k, out, variant):
     """From the column quantizers' codes, against 64 bits of the same codes; empty groups."""
     import torch
     dy = to_device(W.random_rows(max(tokens, 1), n, "bf16", seed=n), "bf16")[:tokens]
@@ -390,7 +399,7 @@ def test_weight_gradient_of_one_group():
     assert torch.equal(g, H.matmul_fp8(qd, sd, qx, sx, dtype=torch.float32))
 
 
-def test_ends_out_of_range_stay_in_bounds():
+def test_ends_out_of_range_stay_in_bounds(variant):
     """Ends below 0, past the rows or going down: wrong rows at most, neighbours untouched."""
     import torch
     rng = np.random.default_rng(2)
