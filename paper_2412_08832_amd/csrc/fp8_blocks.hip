@@ -133,22 +133,30 @@ __device__ __forceinline__ float widen(uint32_t h) {
   }
 }
 
-// 8 values of a row from `p` on, of which the first `valid` exist (the others are 0).
-// Rows may start at any 2-byte address; the hardware takes 16-byte loads from there.
+// 8 values of a row, widened.
 template <int DT>
-__device__ __forceinline__ void load8(const uint16_t *p, int valid, float (&v)[8]) {
-  typedef u4 u4_any __attribute__((aligned(2)));
-  if (valid >= 8) {
-    const u4 r = *reinterpret_cast<const u4_any *>(p);
+__device__ __forceinline__ void widen8(u4 raw, float (&v)[8]) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      v[2 * j] = widen<DT>(r[j] & 0xFFFFu);
-      v[2 * j + 1] = widen<DT>(r[j] >> 16);
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j < valid ? widen<DT>(p[j]) : 0.0f;
+  for (int j = 0; j < 4; ++j) {
+    v[2 * j] = widen<DT>(raw[j] & 0xFFFFu);
+    v[2 * j + 1] = widen<DT>(raw[j] >> 16);
   }
+}
+
+// 8 values from `p` on.  Rows may start at any 2-byte address; the hardware takes 16-byte
+// loads from there.
+__device__ __forceinline__ u4 load8(const uint16_t *p) {
+  typedef u4 u4_any __attribute__((aligned(2)));
+  return *reinterpret_cast<const u4_any *>(p);
+}
+
+// The first `valid` < 8 of them, and zeros.
+__device__ __forceinline__ u4 load_some(const uint16_t *p, int valid) {
+  u4 raw = {0, 0, 0, 0};
+#pragma unroll
+  for (int j = 0; j < 7; ++j)
+    if (j < valid) raw[j / 2] |= (uint32_t)p[j] << (16 * (j % 2));
+  return raw;
 }
 
 // Maximum that ignores NaN (fmaxf returns the other operand).
@@ -185,54 +193,112 @@ __device__ __forceinline__ void store_codes8(uint8_t *p, u2 c, int valid) {
   }
 }
 
+// The value of lane ^ BIT, by permutations inside rows of 16 lanes (xor 4: row_half_mirror,
+// which is xor 7, and quad_perm xor 3).
+template <int BIT>
+__device__ __forceinline__ float lane_xor(float v) {
+  const auto dpp = [](int x, auto ctrl) {
+    return __builtin_amdgcn_mov_dpp(x, decltype(ctrl)::value, 0xF, 0xF, true);
+  };
+  const int x = __builtin_bit_cast(int, v);
+  if constexpr (BIT == 1)
+    return __builtin_bit_cast(float, dpp(x, std::integral_constant<int, 0xB1>{}));
+  else if constexpr (BIT == 2)
+    return __builtin_bit_cast(float, dpp(x, std::integral_constant<int, 0x4E>{}));
+  else
+    return __builtin_bit_cast(float, dpp(dpp(x, std::integral_constant<int, 0x141>{}),
+                                         std::integral_constant<int, 0x1B>{}));
+}
+
+// Maximum over 16 lanes: xor 1 and 2, then the mirrors of 8 and 16 lanes, whose halves
+// hold one value each by then.
+__device__ __forceinline__ float max16(float a) {
+  a = fmaxf(a, lane_xor<1>(a));
+  a = fmaxf(a, lane_xor<2>(a));
+  a = fmaxf(a, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, a), 0x141,
+                                                                  0xF, 0xF, true)));
+  return fmaxf(a, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, a),
+                                                                     0x140, 0xF, 0xF, true)));
+}
+
+template <int BIT>
+__device__ __forceinline__ void lane_butterflies(float (&v)[8], int lane) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float other = lane_xor<BIT>(v[j]);
+    v[j] = (lane & BIT) != 0 ? other - v[j] : v[j] + other;
+  }
+}
+
+// Blocks of a group of lanes: 8192 rows of 8192 take 34.2 us with two (5.9 TB/s), 40.2
+// with one, 34.9 with four.
+constexpr int kTurns = 2;
+
 // Rows rotated by 2^L <= 64 values: 16 lanes hold a block of 128, 8 consecutive values
 // each, so the stages on index bits 0-2 are in registers and those on bits 3-5 between
-// lanes.  HBM-bound: one 16-byte load and one 8-byte store per lane.
+// lanes.  HBM-bound; a group of lanes takes kTurns blocks, whose loads go out together.
 template <int DT, int L>
 __global__ __launch_bounds__(256) void short_rotation_kernel(
     const uint16_t *in, int64_t in_stride, uint8_t *codes, int64_t codes_stride, float *scales,
     int64_t scales_stride, int64_t m, int k, int blocks, float scale) {
   const int sub = threadIdx.x & 15;
-  const int64_t total = m * blocks, step = (int64_t)gridDim.x * 16;
-  // every lane of a wave takes part in the exchanges, so the bound is the wave's
-  for (int64_t i0 = (int64_t)blockIdx.x * 16 + (threadIdx.x / kWave) * 4; i0 < total; i0 += step) {
-    const int64_t i = i0 + ((threadIdx.x >> 4) & 3);
-    const int64_t row = i < total ? i / blocks : 0;
-    const int block = i < total ? (int)(i - row * blocks) : 0;
-    const int col = block * kBlock + sub * 8;
-    const int valid = i < total ? k - col : 0;
-    float v[8];
-    load8<DT>(in + row * in_stride + col, valid, v);
+  const int64_t total = m * blocks, step = (int64_t)gridDim.x * 16 * kTurns;
+  // every lane of a wave takes part in the exchanges, so the bound is the workgroup's; the
+  // division is in 32 bits where it can be
+  for (int64_t i0 = (int64_t)blockIdx.x * 16 * kTurns; i0 < total; i0 += step) {
+    u4 raw[kTurns];
+    int64_t row[kTurns];
+    int block[kTurns], valid[kTurns];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= scale;
+    for (int u = 0; u < kTurns; ++u) {
+      const int64_t i = i0 + u * 16 + (threadIdx.x >> 4);
+      row[u] = i >= total         ? 0
+               : total >> 32 == 0 ? (int64_t)((uint32_t)i / (uint32_t)blocks)
+                                  : i / blocks;
+      block[u] = i < total ? (int)(i - row[u] * blocks) : 0;
+      valid[u] = i < total ? k - block[u] * kBlock - sub * 8 : 0;
+    }
+    bool some = false;
 #pragma unroll
-    for (int b = 0; b < 3; ++b) {
-      if (b >= L) break;
+    for (int u = 0; u < kTurns; ++u) {
+      some |= valid[u] < 8;
+      const uint16_t *from = in + row[u] * in_stride;
+      raw[u] = u4{0, 0, 0, 0};
+      if (valid[u] >= 8) raw[u] = load8(from + block[u] * kBlock + sub * 8);
+    }
+    if (some) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if ((j & (1 << b)) == 0) {
-          const float x = v[j], y = v[j | (1 << b)];
-          v[j] = x + y;
-          v[j | (1 << b)] = x - y;
+      for (int u = 0; u < kTurns; ++u)
+        if (valid[u] < 8)
+          raw[u] = load_some(in + row[u] * in_stride + block[u] * kBlock + sub * 8, valid[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kTurns; ++u) {
+      float v[8];
+      widen8<DT>(raw[u], v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] *= scale;
+#pragma unroll
+      for (int b = 0; b < 3; ++b) {
+        if (b >= L) break;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if ((j & (1 << b)) == 0) {
+            const float x = v[j], y = v[j | (1 << b)];
+            v[j] = x + y;
+            v[j | (1 << b)] = x - y;
+          }
         }
       }
-    }
-#pragma unroll
-    for (int b = 3; b < 6; ++b) {
-      if (b >= L) break;
-      const int bit = 1 << (b - 3);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float other = __shfl_xor(v[j], bit);
-        v[j] = (sub & bit) != 0 ? other - v[j] : v[j] + other;
+      if constexpr (L > 3) lane_butterflies<1>(v, sub);
+      if constexpr (L > 4) lane_butterflies<2>(v, sub);
+      if constexpr (L > 5) lane_butterflies<4>(v, sub);
+      const float a = max16(abs_max(v));
+      if (valid[u] > 0) {
+        store_codes8(codes + row[u] * codes_stride + block[u] * kBlock + sub * 8,
+                     codes8(v, inverse_scale(a)), valid[u]);
+        if (sub == 0) scales[row[u] * scales_stride + block[u]] = a / 448.0f;
       }
-    }
-    float a = abs_max(v);
-#pragma unroll
-    for (int d = 1; d < 16; d *= 2) a = fmaxf(a, __shfl_xor(a, d));
-    if (valid > 0) {
-      store_codes8(codes + row * codes_stride + col, codes8(v, inverse_scale(a)), valid);
-      if (sub == 0) scales[row * scales_stride + block] = a / 448.0f;
     }
   }
 }
@@ -242,7 +308,7 @@ hipError_t short_rotations(const uint16_t *in, int64_t in_stride, uint8_t *codes
                            int64_t codes_stride, float *scales, int64_t scales_stride, int64_t m,
                            int k, int L, float scale, hipStream_t stream) {
   const int blocks = (k + kBlock - 1) / kBlock;
-  const int64_t groups = (m * blocks + 15) / 16;
+  const int64_t groups = (m * blocks + 16 * kTurns - 1) / (16 * kTurns);
   const dim3 grid((uint32_t)(groups < (1 << 20) ? groups : (1 << 20)));
   const auto go = [&](auto l) {
     hipLaunchKernelGGL((short_rotation_kernel<DT, decltype(l)::value>), grid, dim3(256), 0, stream,
@@ -317,10 +383,27 @@ __global__ __launch_bounds__(256) void tile_kernel(TileArgs p) {
   const int col = col0 + cg * 8;
   float v[8][8];
   const int rows = row_end - row0;  // <= 0: a block past the last group, all zero
+  {
+    // all loads before the first use; rows past the end repeat the last one, as zeros
+    u4 raw[8];
+    if (p.k - col >= 8) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = rg * 8 + i;
-    load8<DT>(in + (int64_t)(row0 + r) * p.in_stride + col, r < rows ? p.k - col : 0, v[i]);
+      for (int i = 0; i < 8; ++i) {
+        const int r = rg * 8 + i, last = rows > 0 ? rows - 1 : 0;
+        raw[i] = load8(in + (int64_t)(row0 + (r < last ? r : last)) * p.in_stride + col);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        raw[i] = rg * 8 + i < rows
+                     ? load_some(in + (int64_t)(row0 + rg * 8 + i) * p.in_stride + col, p.k - col)
+                     : u4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (rg * 8 + i >= rows) raw[i] = u4{0, 0, 0, 0};
+      widen8<DT>(raw[i], v[i]);
+    }
   }
   float mul[8];
   if constexpr (COLUMNS) {
@@ -334,14 +417,15 @@ __global__ __launch_bounds__(256) void tile_kernel(TileArgs p) {
       if ((t & 48) == 0) maxima[wave][cg * 8 + j] = a;
     }
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int c = cg * 8 + j;
-      const float a = fmaxf(fmaxf(maxima[0][c], maxima[1][c]), fmaxf(maxima[2][c], maxima[3][c]));
-      mul[j] = inverse_scale(a);
-      if (rg == 0 && col + j < p.k)
-        p.scales[(int64_t)(col + j) * p.scales_stride + out_block] = a / 448.0f;
+    if (t < kBlock) {
+      const float a = fmaxf(fmaxf(maxima[0][t], maxima[1][t]), fmaxf(maxima[2][t], maxima[3][t]));
+      maxima[0][t] = inverse_scale(a);
+      if (col0 + t < p.k)
+        p.scales[(int64_t)(col0 + t) * p.scales_stride + out_block] = a / 448.0f;
     }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mul[j] = maxima[0][cg * 8 + j];
   } else {
     float a = abs_max(v[0]);
 #pragma unroll
@@ -506,25 +590,21 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   }
 }
 
-// 16 consecutive outputs of a row, of which the first `valid` exist.
-template <int OUT>
-__device__ __forceinline__ void store_row16(void *out, int64_t at, const float (&v)[16], int valid,
-                                            bool aligned) {
-  if (valid >= 16 && aligned) {
+// 16 bytes of consecutive outputs of a row, of which the first `valid` exist.
+template <int OUT, int N>
+__device__ __forceinline__ void store_row(void *out, int64_t at, const float (&v)[N], int valid,
+                                          bool aligned) {
+  if (valid >= N && aligned) {
     if constexpr (OUT == HADACORE_FP32) {
-      f4 *p = reinterpret_cast<f4 *>(static_cast<float *>(out) + at);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) p[q] = f4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+      *reinterpret_cast<f4 *>(static_cast<float *>(out) + at) = f4{v[0], v[1], v[2], v[3]};
     } else {
-      u4 *p = reinterpret_cast<u4 *>(static_cast<uint16_t *>(out) + at);
-#pragma unroll
-      for (int q = 0; q < 2; ++q)
-        p[q] = u4{pack2<OUT>(v[8 * q], v[8 * q + 1]), pack2<OUT>(v[8 * q + 2], v[8 * q + 3]),
-                  pack2<OUT>(v[8 * q + 4], v[8 * q + 5]), pack2<OUT>(v[8 * q + 6], v[8 * q + 7])};
+      *reinterpret_cast<u4 *>(static_cast<uint16_t *>(out) + at) =
+          u4{pack2<OUT>(v[0], v[1]), pack2<OUT>(v[2], v[3]), pack2<OUT>(v[4], v[5]),
+             pack2<OUT>(v[6], v[7])};
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
+    for (int j = 0; j < N; ++j)
       if (j < valid) store_out<OUT>(out, at + j, v[j]);
   }
 }
@@ -590,6 +670,12 @@ __device__ __forceinline__ TileAt tile_at(uint32_t id, uint32_t total, int tiles
   return {matrix, band * kBand + in_band % high, in_band / high};
 }
 
+// Which of 64 columns row i of the j-th of four MFMAs is (a lane holds rows 4 g .. 4 g + 3).
+template <bool FULL>
+__device__ __forceinline__ int tile_column(int j, int i) {
+  return FULL ? 16 * j + i : 32 * (j >> 1) + 8 * (i >> 2) + 4 * (j & 1) + (i & 3);
+}
+
 // The whole tiles' kernel: BM x BN outputs by WM x WN waves, in steps of a block of k.
 //
 // The rows of A and B and their scales go through D stages of LDS, loaded D - 1 steps
@@ -600,8 +686,9 @@ __device__ __forceinline__ TileAt tile_at(uint32_t id, uint32_t total, int tiles
 // columns n of one row m: its A scale is one value, and its stores are along the row.
 // Lane l of an MFMA holds 32 bytes of row l & 15 of either operand: the 16-byte chunks
 // g and g + 4, g = l >> 4, of the 128 (any order of k will do that both share).  The rows
-// of B are laid out in LDS so that row 16 j + i of 64 is column 16 (i / 4) + 4 j + i % 4 of
-// the tile: lane group g then holds columns 16 g .. 16 g + 15 over its four MFMAs.
+// of B are laid out in LDS so that a lane's results make 16-byte stores and the stores of
+// its four lane groups 64 bytes of a row: in 32 bits the j-th MFMA's rows are its columns,
+// in 16 bits two MFMAs' results are joined (tile_column).
 //
 // LDS rows are 128 bytes; chunk c of row r lies at c ^ ((r >> 1) & 7), which the loads
 // obey by choosing their global chunk, since LDS addresses of a load run with the lane.
@@ -674,7 +761,7 @@ __global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs 
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
     const int s = (i < kLoadsA ? i : i - kLoadsA) * kThreads + t, r = s >> 3;
-    const int c = (r & ~63) + 16 * ((r & 15) >> 2) + 4 * ((r >> 4) & 3) + (r & 3);
+    const int c = (r & ~63) + tile_column<FULL>((r >> 4) & 3, r & 15);
     const int row = i < kLoadsA ? (r < rows ? r : rows - 1) : (c < columns ? c : columns - 1);
     off[i] = row * (int)(i < kLoadsA ? p.a_pitch : p.b_pitch) + (((s & 7) ^ ((s >> 4) & 7)) << 4);
   }
@@ -761,7 +848,7 @@ __global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs 
 #pragma unroll
       for (int j = 0; j < TN; ++j)
         col[j] = *reinterpret_cast<const f4 *>(
-            &scales[stage][BM + wn * (BN / WN) + (j & ~3) * 16 + 16 * g + 4 * (j & 3)]);
+            &scales[stage][BM + wn * (BN / WN) + (j & ~3) * 16 + tile_column<FULL>(j & 3, 4 * g)]);
     } else {
       uniform_b = scales[stage][BM + wn * (BN / WN) / kBlock];
     }
@@ -846,26 +933,26 @@ __global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs 
         for (int q = 0; q < KS - 1; ++q) acc[i][j] += sums[((q * TM + i) * TN + j) * kThreads + t];
   }
 
-  const int wide = FULL ? 4 : 2;
+  constexpr int kWide = FULL ? 4 : 2, kStore = 16 / kWide;
   const bool aligned =
-      ((reinterpret_cast<uintptr_t>(p.out) | (uintptr_t)((p.out_pitch | out_at) * wide)) & 15) == 0;
+      ((reinterpret_cast<uintptr_t>(p.out) | (uintptr_t)((p.out_pitch | out_at) * kWide)) & 15) == 0;
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int row = m0 + wm * (BM / WM) + i * 16 + li;
     if (row >= m_end) continue;
 #pragma unroll
-    for (int j = 0; j < TN; j += 4) {
-      const int column = n0 + wn * (BN / WN) + j * 16 + 16 * g;
-      float v[16];
+    for (int j = 0; j < TN; j += kStore / 4) {
+      const int column = n0 + wn * (BN / WN) + (j & ~3) * 16 + tile_column<FULL>(j & 3, 4 * g);
+      float v[kStore];
 #pragma unroll
-      for (int q = 0; q < 16; ++q) v[q] = acc[i][j + q / 4][q % 4];
-      const int64_t at = out_at + (int64_t)row * p.out_pitch + column;
+      for (int q = 0; q < kStore; ++q) v[q] = acc[i][j + q / 4][q % 4];
+      const int64_t to = out_at + (int64_t)row * p.out_pitch + column;
       if constexpr (FULL)
-        store_row16<HADACORE_FP32>(p.out, at, v, p.n - column, aligned);
+        store_row<HADACORE_FP32>(p.out, to, v, p.n - column, aligned);
       else if (p.out_type == HADACORE_FP16)
-        store_row16<HADACORE_FP16>(p.out, at, v, p.n - column, aligned);
+        store_row<HADACORE_FP16>(p.out, to, v, p.n - column, aligned);
       else
-        store_row16<HADACORE_BF16>(p.out, at, v, p.n - column, aligned);
+        store_row<HADACORE_BF16>(p.out, to, v, p.n - column, aligned);
     }
   }
 }

@@ -461,39 +461,42 @@ def _stream_of(stream, device: int):
 
 
 def _padded_rows(shape: tuple, device):
-    """A uint8 tensor whose rows start on 16-byte boundaries and are readable, as zeros,
-    up to the next one: what the quantizers write and the products read."""
+    """A uint8 tensor whose rows start on 16-byte boundaries and are readable up to the
+    next one (what lies there is ignored): what the quantizers write and the products read."""
     k = shape[-1]
     if k % 16 == 0:
         return _torch.empty(shape, dtype=_torch.uint8, device=device)
-    # whole rows are cleared, a copy of 1/3 of the quantizer's bytes, for odd sizes only
-    return _torch.zeros((*shape[:-1], -(-k // 16) * 16), dtype=_torch.uint8,
+    return _torch.empty((*shape[:-1], (k + 15) // 16 * 16), dtype=_torch.uint8,
                         device=device)[..., :k]
 
 
-def _check_codes(name: str, codes, scales, dim: int, rows: int, device: int):
-    """Codes and scales of a product's operand: types, devices, unit column strides, the
-    shape of the scales (``rows`` of them) and that every row of codes is readable up to
-    the next multiple of 16 bytes."""
+def _operand(name: str, codes, scales, rows: int, device: int):
+    """Checks of an operand's codes (2-D, or 3-D for a batch) and scales, of which there are
+    ``rows`` to a matrix: types, devices, unit column strides, shapes, and that every row of
+    codes is readable up to the next multiple of 16 bytes.  Returns the row strides of both;
+    of a single row, whose stride is never used, one that passes."""
     if codes.dtype not in _code_types:
         raise TypeError(f"{name}: codes must be uint8 or float8_e4m3fn, got {codes.dtype}")
     if scales.dtype != _torch.float32:
         raise TypeError(f"{name}: scales must be float32, got {scales.dtype}")
-    if codes.dim() != dim or scales.dim() != dim:
-        raise ValueError(f"{name}: expected {dim}-D codes and scales")
+    shape, steps = codes.shape, codes.stride()
+    k = shape[-1]
+    blocks = (k + 127) >> 7
+    want = (*shape[:-2], rows, blocks)
+    if scales.shape != want:
+        raise ValueError(f"{name}: expected scales of shape {want}, got {tuple(scales.shape)}")
     if codes.get_device() != device or scales.get_device() != device:
         raise ValueError(f"{name}: all tensors must be on the same ROCm device")
-    k = codes.shape[-1]
-    want = (*codes.shape[:-2], rows, (k + 127) // 128)
-    if tuple(scales.shape) != want:
-        raise ValueError(f"{name}: expected scales of shape {want}, got {tuple(scales.shape)}")
-    if (k > 1 and codes.stride(-1) != 1) or (want[-1] > 1 and scales.stride(-1) != 1):
+    scale_steps = scales.stride()
+    if (k > 1 and steps[-1] != 1) or (blocks > 1 and scale_steps[-1] != 1):
         raise ValueError(f"{name}: rows must be contiguous (column stride 1)")
-    if k % 16 and codes.numel():
-        last = sum((n - 1) * s for n, s in zip(codes.shape[:-1], codes.stride()))
-        if codes.storage_offset() + last + (k + 15) // 16 * 16 > codes.untyped_storage().nbytes():
+    if k & 15 and codes.numel():
+        last = sum((n - 1) * s for n, s in zip(shape[:-1], steps))
+        if codes.storage_offset() + last + ((k + 15) & ~15) > codes.untyped_storage().nbytes():
             raise ValueError(f"{name}: the last row of codes must be readable up to a multiple of "
                              "16 bytes (as the quantizers allocate it)")
+    return (0 if k == 0 else steps[-2] if shape[-2] > 1 else (k + 15) & ~15,
+            scale_steps[-2] if rows > 1 else blocks)
 
 
 def _row_stride(t, least: int) -> int:
@@ -505,7 +508,7 @@ def _pitch(codes) -> int:
     """The row stride of codes (of a single row: its padded length; of empty rows 0)."""
     if codes.shape[-1] == 0:
         return 0
-    return codes.stride(-2) if codes.shape[-2] > 1 else -(-codes.shape[-1] // 16) * 16
+    return codes.stride(-2) if codes.shape[-2] > 1 else (codes.shape[-1] + 15) & ~15
 
 
 def _new_scales(scales, shape: tuple, device):
@@ -631,16 +634,16 @@ def quantize_fp8_tiles(w, transposed: bool = False, stream=None):
 
 
 def _product_out(out, shape: tuple, dtype, like):
-    """The output of a product and its type's code."""
+    """The output of a product, its type's code and its row stride."""
     if out is None:
         out = _torch.empty(shape, dtype=dtype or _torch.bfloat16, device=like.device)
-    elif tuple(out.shape) != shape or out.device != like.device or \
+    elif out.shape != shape or out.device != like.device or \
             (shape[-1] > 1 and out.stride(-1) != 1) or (dtype is not None and out.dtype != dtype):
         raise ValueError(f"out must be a {shape} tensor of the output type with contiguous rows")
     code = _out_codes.get(out.dtype)
     if code is None:
         raise TypeError(f"expected an output of float16, bfloat16 or float32, got {out.dtype}")
-    return out, code
+    return out, code, out.stride(-2) if shape[-2] > 1 else shape[-1]
 
 
 def matmul_fp8(a, a_scales, b, b_scales, out=None, dtype=None, stream=None):
@@ -657,19 +660,17 @@ def matmul_fp8(a, a_scales, b, b_scales, out=None, dtype=None, stream=None):
         raise ValueError("expected 2-D tensors on a ROCm device")
     device = a.get_device()
     m, k = a.shape
-    n = b.shape[0]
-    if b.shape[1] != k:
-        raise ValueError(f"a has {k} columns and b {b.shape[1]}")
-    tiles = (n + 127) // 128
-    by_row = b_scales.dim() == 2 and b_scales.shape[0] == n and n != tiles
-    _check_codes("a", a, a_scales, 2, m, device)
-    _check_codes("b", b, b_scales, 2, n if by_row else tiles, device)
-    out, code = _product_out(out, (m, n), dtype, a)
-    blocks = (k + 127) // 128
-    _call("hadacore_matmul_fp8", device, a.data_ptr(), _pitch(a), a_scales.data_ptr(),
-          _row_stride(a_scales, blocks), b.data_ptr(), _pitch(b), b_scales.data_ptr(),
-          _row_stride(b_scales, blocks), 1 if by_row else 128, out.data_ptr(),
-          _row_stride(out, n), code, m, n, k, _stream_of(stream, device))
+    n, k_b = b.shape
+    if k_b != k:
+        raise ValueError(f"a has {k} columns and b {k_b}")
+    tiles = (n + 127) >> 7
+    by_row = n != tiles and b_scales.dim() == 2 and b_scales.shape[0] == n
+    a_stride, sa_stride = _operand("a", a, a_scales, m, device)
+    b_stride, sb_stride = _operand("b", b, b_scales, n if by_row else tiles, device)
+    out, code, out_stride = _product_out(out, (m, n), dtype, a)
+    _call("hadacore_matmul_fp8", device, a.data_ptr(), a_stride, a_scales.data_ptr(), sa_stride,
+          b.data_ptr(), b_stride, b_scales.data_ptr(), sb_stride, 1 if by_row else 128,
+          out.data_ptr(), out_stride, code, m, n, k, _stream_of(stream, device))
     return out
 
 
@@ -686,20 +687,19 @@ def grouped_matmul_fp8(a, a_scales, b, b_scales, ends, out=None, dtype=None, str
         raise ValueError("expected a 2-D and a 3-D tensor on a ROCm device")
     device = a.get_device()
     m, k = a.shape
-    groups, n = b.shape[:2]
-    if b.shape[2] != k:
-        raise ValueError(f"a has {k} columns and b {b.shape[2]}")
+    groups, n, k_b = b.shape
+    if k_b != k:
+        raise ValueError(f"a has {k} columns and b {k_b}")
     _check_ends(ends, device)
-    if ends.numel() != groups:
-        raise ValueError(f"{ends.numel()} ends for {groups} groups")
-    _check_codes("a", a, a_scales, 2, m, device)
-    _check_codes("b", b, b_scales, 3, (n + 127) // 128, device)
-    out, code = _product_out(out, (m, n), dtype, a)
-    blocks = (k + 127) // 128
-    _call("hadacore_matmul_fp8_grouped", device, a.data_ptr(), _pitch(a), a_scales.data_ptr(),
-          _row_stride(a_scales, blocks), b.data_ptr(), _pitch(b), b.stride(0), b_scales.data_ptr(),
-          _row_stride(b_scales, blocks), b_scales.stride(0), ends.data_ptr(), groups,
-          out.data_ptr(), _row_stride(out, n), code, m, n, k, _stream_of(stream, device))
+    if ends.shape[0] != groups:
+        raise ValueError(f"{ends.shape[0]} ends for {groups} groups")
+    a_stride, sa_stride = _operand("a", a, a_scales, m, device)
+    b_stride, sb_stride = _operand("b", b, b_scales, (n + 127) >> 7, device)
+    out, code, out_stride = _product_out(out, (m, n), dtype, a)
+    _call("hadacore_matmul_fp8_grouped", device, a.data_ptr(), a_stride, a_scales.data_ptr(),
+          sa_stride, b.data_ptr(), b_stride, b.stride(0), b_scales.data_ptr(), sb_stride,
+          b_scales.stride(0), ends.data_ptr(), groups, out.data_ptr(), out_stride, code, m, n, k,
+          _stream_of(stream, device))
     return out
 
 
@@ -718,19 +718,20 @@ def grouped_weight_gradient_fp8(dy, dy_scales, x, x_scales, ends=None, out=None,
         raise ValueError("expected 2-D tensors on a ROCm device")
     device = dy.get_device()
     n, places = dy.shape
-    k = x.shape[0]
-    if x.shape[1] != places:
-        raise ValueError(f"dy has {places} places and x {x.shape[1]}")
-    _check_codes("dy", dy, dy_scales, 2, n, device)
-    _check_codes("x", x, x_scales, 2, k, device)
-    if ends is not None:
+    k, places_x = x.shape
+    if places_x != places:
+        raise ValueError(f"dy has {places} places and x {places_x}")
+    dy_stride, sdy_stride = _operand("dy", dy, dy_scales, n, device)
+    x_stride, sx_stride = _operand("x", x, x_scales, k, device)
+    if ends is None:
+        groups, ends_ptr, shape = 1, None, (n, k)
+    else:
         _check_ends(ends, device)
-    groups = 1 if ends is None else ends.numel()
-    out, code = _product_out(out, (n, k) if ends is None else (groups, n, k), dtype, dy)
-    blocks = places // 128
-    _call("hadacore_weight_gradient_fp8_grouped", device, dy.data_ptr(), _pitch(dy),
-          dy_scales.data_ptr(), _row_stride(dy_scales, blocks), x.data_ptr(), _pitch(x),
-          x_scales.data_ptr(), _row_stride(x_scales, blocks),
-          None if ends is None else ends.data_ptr(), groups, out.data_ptr(), _row_stride(out, k),
-          0 if ends is None else out.stride(0), code, places, n, k, _stream_of(stream, device))
+        groups, ends_ptr = ends.shape[0], ends.data_ptr()
+        shape = (groups, n, k)
+    out, code, out_stride = _product_out(out, shape, dtype, dy)
+    _call("hadacore_weight_gradient_fp8_grouped", device, dy.data_ptr(), dy_stride,
+          dy_scales.data_ptr(), sdy_stride, x.data_ptr(), x_stride, x_scales.data_ptr(), sx_stride,
+          ends_ptr, groups, out.data_ptr(), out_stride, out.stride(0) if groups > 1 else 0, code,
+          places, n, k, _stream_of(stream, device))
     return out
