@@ -98,28 +98,28 @@ __device__ __forceinline__ Piece find_piece(const int32_t *ends, int groups, int
   return {-1, 0, 0};
 }
 
-// The blocks of 128 rows before group g, and in it, with every group padded to whole
+// The blocks of 128 rows before group `group`, and in it, with every group padded to whole
 // blocks.  Called by whole waves.
-__device__ __forceinline__ void group_blocks(const int32_t *ends, int groups, int rows, int g,
+__device__ __forceinline__ void group_blocks(const int32_t *ends, int groups, int rows, int group,
                                              int &before, int &count) {
   const int lane = threadIdx.x & (kWave - 1);
-  int sum = 0, own = 0;
-  for (int i = lane; i <= g && i < groups; i += kWave) {
-    const int low = i > 0 ? clamp_end(ends[i - 1], rows) : 0;
-    const int high = clamp_end(ends[i], rows);
-    const int b = high > low ? (high - low + kBlock - 1) / kBlock : 0;
-    if (i < g)
-      sum += b;
-    else
-      own = b;
+  int base = 0, start = 0;  // blocks and rows before these 64 groups
+  for (int g0 = 0; g0 < groups; g0 += kWave) {
+    const int g = g0 + lane;
+    const int high = g < groups ? clamp_end(ends[g], rows) : rows;
+    const int low = __builtin_amdgcn_update_dpp(start, high, 0x138, 0xF, 0xF, false);
+    const int blocks = g < groups && high > low ? (high - low + kBlock - 1) / kBlock : 0;
+    const int sum = prefix_sum(blocks);
+    if (group < g0 + kWave) {
+      before = base + __builtin_amdgcn_readlane(sum - blocks, group - g0);
+      count = __builtin_amdgcn_readlane(blocks, group - g0);
+      return;
+    }
+    base += __builtin_amdgcn_readlane(sum, kWave - 1);
+    start = __builtin_amdgcn_readlane(high, kWave - 1);
   }
-#pragma unroll
-  for (int d = kWave / 2; d > 0; d /= 2) {
-    sum += __shfl_xor(sum, d);
-    own += __shfl_xor(own, d);
-  }
-  before = __builtin_amdgcn_readfirstlane(sum);
-  count = __builtin_amdgcn_readfirstlane(own);
+  before = base;
+  count = 0;
 }
 
 // ---- quantizers ------------------------------------------------------------------
@@ -501,7 +501,9 @@ struct ProductArgs {
   const int32_t *ends;
   int groups;
   int m, n, k;
-  int tiles_m, tiles_n;  // the grid (kGradient: of each group; kGroups: at most)
+  int tiles_m, tiles_n;  // the tiles (kGradient: of each group; kGroups: at most)
+  uint32_t tiles;        // in all
+  bool nt_out;           // outputs with the streaming cache policy
   int kind, out_type;
 };
 
@@ -593,15 +595,19 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 // 16 bytes of consecutive outputs of a row, of which the first `valid` exist.
 template <int OUT, int N>
 __device__ __forceinline__ void store_row(void *out, int64_t at, const float (&v)[N], int valid,
-                                          bool aligned) {
+                                          bool aligned, bool nt) {
   if (valid >= N && aligned) {
-    if constexpr (OUT == HADACORE_FP32) {
-      *reinterpret_cast<f4 *>(static_cast<float *>(out) + at) = f4{v[0], v[1], v[2], v[3]};
-    } else {
-      *reinterpret_cast<u4 *>(static_cast<uint16_t *>(out) + at) =
-          u4{pack2<OUT>(v[0], v[1]), pack2<OUT>(v[2], v[3]), pack2<OUT>(v[4], v[5]),
-             pack2<OUT>(v[6], v[7])};
-    }
+    u4 bits;
+    if constexpr (OUT == HADACORE_FP32)
+      bits = __builtin_bit_cast(u4, f4{v[0], v[1], v[2], v[3]});
+    else
+      bits = u4{pack2<OUT>(v[0], v[1]), pack2<OUT>(v[2], v[3]), pack2<OUT>(v[4], v[5]),
+                pack2<OUT>(v[6], v[7])};
+    u4 *to = reinterpret_cast<u4 *>(static_cast<char *>(out) + at * (OUT == HADACORE_FP32 ? 4 : 2));
+    if (nt)  // in asm: the compiler would make one ordinary store of the two branches
+      asm volatile("global_store_dwordx4 %0, %1, off sc1 nt" ::"v"(to), "v"(bits) : "memory");
+    else
+      *to = bits;
   } else {
 #pragma unroll
     for (int j = 0; j < N; ++j)
@@ -638,11 +644,13 @@ struct Operand<true> {
       }
     }
   }
+  __device__ __forceinline__ static f4 part(int s, const Operand &x, const Operand &y, f4 r) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.values[s], y.values[s], r, 0, 0, 0);
+  }
   __device__ __forceinline__ static f4 product(const Operand &x, const Operand &y) {
     f4 r = {0, 0, 0, 0};
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
-      r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.values[s], y.values[s], r, 0, 0, 0);
+    for (int s = 0; s < 4; ++s) r = part(s, x, y, r);
     return r;
   }
 };
@@ -692,7 +700,7 @@ __device__ __forceinline__ int tile_column(int j, int i) {
 //
 // LDS rows are 128 bytes; chunk c of row r lies at c ^ ((r >> 1) & 7), which the loads
 // obey by choosing their global chunk, since LDS addresses of a load run with the lane.
-template <int BM, int BN, int WM, int WN, int D, int KS, bool BROWS, bool FULL>
+template <int BM, int BN, int WM, int WN, int D, int KS, bool LOOP, bool BROWS, bool FULL>
 __global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs p) {
   constexpr int kThreads = WM * WN * kWave;  // of one share of k
   constexpr int TM = BM / WM / 16, TN = BN / WN / 16;  // MFMA tiles of a wave
@@ -705,6 +713,7 @@ __global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs 
   constexpr int kLoads = kTiles + kScales;
   static_assert(kLoads * (D - 2) < 64, "loads in flight that one wait can count");
   constexpr int kStageBytes = (BM + BN) * kBlock;
+  static_assert(!LOOP || (D == 2 && KS == 1), "a loop over tiles loads one block ahead");
   __shared__ __align__(16) uint8_t tiles[KS * D * kStageBytes];
   __shared__ __align__(16) float scales_of[KS][D][kScales * kThreads];
 
@@ -716,65 +725,89 @@ __global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs 
   float (*const scales)[kScales * kThreads] = scales_of[share];
   const int g = lane >> 4, li = lane & 15;
 
-  // which tile
-  int m0, n0, m_end = p.m, kb0 = 0, kb1 = (p.k + kBlock - 1) / kBlock;
-  const uint8_t *b = p.b;
-  const float *sb = p.sb;
-  int64_t out_at = 0;
-  const TileAt tile = tile_at(blockIdx.x, gridDim.x, p.tiles_m, p.tiles_n);
-  n0 = tile.n * BN;
-  if (p.kind == kGroups) {
-    const Piece piece = find_piece(p.ends, p.groups, p.m, BM, tile.m, true);
-    if (piece.group < 0) return;
-    m0 = piece.low;
-    m_end = piece.high;
-    if (m0 < 0 || m0 >= m_end) return;
-    if (piece.group == p.groups) {
-      kb1 = 0;  // rows after the last group: zeros
-    } else {
-      b += piece.group * p.b_batch;
-      sb += piece.group * p.sb_batch;
-    }
-  } else {
-    m0 = tile.m * BM;
-    if (p.kind == kGradient) {
-      out_at = tile.matrix * p.out_batch;
+  const int tail = p.k & (kBlock - 1), kb_tail = tail != 0 ? p.k / kBlock : -1;
+
+  // Tile `id`: its rows and columns, where its outputs start, and its blocks of k.
+  struct Tile {
+    int m0, n0, m_end, kb0, kb1;
+    int64_t out_at;
+    const uint8_t *b;
+    const float *sb;
+  };
+  const auto place = [&](uint32_t id, Tile &to) {
+    const TileAt at = tile_at(id, p.tiles, p.tiles_m, p.tiles_n);
+    to = {at.m * BM, at.n * BN, p.m, 0, (p.k + kBlock - 1) / kBlock, 0, p.b, p.sb};
+    if (p.kind == kGroups) {
+      const Piece piece = find_piece(p.ends, p.groups, p.m, BM, at.m, true);
+      to.m0 = piece.low;
+      to.m_end = piece.high;
+      if (piece.group < 0 || to.m0 < 0 || to.m0 >= to.m_end) return false;
+      if (piece.group == p.groups) {
+        to.kb1 = 0;  // rows after the last group: zeros
+      } else {
+        to.b += piece.group * p.b_batch;
+        to.sb += piece.group * p.sb_batch;
+      }
+    } else if (p.kind == kGradient) {
+      to.out_at = at.matrix * p.out_batch;
       if (p.ends != nullptr) {
         int before, count;
-        group_blocks(p.ends, p.groups, p.k, tile.matrix, before, count);
-        kb0 = before < kb1 ? before : kb1;
-        kb1 = before + count < kb1 ? before + count : kb1;
+        group_blocks(p.ends, p.groups, p.k, at.matrix, before, count);
+        to.kb0 = before < to.kb1 ? before : to.kb1;
+        to.kb1 = before + count < to.kb1 ? before + count : to.kb1;
       }
     }
-  }
-  // this share of the blocks of k, and the steps that all shares take
-  const int steps = KS == 1 ? kb1 - kb0 : (kb1 - kb0 + KS - 1) / KS;
-  if constexpr (KS > 1) {
-    kb0 = kb0 + share * steps < kb1 ? kb0 + share * steps : kb1;
-    kb1 = kb0 + steps < kb1 ? kb0 + steps : kb1;
-  }
-  // the rows past the end repeat the last one; their results are not stored
-  const int rows = m_end - m0, columns = p.n - n0;
-  const u4 ra = buffer_words(p.a + (int64_t)m0 * p.a_pitch);
-  const u4 rb = buffer_words(b + (int64_t)n0 * p.b_pitch);
+    return true;
+  };
+  // The next tile that has something to sum, into `tile`; those that have not get zeros.
+  Tile tile;
+  uint32_t id = blockIdx.x;
+  const auto take = [&] {
+    for (; id < p.tiles; id += gridDim.x) {
+      if (!place(id, tile)) continue;
+      if (tile.kb0 < tile.kb1) {
+        id += gridDim.x;
+        return true;
+      }
+      for (int e = threadIdx.x; e < BM * BN; e += KS * kThreads) {
+        const int row = tile.m0 + e / BN, column = tile.n0 + e % BN;
+        const int64_t to = tile.out_at + (int64_t)row * p.out_pitch + column;
+        if (row < tile.m_end && column < p.n) {
+          if constexpr (FULL)
+            static_cast<float *>(p.out)[to] = 0.0f;
+          else
+            static_cast<uint16_t *>(p.out)[to] = 0;
+        }
+      }
+    }
+    return false;
+  };
+
+  // Where the loads of `tile` come from.
+  u4 ra, rb;
   int off[kTiles];
-#pragma unroll
-  for (int i = 0; i < kTiles; ++i) {
-    const int s = (i < kLoadsA ? i : i - kLoadsA) * kThreads + t, r = s >> 3;
-    const int c = (r & ~63) + tile_column<FULL>((r >> 4) & 3, r & 15);
-    const int row = i < kLoadsA ? (r < rows ? r : rows - 1) : (c < columns ? c : columns - 1);
-    off[i] = row * (int)(i < kLoadsA ? p.a_pitch : p.b_pitch) + (((s & 7) ^ ((s >> 4) & 7)) << 4);
-  }
-  // the threads past the scales bring the last one again
   const float *scale_at[kScales];
+  const auto aim = [&] {
+    // the rows past the end repeat the last one; their results are not stored
+    const int rows = tile.m_end - tile.m0, columns = p.n - tile.n0;
+    ra = buffer_words(p.a + (int64_t)tile.m0 * p.a_pitch);
+    rb = buffer_words(tile.b + (int64_t)tile.n0 * p.b_pitch);
 #pragma unroll
-  for (int i = 0; i < kScales; ++i) {
-    const int r = i * kThreads + t, last = BROWS ? p.n - 1 : (p.n - 1) / kBlock;
-    const int c = (BROWS ? n0 : n0 / kBlock) + r - BM;
-    scale_at[i] = r < BM ? p.sa + (int64_t)(m0 + (r < rows ? r : rows - 1)) * p.sa_pitch
-                         : sb + (int64_t)(c < last ? c : last) * p.sb_pitch;
-  }
-  const int tail = p.k & (kBlock - 1), kb_tail = tail != 0 ? p.k / kBlock : -1;
+    for (int i = 0; i < kTiles; ++i) {
+      const int s = (i < kLoadsA ? i : i - kLoadsA) * kThreads + t, r = s >> 3;
+      const int c = (r & ~63) + tile_column<FULL>((r >> 4) & 3, r & 15);
+      const int row = i < kLoadsA ? (r < rows ? r : rows - 1) : (c < columns ? c : columns - 1);
+      off[i] = row * (int)(i < kLoadsA ? p.a_pitch : p.b_pitch) + (((s & 7) ^ ((s >> 4) & 7)) << 4);
+    }
+    // the threads past the scales bring the last one again
+#pragma unroll
+    for (int i = 0; i < kScales; ++i) {
+      const int r = i * kThreads + t, last = BROWS ? p.n - 1 : (p.n - 1) / kBlock;
+      const int c = (BROWS ? tile.n0 : tile.n0 / kBlock) + r - BM;
+      scale_at[i] = r < BM ? p.sa + (int64_t)(tile.m0 + (r < rows ? r : rows - 1)) * p.sa_pitch
+                           : tile.sb + (int64_t)(c < last ? c : last) * p.sb_pitch;
+    }
+  };
 
   // One of a thread's kLoads loads of block kb.  In the last, partial block (TAIL) chunks
   // wholly past k may lie past the matrix: the row's first one is loaded instead.
@@ -797,11 +830,6 @@ __global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs 
   };
 
   f4 acc[TM][TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = f4{0, 0, 0, 0};
-
   const int key = (li >> 1) & 7;
   const int chunk0 = li * kBlock + ((g ^ key) << 4), chunk1 = li * kBlock + (((g + 4) ^ key) << 4);
   const auto fragment = [&](const uint8_t *tile_rows, auto is_tail) {
@@ -817,143 +845,237 @@ __global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs 
 
   using No = std::false_type;
   using Yes = std::true_type;
-  // One step: the products of block kb, in `stage`, and in between the loads of block
-  // kb + D - 1 (LOAD: 0 none, 1 a whole block, 2 the tail) into the stage that the last step
-  // has read.  Issuing them all first would hold up the wave, which takes its turn at the
+  // the stores of a tile that is whole and aligned: one of 16 bytes for each kStore results
+  constexpr int kWide = FULL ? 4 : 2, kStore = 16 / kWide, kStores = TM * TN * 4 / kStore;
+  static_assert(kStores < 64, "stores in flight that one wait can count");
+  // One step: the products of the block in `stage`, of which `ahead` more are on their way,
+  // and in between the loads of block `load_kb` (LOAD: 0 none, 1 a whole block, 2 the tail)
+  // into the stage that the last step has read.  Issuing them all first would hold up the wave, which takes its turn at the
   // address unit, 16 cycles a load; the first half of the step leaves them time to arrive.
-  const auto step = [&](int kb, int stage, auto what, auto is_tail) {
+  // `storing`: kStores stores went out after this block's loads, and need not have ended.
+  const auto step = [&](int stage, int ahead, int load_kb, auto what, auto is_tail,
+                        bool storing = false) {
     constexpr int LOAD = decltype(what)::value;
     // this block has come; the barrier also ends the last step's reads
-    wait_stages<D - 2, kLoads>(kb1 - 1 - kb);
+    if (LOOP && storing)
+      wait_stages<1, kStores>(1);
+    else
+      wait_stages<D - 2, kLoads>(ahead);
     __syncthreads();
     const uint8_t *la = ring + stage * kStageBytes + wm * (BM / WM) * kBlock;
     const uint8_t *lb = ring + stage * kStageBytes + (BM + wn * (BN / WN)) * kBlock;
     const int into = stage == 0 ? D - 1 : stage - 1;
-    // The scaling of a product waits for its MFMA, so it is done kAhead products later;
-    // the operand of the next row of products is read during this one's.  The barriers of
-    // the scheduler keep that order, which the compiler would undo.
-    constexpr int kAhead = 3;
-    f4 r[kAhead + 1];
-    Operand<FULL> fa[2], fb[TN];
-    fa[0].set(fragment(la, is_tail));
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      fb[j].set(fragment(lb + j * 16 * kBlock, is_tail));
-      __builtin_amdgcn_sched_barrier(0);
-    }
     f4 col[TN];
-    float uniform_b = 0.0f;
-    if constexpr (BROWS) {
+    float uniform_b = 0.0f, s[TM];
+    const auto load_scales = [&] {
+      if constexpr (BROWS) {
 #pragma unroll
-      for (int j = 0; j < TN; ++j)
-        col[j] = *reinterpret_cast<const f4 *>(
-            &scales[stage][BM + wn * (BN / WN) + (j & ~3) * 16 + tile_column<FULL>(j & 3, 4 * g)]);
-    } else {
-      uniform_b = scales[stage][BM + wn * (BN / WN) / kBlock];
-    }
-    float s[TM];
-#pragma unroll
-    for (int i = 0; i < TM; ++i) s[i] = scales[stage][wm * (BM / WM) + i * 16 + li];
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int c = 0; c < TM * TN + kAhead; ++c) {
-      if (c < TM * TN) {
-        const int i = c / TN, j = c % TN;
-        if (j == 0 && i + 1 < TM) fa[(i + 1) & 1].set(fragment(la + (i + 1) * 16 * kBlock, is_tail));
-        r[c % (kAhead + 1)] = Operand<FULL>::product(fb[j], fa[i & 1]);
+        for (int j = 0; j < TN; ++j)
+          col[j] = *reinterpret_cast<const f4 *>(
+              &scales[stage][BM + wn * (BN / WN) + (j & ~3) * 16 + tile_column<FULL>(j & 3, 4 * g)]);
+      } else {
+        uniform_b = scales[stage][BM + wn * (BN / WN) / kBlock];
       }
-      if (c >= kAhead) {
-        const int d = c - kAhead, i = d / TN, j = d % TN;
-        if (!BROWS && j == 0) s[i] *= uniform_b;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          acc[i][j][q] = __builtin_fmaf(r[d % (kAhead + 1)][q], BROWS ? s[i] * col[j][q] : s[i],
-                                        acc[i][j][q]);
-        // keeps the sums here: the compiler would move them past the next barrier
-        asm volatile("" : "+v"(acc[i][j]));
-      }
+      for (int i = 0; i < TM; ++i) s[i] = scales[stage][wm * (BM / WM) + i * 16 + li];
+    };
+    const auto scale = [&](int i, int j, const f4 &r) {
+      if (!BROWS && j == 0) s[i] *= uniform_b;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        acc[i][j][q] = __builtin_fmaf(r[q], BROWS ? s[i] * col[j][q] : s[i], acc[i][j][q]);
+      // keeps the sums here: the compiler would move them past the next barrier
+      asm volatile("" : "+v"(acc[i][j]));
+    };
+    // spreads the loads over the first half of TM * TN products
+    const auto load_slot = [&](int c) {
       if constexpr (LOAD != 0) {
         constexpr int kOver = TM * TN / 2;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
           if (i * kOver / kLoads == c)
-            load_piece(kb + D - 1, into, i, std::bool_constant<LOAD == 2>{});
+            load_piece(load_kb, into, i, std::bool_constant<LOAD == 2>{});
       }
+    };
+    // Scaling a product waits for its MFMA, so it is done later, between the next ones, and
+    // the operand of the next row of products is read during this one's.  The barriers of
+    // the scheduler keep that order, which the compiler would undo.
+    Operand<FULL> fa[2], fb[TN];
+    if constexpr (FULL) {
+      // a row of products at once, as TN chains of four MFMAs that do not wait for each
+      // other; the next row's codes are widened when they have come
+      i8v raw = fragment(la, is_tail);
+      i8v raw_b[TN];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) raw_b[j] = fragment(lb + j * 16 * kBlock, is_tail);
+      load_scales();
+      fa[0].set(raw);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) fb[j].set(raw_b[j]);
+      f4 r[2][TN];
       __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        if (i + 1 < TM) raw = fragment(la + (i + 1) * 16 * kBlock, is_tail);
+#pragma unroll
+        for (int part = 0; part < 4; ++part) {
+#pragma unroll
+          for (int j = 0; j < TN; ++j)
+            r[i & 1][j] = Operand<FULL>::part(part, fb[j], fa[i & 1],
+                                              part == 0 ? f4{0, 0, 0, 0} : r[i & 1][j]);
+#pragma unroll
+          for (int j = part * TN / 4; j < (part + 1) * TN / 4; ++j) {
+            if (i > 0) scale(i - 1, j, r[(i - 1) & 1][j]);
+            load_slot(i * TN + j);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (i + 1 < TM) fa[(i + 1) & 1].set(raw);
+      }
+#pragma unroll
+      for (int j = 0; j < TN; ++j) scale(TM - 1, j, r[(TM - 1) & 1][j]);
+    } else {
+      constexpr int kAhead = 3;
+      f4 r[kAhead + 1];
+      fa[0].set(fragment(la, is_tail));
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        fb[j].set(fragment(lb + j * 16 * kBlock, is_tail));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      load_scales();
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int c = 0; c < TM * TN + kAhead; ++c) {
+        if (c < TM * TN) {
+          const int i = c / TN, j = c % TN;
+          if (j == 0 && i + 1 < TM)
+            fa[(i + 1) & 1].set(fragment(la + (i + 1) * 16 * kBlock, is_tail));
+          r[c % (kAhead + 1)] = Operand<FULL>::product(fb[j], fa[i & 1]);
+        }
+        if (c >= kAhead)
+          scale((c - kAhead) / TN, (c - kAhead) % TN, r[(c - kAhead) % (kAhead + 1)]);
+        load_slot(c);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   };
 
-  if (kb0 < kb1) {
+  // Whether the tile was whole and aligned is returned.
+  const auto store = [&](const Tile &of) {
+    const bool aligned = ((reinterpret_cast<uintptr_t>(p.out) |
+                           (uintptr_t)((p.out_pitch | of.out_at) * kWide)) & 15) == 0;
 #pragma unroll
-    for (int d = 0; d < D - 1; ++d) {
-      if (kb0 + d >= kb1) continue;
+    for (int i = 0; i < TM; ++i) {
+      const int row = of.m0 + wm * (BM / WM) + i * 16 + li;
+      if (row >= of.m_end) continue;
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        if (kb0 + d == kb_tail)
-          load_piece(kb0 + d, d, i, Yes{});
+      for (int j = 0; j < TN; j += kStore / 4) {
+        const int column = of.n0 + wn * (BN / WN) + (j & ~3) * 16 + tile_column<FULL>(j & 3, 4 * g);
+        float v[kStore];
+#pragma unroll
+        for (int q = 0; q < kStore; ++q) v[q] = acc[i][j + q / 4][q % 4];
+        const int64_t to = of.out_at + (int64_t)row * p.out_pitch + column;
+        if constexpr (FULL)
+          store_row<HADACORE_FP32>(p.out, to, v, p.n - column, aligned, p.nt_out);
+        else if (p.out_type == HADACORE_FP16)
+          store_row<HADACORE_FP16>(p.out, to, v, p.n - column, aligned, p.nt_out);
         else
-          load_piece(kb0 + d, d, i, No{});
+          store_row<HADACORE_BF16>(p.out, to, v, p.n - column, aligned, p.nt_out);
       }
     }
-    const int whole = kb1 - 1 == kb_tail ? kb1 - 1 : kb1;  // end of the whole blocks
-    int kb = kb0, stage = 0;
-    const auto after = [](int s) { return s == D - 1 ? 0 : s + 1; };
-    for (; kb + D - 1 < whole; ++kb, stage = after(stage))
-      step(kb, stage, std::integral_constant<int, 1>{}, No{});
-    if (kb + D - 1 < kb1) {
-      step(kb, stage, std::integral_constant<int, 2>{}, No{});
-      ++kb;
-      stage = after(stage);
+    return aligned && of.m_end - of.m0 >= BM && p.n - of.n0 >= BN;
+  };
+  const auto clear = [&] {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = f4{0, 0, 0, 0};
+  };
+  const auto load_first = [&](int kb, int stage) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      if (kb == kb_tail)
+        load_piece(kb, stage, i, Yes{});
+      else
+        load_piece(kb, stage, i, No{});
     }
-    for (; kb < whole; ++kb, stage = after(stage))
-      step(kb, stage, std::integral_constant<int, 0>{}, No{});
-    if (kb < kb1) step(kb, stage, std::integral_constant<int, 0>{}, Yes{});
-  }
-  if constexpr (KS > 1) {
-    // the other shares' barriers, then the sums of the shares, added in their order
-    for (int i = kb1 - kb0; i < steps; ++i) __syncthreads();
-    static_assert((KS - 1) * BM * BN * 4 <= sizeof(tiles), "the sums fit the stages");
-    f4 *sums = reinterpret_cast<f4 *>(tiles);
-    __syncthreads();
-    if (share > 0) {
+  };
+  using None = std::integral_constant<int, 0>;
+  using Whole = std::integral_constant<int, 1>;
+  using Partial = std::integral_constant<int, 2>;
+  const auto after = [](int stage) { return stage == D - 1 ? 0 : stage + 1; };
+
+  if (!take()) return;
+  aim();
+  if constexpr (LOOP) {
+    // The workgroup goes through tiles: the last step of one loads the first block of the
+    // next, whose loads are under way while this one's results are stored.
+    load_first(tile.kb0, 0);
+    bool more = true, storing = false;
+    for (int stage = 0; more;) {
+      const Tile now = tile;
+      clear();
+      for (int kb = now.kb0; kb < now.kb1; ++kb, stage = after(stage)) {
+        int next = kb + 1;
+        if (next == now.kb1) {
+          more = take();
+          if (more) aim();
+          // after the last tile its last block once more, which nobody reads
+          next = more ? tile.kb0 : kb;
+        }
+        step(stage, 0, next, Whole{}, No{}, storing);
+        storing = false;
+      }
+      storing = store(now);
+    }
+    wait_stages<0, 0>(0);
+  } else {
+    // One tile to a workgroup.  This share of the blocks of k, and the steps that all take:
+    const int steps = (tile.kb1 - tile.kb0 + KS - 1) / KS;
+    const int kb0 = tile.kb0 + share * steps < tile.kb1 ? tile.kb0 + share * steps : tile.kb1;
+    const int kb1 = kb0 + steps < tile.kb1 ? kb0 + steps : tile.kb1;
+    clear();
+    if (kb0 < kb1) {
+#pragma unroll
+      for (int d = 0; d < D - 1; ++d)
+        if (kb0 + d < kb1) load_first(kb0 + d, d);
+      const int whole = kb1 - 1 == kb_tail ? kb1 - 1 : kb1;  // end of the whole blocks
+      int kb = kb0, stage = 0;
+      for (; kb + D - 1 < whole; ++kb, stage = after(stage))
+        step(stage, kb1 - 1 - kb, kb + D - 1, Whole{}, No{});
+      if (kb + D - 1 < kb1) {
+        step(stage, kb1 - 1 - kb, kb + D - 1, Partial{}, No{});
+        ++kb;
+        stage = after(stage);
+      }
+      for (; kb < whole; ++kb, stage = after(stage)) step(stage, kb1 - 1 - kb, 0, None{}, No{});
+      if (kb < kb1) step(stage, 0, 0, None{}, Yes{});
+    }
+    if constexpr (KS > 1) {
+      // the other shares' barriers, then the sums of the shares, added in their order
+      for (int i = kb1 - kb0; i < steps; ++i) __syncthreads();
+      static_assert((KS - 1) * BM * BN * 4 <= sizeof(tiles), "the sums fit the stages");
+      f4 *sums = reinterpret_cast<f4 *>(tiles);
+      __syncthreads();
+      if (share > 0) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j)
+            sums[(((share - 1) * TM + i) * TN + j) * kThreads + t] = acc[i][j];
+      }
+      __syncthreads();
+      if (share > 0) return;
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j)
-          sums[(((share - 1) * TM + i) * TN + j) * kThreads + t] = acc[i][j];
+#pragma unroll
+          for (int q = 0; q < KS - 1; ++q) acc[i][j] += sums[((q * TM + i) * TN + j) * kThreads + t];
     }
-    __syncthreads();
-    if (share > 0) return;
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-      for (int j = 0; j < TN; ++j)
-#pragma unroll
-        for (int q = 0; q < KS - 1; ++q) acc[i][j] += sums[((q * TM + i) * TN + j) * kThreads + t];
-  }
-
-  constexpr int kWide = FULL ? 4 : 2, kStore = 16 / kWide;
-  const bool aligned =
-      ((reinterpret_cast<uintptr_t>(p.out) | (uintptr_t)((p.out_pitch | out_at) * kWide)) & 15) == 0;
-#pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int row = m0 + wm * (BM / WM) + i * 16 + li;
-    if (row >= m_end) continue;
-#pragma unroll
-    for (int j = 0; j < TN; j += kStore / 4) {
-      const int column = n0 + wn * (BN / WN) + (j & ~3) * 16 + tile_column<FULL>(j & 3, 4 * g);
-      float v[kStore];
-#pragma unroll
-      for (int q = 0; q < kStore; ++q) v[q] = acc[i][j + q / 4][q % 4];
-      const int64_t to = out_at + (int64_t)row * p.out_pitch + column;
-      if constexpr (FULL)
-        store_row<HADACORE_FP32>(p.out, to, v, p.n - column, aligned);
-      else if (p.out_type == HADACORE_FP16)
-        store_row<HADACORE_FP16>(p.out, to, v, p.n - column, aligned);
-      else
-        store_row<HADACORE_BF16>(p.out, to, v, p.n - column, aligned);
-    }
+    store(tile);
   }
 }
 
@@ -1130,11 +1252,20 @@ hipError_t launch_tiles(ProductArgs p, bool b_rows, hipStream_t stream) {
   int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
   if (p.kind == kGradient) tiles *= p.groups;
   if (tiles * (KS * WM * WN * kWave) >= (int64_t(1) << 32)) return hipErrorInvalidValue;
-  const dim3 grid((uint32_t)tiles), block(KS * WM * WN * kWave);
+  p.tiles = (uint32_t)tiles;
+  // where there are more tiles than run together, and whole blocks, workgroups go through them
+  constexpr bool kMayLoop = D == 2 && KS == 1;
+  const int64_t slots = (int64_t)device_cus() * (BM * BN <= 128 * 128 ? 2 : 1);
+  const bool loop = kMayLoop && tiles > slots && p.k % kBlock == 0;
+  const dim3 grid((uint32_t)(loop ? slots : tiles)), block(KS * WM * WN * kWave);
   const auto go = [&](auto rows, auto full) {
-    hipLaunchKernelGGL((product_kernel<BM, BN, WM, WN, D, KS, decltype(rows)::value,
-                                       decltype(full)::value>),
-                       grid, block, 0, stream, p);
+    constexpr bool kRows = decltype(rows)::value, kFull = decltype(full)::value;
+    if (loop)
+      hipLaunchKernelGGL((product_kernel<BM, BN, WM, WN, D, KS, kMayLoop, kRows, kFull>), grid,
+                         block, 0, stream, p);
+    else
+      hipLaunchKernelGGL((product_kernel<BM, BN, WM, WN, D, KS, false, kRows, kFull>), grid, block,
+                         0, stream, p);
     return hipGetLastError();
   };
   if (p.out_type == HADACORE_FP32) {
@@ -1183,7 +1314,13 @@ int tile_override() {
   return -1;
 }
 
-hipError_t launch_product(const ProductArgs &p, bool b_rows, hipStream_t stream) {
+hipError_t launch_product(ProductArgs p, bool b_rows, hipStream_t stream) {
+  // Outputs of this size do not stay in the last-level cache for their reader, and push out
+  // of the L2s what other tiles still read.  With the policy SC1 | NT, us: 128 MiB of 16384
+  // x 4096 bf16 outputs 240 instead of 264 (k = 4096), 74.7 instead of 82.9 (k = 1024), 256
+  // MiB of gradients 182 instead of 200; 64 MiB by expert 193 instead of 190.
+  p.nt_out = (int64_t)p.m * p.n * (p.kind == kGradient ? p.groups : 1) *
+                 (p.out_type == HADACORE_FP32 ? 4 : 2) >= (int64_t(1) << 27);
   const int64_t groups = p.kind == kGroups ? (p.groups < p.m ? p.groups : p.m) : 1;
   int forced = tile_override();
   if (forced == 3 && p.out_type == HADACORE_FP32) forced = -1;

@@ -427,6 +427,66 @@ def test_broadcast_weights():
     R.check_product(ha, hsa, hb, hsb, _host(y), "fp32")
 
 
+# more tiles than run together, which workgroups go through one after the other
+MANY = pytest.mark.parametrize("out", OUTS)
+
+
+def _some_rows(m):
+    return np.unique(np.r_[np.arange(0, m, 9), m - 1])
+
+
+@MANY
+@pytest.mark.parametrize("tall", [128, 1])
+@pytest.mark.parametrize("m,n,k", [(4300, 4400, 128), (2200, 4168, 384), (4097, 4352, 200)])
+def test_matmul_many_tiles(m, n, k, tall, out, variant):
+    import torch
+    rng = np.random.default_rng(m + k)
+    a, sa, ha, hsa = _codes(rng, m, k)
+    b, sb, hb, hsb = _codes(rng, n, k, scale_rows=-(-n // tall), spread=0.05 / k ** 0.5)
+    y = H.matmul_fp8(a, sa, b, sb, dtype=_torch_type(out))
+    rows = _some_rows(m)
+    R.check_product(ha[rows], hsa[rows], hb, hsb, _host(y[torch.from_numpy(rows).cuda()]), out, tall)
+
+
+@MANY
+def test_grouped_many_tiles(out, variant):
+    import torch
+    n, k, ends = 4400, 256, [0, 700, 700, 701, 1900, 1900, 2300, 3300, 3301]
+    tokens, groups = 3500, len(ends)
+    rng = np.random.default_rng(5)
+    a, sa, ha, hsa = _codes(rng, tokens, k)
+    b, sb, hb, hsb = _codes(rng, groups * n, k, scale_rows=groups * 35, spread=0.01)
+    y = H.grouped_matmul_fp8(a, sa, b.view(groups, n, k), sb.view(groups, 35, 2), _ends(ends),
+                             dtype=_torch_type(out))
+    hb, hsb, low = hb.reshape(groups, n, k), hsb.reshape(groups, 35, 2), 0
+    for g, high in enumerate(ends):
+        rows = low + _some_rows(high - low) if high > low else []
+        if len(rows):
+            R.check_product(ha[rows], hsa[rows], hb[g], hsb[g],
+                            _host(y[torch.from_numpy(rows).cuda()]), out, 128, f"group {g}")
+        low = high
+    assert (y[low:] == 0).all()
+
+
+@MANY
+def test_weight_gradient_many_tiles(out, variant):
+    import torch
+    n, k, ends = 1300, 1544, [0, 100, 100, 430, 431, 700, 700, 900, 1000]
+    rng = np.random.default_rng(6)
+    groups, places = R.padded_places(ends, 1000)
+    d, sd, hd, hsd = _codes(rng, n, places, spread=0.3)
+    x, sx, hx, hsx = _codes(rng, k, places, spread=0.01)
+    g = _host(H.grouped_weight_gradient_fp8(d, sd, x, sx, _ends(ends), dtype=_torch_type(out)))
+    rows = _some_rows(n)
+    for e, low, count, at, blocks in groups:
+        if count == 0:
+            assert (g[e] == 0).all()
+            continue
+        cut, cuts = slice(at, at + blocks * 128), slice(at // 128, at // 128 + blocks)
+        R.check_product(hd[rows, cut], hsd[rows, cuts], hx[:, cut], hsx[:, cuts], g[e][rows], out, 1,
+                        f"group {e}")
+
+
 # ---- offsets beyond 32 bits ----------------------------------------------------------
 
 
