@@ -98,6 +98,23 @@ __device__ __forceinline__ Piece find_piece(const int32_t *ends, int groups, int
   return {-1, 0, 0};
 }
 
+// How many pieces there are.
+__device__ __forceinline__ int count_pieces(const int32_t *ends, int groups, int rows, int unit,
+                                            bool rest) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int count = 0, start = 0;
+  const int all = groups + (rest ? 1 : 0);
+  for (int g0 = 0; g0 < all; g0 += kWave) {
+    const int g = g0 + lane;
+    const int high = g < groups ? clamp_end(ends[g], rows) : rows;
+    const int low = __builtin_amdgcn_update_dpp(start, high, 0x138, 0xF, 0xF, false);
+    const int pieces = g < all && high > low ? (high - low + unit - 1) / unit : 0;
+    count += __builtin_amdgcn_readlane(prefix_sum(pieces), kWave - 1);
+    start = __builtin_amdgcn_readlane(high, kWave - 1);
+  }
+  return count;
+}
+
 // The blocks of 128 rows before group `group`, and in it, with every group padded to whole
 // blocks.  Called by whole waves.
 __device__ __forceinline__ void group_blocks(const int32_t *ends, int groups, int rows, int group,
@@ -678,10 +695,10 @@ __device__ __forceinline__ TileAt tile_at(uint32_t id, uint32_t total, int tiles
   return {matrix, band * kBand + in_band % high, in_band / high};
 }
 
-// Which of 64 columns row i of the j-th of four MFMAs is (a lane holds rows 4 g .. 4 g + 3).
+// Which of 32 columns row i of the j-th of two MFMAs is (a lane holds rows 4 g .. 4 g + 3).
 template <bool FULL>
 __device__ __forceinline__ int tile_column(int j, int i) {
-  return FULL ? 16 * j + i : 32 * (j >> 1) + 8 * (i >> 2) + 4 * (j & 1) + (i & 3);
+  return FULL ? 16 * j + i : 8 * (i >> 2) + 4 * j + (i & 3);
 }
 
 // The whole tiles' kernel: BM x BN outputs by WM x WN waves, in steps of a block of k.
@@ -700,75 +717,97 @@ __device__ __forceinline__ int tile_column(int j, int i) {
 //
 // LDS rows are 128 bytes; chunk c of row r lies at c ^ ((r >> 1) & 7), which the loads
 // obey by choosing their global chunk, since LDS addresses of a load run with the lane.
+// A tile's rows and columns, where its outputs start, and its blocks of k.
+struct Tile {
+  int m0, n0, m_end, kb0, kb1;
+  int64_t out_at;
+  const uint8_t *b;
+  const float *sb;
+};
+
+// The tiles of a workgroup: first + blockIdx.x, + gridDim.x, ... below `end`, of `total`
+// tiles of bm x bn; or, with `parts`, the quarters of the tiles from `first` on, the first
+// quarters of all before the second ones.
+struct Tiles {
+  int bm, bn, tiles_m;
+  uint32_t total, first, end, parts, id;
+
+  __device__ __forceinline__ bool next(const ProductArgs &p, Tile &to) {
+    for (; id < end; id += gridDim.x) {
+      const uint32_t part = parts ? id / parts : 0;
+      const TileAt at = tile_at(first + (parts ? id % parts : id), total, tiles_m, p.tiles_n);
+      to = {at.m * bm, at.n * bn, p.m, 0, (p.k + kBlock - 1) / kBlock, 0, p.b, p.sb};
+      if (p.kind == kGroups) {
+        const Piece piece = find_piece(p.ends, p.groups, p.m, bm, at.m, true);
+        to.m0 = piece.low;
+        to.m_end = piece.high;
+        if (piece.group < 0 || to.m0 < 0) continue;
+        if (piece.group == p.groups) {
+          to.kb1 = 0;  // rows after the last group: zeros
+        } else {
+          to.b += piece.group * p.b_batch;
+          to.sb += piece.group * p.sb_batch;
+        }
+      } else if (p.kind == kGradient) {
+        to.out_at = at.matrix * p.out_batch;
+        if (p.ends != nullptr) {
+          int before, count;
+          group_blocks(p.ends, p.groups, p.k, at.matrix, before, count);
+          to.kb0 = before < to.kb1 ? before : to.kb1;
+          to.kb1 = before + count < to.kb1 ? before + count : to.kb1;
+        }
+      }
+      to.m0 += (int)(part >> 1) * (bm / 2);
+      to.n0 += (int)(part & 1) * (bn / 2);
+      if (to.m0 >= to.m_end || to.n0 >= p.n) continue;
+      id += gridDim.x;
+      return true;
+    }
+    return false;
+  }
+};
+
+template <int BM, int BN, int WM, int WN, int D, int KS, bool BROWS>
+struct Shape {
+  static constexpr int kThreads = WM * WN * kWave;  // of one share of k
+  // scales of A's rows, then of B's columns or blocks of columns
+  static constexpr int SB = BROWS ? BN : BN / kBlock > 0 ? BN / kBlock : 1;
+  static constexpr int kScales = (BM + SB + kThreads - 1) / kThreads;
+  static constexpr int kStageBytes = (BM + BN) * kBlock;
+  static constexpr int kTileBytes = KS * D * kStageBytes, kScaleFloats = KS * D * kScales * kThreads;
+};
+
+// Sums the tiles of `which`, through `tiles` and `scale_memory` of LDS.
 template <int BM, int BN, int WM, int WN, int D, int KS, bool LOOP, bool BROWS, bool FULL>
-__global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs p) {
-  constexpr int kThreads = WM * WN * kWave;  // of one share of k
+__device__ __forceinline__ void sum_tiles(const ProductArgs &p, uint8_t *tiles, float *scale_memory,
+                                          Tiles which) {
+  using S = Shape<BM, BN, WM, WN, D, KS, BROWS>;
+  constexpr int kThreads = S::kThreads, kScales = S::kScales;
   constexpr int TM = BM / WM / 16, TN = BN / WN / 16;  // MFMA tiles of a wave
-  static_assert(TN % 4 == 0 && kBlock % (BN / WN) == 0, "a wave's columns are in one block of B");
+  static_assert(TN % 2 == 0 && kBlock % (BN / WN) == 0, "a wave's columns are in one block of B");
   constexpr int kLoadsA = BM * 8 / kThreads, kLoadsB = BN * 8 / kThreads;
   constexpr int kTiles = kLoadsA + kLoadsB;  // loads of 16 bytes a thread
-  // scales of A's rows, then of B's columns or blocks of columns
-  constexpr int SB = BROWS ? BN : BN / kBlock > 0 ? BN / kBlock : 1;
-  constexpr int kScales = (BM + SB + kThreads - 1) / kThreads;
   constexpr int kLoads = kTiles + kScales;
   static_assert(kLoads * (D - 2) < 64, "loads in flight that one wait can count");
-  constexpr int kStageBytes = (BM + BN) * kBlock;
+  constexpr int kStageBytes = S::kStageBytes;
   static_assert(!LOOP || (D == 2 && KS == 1), "a loop over tiles loads one block ahead");
-  __shared__ __align__(16) uint8_t tiles[KS * D * kStageBytes];
-  __shared__ __align__(16) float scales_of[KS][D][kScales * kThreads];
 
   const int share = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
   const int t = threadIdx.x - share * kThreads, lane = t & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(t / kWave);
   const int wm = wave / WN, wn = wave % WN;
   uint8_t *const ring = tiles + share * D * kStageBytes;
-  float (*const scales)[kScales * kThreads] = scales_of[share];
+  float (*const scales)[kScales * kThreads] =
+      reinterpret_cast<float (*)[kScales * kThreads]>(scale_memory + share * D * kScales * kThreads);
   const int g = lane >> 4, li = lane & 15;
 
   const int tail = p.k & (kBlock - 1), kb_tail = tail != 0 ? p.k / kBlock : -1;
 
-  // Tile `id`: its rows and columns, where its outputs start, and its blocks of k.
-  struct Tile {
-    int m0, n0, m_end, kb0, kb1;
-    int64_t out_at;
-    const uint8_t *b;
-    const float *sb;
-  };
-  const auto place = [&](uint32_t id, Tile &to) {
-    const TileAt at = tile_at(id, p.tiles, p.tiles_m, p.tiles_n);
-    to = {at.m * BM, at.n * BN, p.m, 0, (p.k + kBlock - 1) / kBlock, 0, p.b, p.sb};
-    if (p.kind == kGroups) {
-      const Piece piece = find_piece(p.ends, p.groups, p.m, BM, at.m, true);
-      to.m0 = piece.low;
-      to.m_end = piece.high;
-      if (piece.group < 0 || to.m0 < 0 || to.m0 >= to.m_end) return false;
-      if (piece.group == p.groups) {
-        to.kb1 = 0;  // rows after the last group: zeros
-      } else {
-        to.b += piece.group * p.b_batch;
-        to.sb += piece.group * p.sb_batch;
-      }
-    } else if (p.kind == kGradient) {
-      to.out_at = at.matrix * p.out_batch;
-      if (p.ends != nullptr) {
-        int before, count;
-        group_blocks(p.ends, p.groups, p.k, at.matrix, before, count);
-        to.kb0 = before < to.kb1 ? before : to.kb1;
-        to.kb1 = before + count < to.kb1 ? before + count : to.kb1;
-      }
-    }
-    return true;
-  };
   // The next tile that has something to sum, into `tile`; those that have not get zeros.
   Tile tile;
-  uint32_t id = blockIdx.x;
   const auto take = [&] {
-    for (; id < p.tiles; id += gridDim.x) {
-      if (!place(id, tile)) continue;
-      if (tile.kb0 < tile.kb1) {
-        id += gridDim.x;
-        return true;
-      }
+    while (which.next(p, tile)) {
+      if (tile.kb0 < tile.kb1) return true;
       for (int e = threadIdx.x; e < BM * BN; e += KS * kThreads) {
         const int row = tile.m0 + e / BN, column = tile.n0 + e % BN;
         const int64_t to = tile.out_at + (int64_t)row * p.out_pitch + column;
@@ -795,7 +834,7 @@ __global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs 
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
       const int s = (i < kLoadsA ? i : i - kLoadsA) * kThreads + t, r = s >> 3;
-      const int c = (r & ~63) + tile_column<FULL>((r >> 4) & 3, r & 15);
+      const int c = (r & ~31) + tile_column<FULL>((r >> 4) & 1, r & 15);
       const int row = i < kLoadsA ? (r < rows ? r : rows - 1) : (c < columns ? c : columns - 1);
       off[i] = row * (int)(i < kLoadsA ? p.a_pitch : p.b_pitch) + (((s & 7) ^ ((s >> 4) & 7)) << 4);
     }
@@ -872,7 +911,7 @@ __global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs 
 #pragma unroll
         for (int j = 0; j < TN; ++j)
           col[j] = *reinterpret_cast<const f4 *>(
-              &scales[stage][BM + wn * (BN / WN) + (j & ~3) * 16 + tile_column<FULL>(j & 3, 4 * g)]);
+              &scales[stage][BM + wn * (BN / WN) + (j & ~1) * 16 + tile_column<FULL>(j & 1, 4 * g)]);
       } else {
         uniform_b = scales[stage][BM + wn * (BN / WN) / kBlock];
       }
@@ -972,7 +1011,7 @@ __global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs 
       if (row >= of.m_end) continue;
 #pragma unroll
       for (int j = 0; j < TN; j += kStore / 4) {
-        const int column = of.n0 + wn * (BN / WN) + (j & ~3) * 16 + tile_column<FULL>(j & 3, 4 * g);
+        const int column = of.n0 + wn * (BN / WN) + (j & ~1) * 16 + tile_column<FULL>(j & 1, 4 * g);
         float v[kStore];
 #pragma unroll
         for (int q = 0; q < kStore; ++q) v[q] = acc[i][j + q / 4][q % 4];
@@ -1056,7 +1095,7 @@ __global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs 
     if constexpr (KS > 1) {
       // the other shares' barriers, then the sums of the shares, added in their order
       for (int i = kb1 - kb0; i < steps; ++i) __syncthreads();
-      static_assert((KS - 1) * BM * BN * 4 <= sizeof(tiles), "the sums fit the stages");
+      static_assert((KS - 1) * BM * BN * 4 <= S::kTileBytes, "the sums fit the stages");
       f4 *sums = reinterpret_cast<f4 *>(tiles);
       __syncthreads();
       if (share > 0) {
@@ -1076,6 +1115,40 @@ __global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs 
           for (int q = 0; q < KS - 1; ++q) acc[i][j] += sums[((q * TM + i) * TN + j) * kThreads + t];
     }
     store(tile);
+  }
+}
+
+// One tile to a workgroup, or (LOOP) as many workgroups as run together, each going through
+// tiles.  SPLIT: the tiles of the last turn, if they would leave half of the workgroups or
+// more without one, are cut into quarters: a turn of quarters with k = 4096 takes 21 us
+// where one of whole tiles takes 60 (16384 tokens over 16 experts: 181 us instead of 191).
+template <int BM, int BN, int WM, int WN, int D, int KS, bool LOOP, bool SPLIT, bool BROWS, bool FULL>
+__global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs p) {
+  using S = Shape<BM, BN, WM, WN, D, KS, BROWS>;
+  // quarters have twice the stages in the same LDS
+  using Q = Shape<BM / 2, BN / 2, WM, WN, 2 * D, KS, BROWS>;
+  static_assert(!SPLIT || Q::kTileBytes <= S::kTileBytes, "quarters fit");
+  __shared__ __align__(16) uint8_t tiles[S::kTileBytes];
+  __shared__ __align__(16) float scales[SPLIT ? Q::kScaleFloats : S::kScaleFloats];
+  Tiles which{BM, BN, p.tiles_m, p.tiles, 0, p.tiles, 0, blockIdx.x};
+  if constexpr (LOOP && SPLIT) {
+    if (p.kind == kGroups) {
+      // ragged groups: the tiles that there are, not those that there may be
+      which.tiles_m = count_pieces(p.ends, p.groups, p.m, BM, true);
+      which.total = (uint32_t)which.tiles_m * (uint32_t)p.tiles_n;
+    }
+    const uint32_t rest = which.total % gridDim.x;
+    const bool split = rest <= gridDim.x / 2;
+    which.end = split ? which.total - rest : which.total;
+    sum_tiles<BM, BN, WM, WN, D, KS, LOOP, BROWS, FULL>(p, tiles, scales, which);
+    if (!split) return;
+    for (uint32_t id = blockIdx.x; id < 4 * rest; id += gridDim.x) {
+      __syncthreads();
+      sum_tiles<BM / 2, BN / 2, WM, WN, 2 * D, KS, false, BROWS, FULL>(
+          p, tiles, scales, Tiles{BM, BN, which.tiles_m, which.total, which.end, id + 1, rest, id});
+    }
+  } else {
+    sum_tiles<BM, BN, WM, WN, D, KS, LOOP, BROWS, FULL>(p, tiles, scales, which);
   }
 }
 
@@ -1254,17 +1327,17 @@ hipError_t launch_tiles(ProductArgs p, bool b_rows, hipStream_t stream) {
   if (tiles * (KS * WM * WN * kWave) >= (int64_t(1) << 32)) return hipErrorInvalidValue;
   p.tiles = (uint32_t)tiles;
   // where there are more tiles than run together, and whole blocks, workgroups go through them
-  constexpr bool kMayLoop = D == 2 && KS == 1;
+  constexpr bool kMayLoop = D == 2 && KS == 1, kSplit = kMayLoop && BM == 256;
   const int64_t slots = (int64_t)device_cus() * (BM * BN <= 128 * 128 ? 2 : 1);
-  const bool loop = kMayLoop && tiles > slots && p.k % kBlock == 0;
+  const bool loop = kMayLoop && p.k % kBlock == 0 && (kSplit || tiles > slots);
   const dim3 grid((uint32_t)(loop ? slots : tiles)), block(KS * WM * WN * kWave);
   const auto go = [&](auto rows, auto full) {
     constexpr bool kRows = decltype(rows)::value, kFull = decltype(full)::value;
     if (loop)
-      hipLaunchKernelGGL((product_kernel<BM, BN, WM, WN, D, KS, kMayLoop, kRows, kFull>), grid,
+      hipLaunchKernelGGL((product_kernel<BM, BN, WM, WN, D, KS, kMayLoop, kSplit, kRows, kFull>), grid,
                          block, 0, stream, p);
     else
-      hipLaunchKernelGGL((product_kernel<BM, BN, WM, WN, D, KS, false, kRows, kFull>), grid, block,
+      hipLaunchKernelGGL((product_kernel<BM, BN, WM, WN, D, KS, false, false, kRows, kFull>), grid, block,
                          0, stream, p);
     return hipGetLastError();
   };
@@ -1346,7 +1419,13 @@ hipError_t launch_product(ProductArgs p, bool b_rows, hipStream_t stream) {
     const float pieces =
         p.kind == kGroups ? (float)p.m / c.bm + 0.5f * groups : ceilf((float)p.m / c.bm);
     const float tiles = pieces * ceilf((float)p.n / c.bn) * (p.kind == kGradient ? p.groups : 1);
-    const float time = ceilf(tiles / c.slots) * (tiles <= 256 ? c.alone : c.full);
+    float time = ceilf(tiles / c.slots) * (tiles <= 256 ? c.alone : c.full);
+    if (i == 3 && p.k % kBlock == 0) {
+      // the last turn in quarters: 128 x 128 by all eight waves, 0.66 us of a step
+      const float rest = fmodf(tiles, c.slots);
+      if (rest <= c.slots / 2)
+        time = floorf(tiles / c.slots) * c.full + ceilf(4 * rest / c.slots) * 0.66f;
+    }
     if (i == 0 || time < least) {
       best = i;
       least = time;
