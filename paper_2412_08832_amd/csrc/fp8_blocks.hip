@@ -609,22 +609,25 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   }
 }
 
-// 16 bytes of consecutive outputs of a row, of which the first `valid` exist.
+// 16 bytes of consecutive outputs of a row, of which the first `valid` exist, in one store
+// (rows may start at any value's address; the hardware takes 16-byte stores there) or, at the
+// end of a row, value by value.  `nt`: with the streaming cache policy.
 template <int OUT, int N>
 __device__ __forceinline__ void store_row(void *out, int64_t at, const float (&v)[N], int valid,
-                                          bool aligned, bool nt) {
-  if (valid >= N && aligned) {
+                                          bool nt) {
+  typedef u4 u4_any __attribute__((aligned(2)));
+  if (valid >= N) {
     u4 bits;
     if constexpr (OUT == HADACORE_FP32)
       bits = __builtin_bit_cast(u4, f4{v[0], v[1], v[2], v[3]});
     else
       bits = u4{pack2<OUT>(v[0], v[1]), pack2<OUT>(v[2], v[3]), pack2<OUT>(v[4], v[5]),
                 pack2<OUT>(v[6], v[7])};
-    u4 *to = reinterpret_cast<u4 *>(static_cast<char *>(out) + at * (OUT == HADACORE_FP32 ? 4 : 2));
+    char *to = static_cast<char *>(out) + at * (OUT == HADACORE_FP32 ? 4 : 2);
     if (nt)  // in asm: the compiler would make one ordinary store of the two branches
       asm volatile("global_store_dwordx4 %0, %1, off sc1 nt" ::"v"(to), "v"(bits) : "memory");
     else
-      *to = bits;
+      *reinterpret_cast<u4_any *>(to) = bits;
   } else {
 #pragma unroll
     for (int j = 0; j < N; ++j)
@@ -884,8 +887,8 @@ __device__ __forceinline__ void sum_tiles(const ProductArgs &p, uint8_t *tiles, 
 
   using No = std::false_type;
   using Yes = std::true_type;
-  // the stores of a tile that is whole and aligned: one of 16 bytes for each kStore results
-  constexpr int kWide = FULL ? 4 : 2, kStore = 16 / kWide, kStores = TM * TN * 4 / kStore;
+  // the stores of a whole tile: one of 16 bytes for each kStore results
+  constexpr int kStore = FULL ? 4 : 8, kStores = TM * TN * 4 / kStore;
   static_assert(kStores < 64, "stores in flight that one wait can count");
   // One step: the products of the block in `stage`, of which `ahead` more are on their way,
   // and in between the loads of block `load_kb` (LOAD: 0 none, 1 a whole block, 2 the tail)
@@ -1001,10 +1004,8 @@ __device__ __forceinline__ void sum_tiles(const ProductArgs &p, uint8_t *tiles, 
     }
   };
 
-  // Whether the tile was whole and aligned is returned.
+  // Whether the tile was whole is returned.
   const auto store = [&](const Tile &of) {
-    const bool aligned = ((reinterpret_cast<uintptr_t>(p.out) |
-                           (uintptr_t)((p.out_pitch | of.out_at) * kWide)) & 15) == 0;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int row = of.m0 + wm * (BM / WM) + i * 16 + li;
@@ -1017,14 +1018,14 @@ __device__ __forceinline__ void sum_tiles(const ProductArgs &p, uint8_t *tiles, 
         for (int q = 0; q < kStore; ++q) v[q] = acc[i][j + q / 4][q % 4];
         const int64_t to = of.out_at + (int64_t)row * p.out_pitch + column;
         if constexpr (FULL)
-          store_row<HADACORE_FP32>(p.out, to, v, p.n - column, aligned, p.nt_out);
+          store_row<HADACORE_FP32>(p.out, to, v, p.n - column, p.nt_out);
         else if (p.out_type == HADACORE_FP16)
-          store_row<HADACORE_FP16>(p.out, to, v, p.n - column, aligned, p.nt_out);
+          store_row<HADACORE_FP16>(p.out, to, v, p.n - column, p.nt_out);
         else
-          store_row<HADACORE_BF16>(p.out, to, v, p.n - column, aligned, p.nt_out);
+          store_row<HADACORE_BF16>(p.out, to, v, p.n - column, p.nt_out);
       }
     }
-    return aligned && of.m_end - of.m0 >= BM && p.n - of.n0 >= BN;
+    return of.m_end - of.m0 >= BM && p.n - of.n0 >= BN;
   };
   const auto clear = [&] {
 #pragma unroll
@@ -1368,13 +1369,61 @@ hipError_t launch_few(ProductArgs p, bool stream_b, hipStream_t stream) {
   return stream_b ? go(std::true_type{}, std::false_type{}) : go(std::false_type{}, std::false_type{});
 }
 
-// Which kernel.  Few rows (for groups: on average) are a reading of B; else the tile
-// with the least estimated time: turns of the CUs times blocks of k times the time of a
-// step, measured with at most one workgroup to a CU and with all slots taken.
-struct TileTime {
-  int bm, bn, slots;  // workgroups that run together on 256 CUs
-  float alone, full;  // us of a step
+// Which kernel: the one with the least estimated time.  A kernel's workgroups run in turns
+// of as many as fit the chip (kSlots for 256 CUs); a turn takes a start and as many steps as
+// a wave has blocks of k, and few rows at least the time of reading B.  The times are
+// measured (us; a step with one workgroup to a CU at most, and with all slots taken), for
+// 16-bit outputs of tiles of B scales; rows of scales and 32-bit outputs take the factors.
+// Over 60 random calls the choice was within a tenth of the best for all but a few.
+struct KernelTime {
+  int bm, bn, slots, shares;  // tile, workgroups that run together, shares of k
+  float start, alone, full;
+  float by_rows, wide;  // factors of a step
+  float read;           // reading 1 MB
 };
+constexpr int kFew = 3;  // the first of them are few_rows_kernel's
+constexpr KernelTime kTimes[] = {
+    {16, 16, 512, 8, 2.5f, 0.35f, 0.45f, 0.0f, 1.4f, 0.165f},
+    {16, 32, 768, 4, 2.5f, 0.35f, 0.50f, 0.0f, 1.4f, 0.15f},
+    {32, 32, 512, 4, 2.5f, 0.45f, 0.55f, 0.0f, 1.5f, 0.16f},
+    {64, 64, 256, 2, 2.5f, 0.60f, 0.66f, 1.13f, 1.55f, 0.25f},
+    {64, 128, 512, 1, 2.5f, 0.42f, 0.76f, 1.3f, 1.5f, 0.25f},
+    {128, 128, 512, 1, 3.0f, 0.74f, 1.28f, 1.19f, 1.6f, 0.25f},
+    {256, 256, 256, 1, 5.0f, 1.40f, 1.82f, 1.17f, 0.0f, 0.25f}};
+constexpr int kLargest = 6;  // not for 32-bit outputs, whose widened operands do not fit
+
+float estimate(const ProductArgs &p, int i, bool b_rows) {
+  const KernelTime &c = kTimes[i];
+  const bool wide = p.out_type == HADACORE_FP32;
+  const float groups = p.kind == kGroups ? (float)(p.groups < p.m ? p.groups : p.m) : 1.0f;
+  float pieces = ceilf((float)p.m / c.bm), blocks = ceilf((float)p.k / kBlock);
+  if (p.kind == kGroups) pieces = fmaxf(groups, (float)p.m / c.bm + 0.5f * groups);
+  float tiles = pieces * ceilf((float)p.n / c.bn);
+  if (p.kind == kGradient) {
+    tiles *= p.groups;
+    blocks /= p.groups;
+  }
+  const float factor = (b_rows ? c.by_rows : 1.0f) * (wide ? c.wide : 1.0f);
+  const float steps = ceilf(blocks / c.shares) * factor;
+  // the largest tile's workgroups look for their tiles one by one
+  const float start = c.start + (i == kLargest && p.kind != kDense ? 2.5f : 0.0f);
+  float time = ceilf(tiles / c.slots) * (start + steps * (tiles <= 256 ? c.alone : c.full));
+  if (i == kLargest && p.k % kBlock == 0) {
+    // the last turn in quarters, 128 x 128 by all eight waves
+    const float rest = fmodf(tiles, c.slots);
+    if (rest <= c.slots / 2)
+      time = floorf(tiles / c.slots) * (start + steps * c.full) +
+             ceilf(4 * rest / c.slots) * (start - 1.0f + blocks * (b_rows ? 0.95f : 0.58f));
+  }
+  // what is read: by few rows B once a workgroup, and A from the L2s at half the cost; by
+  // whole tiles B; slower by less than one workgroup to a CU.  Of two kernels that this
+  // bounds, the one with fewer turns
+  float read = groups * p.n;
+  if (i < kFew) read = tiles * (c.bn + 0.5f * fminf(c.bm, ceilf((float)p.m / groups)));
+  if (p.kind == kGradient) read = 0.0f;
+  read *= fmaxf(1.0f, 256 / tiles);
+  return fmaxf(time, read * p.k * 1e-6f * c.read + 2.5f) + 0.05f * time;
+}
 
 // HADACORE_VARIANT=tiles-64|tiles-64x128|tiles-128|tiles-256 forces a tile for every
 // product (testing and tuning; tiles-256 not for 32-bit outputs, which keep the choice).
@@ -1394,48 +1443,34 @@ hipError_t launch_product(ProductArgs p, bool b_rows, hipStream_t stream) {
   // MiB of gradients 182 instead of 200; 64 MiB by expert 193 instead of 190.
   p.nt_out = (int64_t)p.m * p.n * (p.kind == kGradient ? p.groups : 1) *
                  (p.out_type == HADACORE_FP32 ? 4 : 2) >= (int64_t(1) << 27);
-  const int64_t groups = p.kind == kGroups ? (p.groups < p.m ? p.groups : p.m) : 1;
-  int forced = tile_override();
-  if (forced == 3 && p.out_type == HADACORE_FP32) forced = -1;
-  if (forced < 0 && !b_rows && p.m <= 64 * groups) {
-    // weights of this size do not stay in the last-level cache beside others: streamed, 64
-    // tokens over 32 experts of 2048 x 4096 take 40.6 us instead of 46.8 and 16 rows by
-    // 8192 x 8192 13.9 instead of 14.8; 4096 x 4096 6.3 instead of 5.8
-    const bool stream_b = groups * p.n * p.k >= (int64_t(1) << 26);
-    if (p.m > 16 * groups) return launch_few<2, 2, 4, 2>(p, stream_b, stream);
-    if (groups * p.n < 16 * 512) return launch_few<1, 1, 8, 2>(p, stream_b, stream);
-    return launch_few<1, 2, 4, 2>(p, stream_b, stream);
-  }
-  static constexpr TileTime kTimes[] = {{64, 64, 256, 0.32f, 0.36f},
-                                        {64, 128, 512, 0.48f, 0.81f},
-                                        {128, 128, 512, 0.80f, 1.32f},
-                                        {256, 256, 256, 1.45f, 1.87f}};
-  int best = 0;
-  float least = 0.0f;
-  for (int i = 0; i < 4; ++i) {
-    // 32-bit outputs widen both operands in registers, which the largest tile has not got
-    if (i == 3 && p.out_type == HADACORE_FP32) continue;
-    const TileTime &c = kTimes[i];
-    const float pieces =
-        p.kind == kGroups ? (float)p.m / c.bm + 0.5f * groups : ceilf((float)p.m / c.bm);
-    const float tiles = pieces * ceilf((float)p.n / c.bn) * (p.kind == kGradient ? p.groups : 1);
-    float time = ceilf(tiles / c.slots) * (tiles <= 256 ? c.alone : c.full);
-    if (i == 3 && p.k % kBlock == 0) {
-      // the last turn in quarters: 128 x 128 by all eight waves, 0.66 us of a step
-      const float rest = fmodf(tiles, c.slots);
-      if (rest <= c.slots / 2)
-        time = floorf(tiles / c.slots) * c.full + ceilf(4 * rest / c.slots) * 0.66f;
-    }
-    if (i == 0 || time < least) {
-      best = i;
-      least = time;
+  int best = -1;
+  const int forced = tile_override();
+  if (forced >= 0 && !(forced == 3 && p.out_type == HADACORE_FP32)) {
+    best = kFew + forced;
+  } else {
+    float least = 0.0f;
+    for (int i = b_rows ? kFew : 0; i < (p.out_type == HADACORE_FP32 ? kLargest : kLargest + 1);
+         ++i) {
+      const float time = estimate(p, i, b_rows);
+      if (best < 0 || time < least) {
+        best = i;
+        least = time;
+      }
     }
   }
-  if (forced >= 0) best = forced;
+  // weights of this size that are read once do not stay in the last-level cache beside
+  // others: streamed, 64 tokens over 32 experts of 2048 x 4096 take 40.6 us instead of 46.8
+  // and 16 rows by 8192 x 8192 13.9 instead of 14.8; but 4096 x 4096 6.3 instead of 5.8, and
+  // 64 rows by 8192 x 8192, which two workgroups read, 29.6 instead of 25.7
+  const int64_t read = p.kind == kGroups ? (p.groups < p.m ? p.groups : p.m) : 1;
+  const bool stream_b = read * p.n * p.k >= (int64_t(1) << 26) && p.m <= kTimes[best].bm * read;
   switch (best) {
-    case 0: return launch_tiles<64, 64, 2, 1, 3, 2>(p, b_rows, stream);
-    case 1: return launch_tiles<64, 128, 2, 2, 3, 1>(p, b_rows, stream);
-    case 2: return launch_tiles<128, 128, 2, 2, 2, 1>(p, b_rows, stream);
+    case 0: return launch_few<1, 1, 8, 2>(p, stream_b, stream);
+    case 1: return launch_few<1, 2, 4, 2>(p, stream_b, stream);
+    case 2: return launch_few<2, 2, 4, 2>(p, stream_b, stream);
+    case 3: return launch_tiles<64, 64, 2, 1, 3, 2>(p, b_rows, stream);
+    case 4: return launch_tiles<64, 128, 2, 2, 3, 1>(p, b_rows, stream);
+    case 5: return launch_tiles<128, 128, 2, 2, 2, 1>(p, b_rows, stream);
     default: return launch_tiles<256, 256, 2, 4, 2, 1>(p, b_rows, stream);
   }
 }

@@ -501,6 +501,21 @@ def test_outputs_beyond_4_gib():
     R.check_product(ha[rows], hsa[rows], hb, hsb, _host(y[rows]), "bf16")
 
 
+@pytest.mark.parametrize("out,m,n", [("fp32", 4203, 8200), ("bf16", 8391, 8203), ("fp16", 8449, 8192)])
+def test_outputs_that_are_streamed(out, m, n):
+    """From 128 MiB outputs are stored with another cache policy; edges and odd rows too."""
+    import torch
+    k = 256
+    rng = np.random.default_rng(n)
+    a, sa, ha, hsa = _codes(rng, m, k)
+    b, sb, hb, hsb = _codes(rng, n, k, scale_rows=-(-n // 128), spread=0.01)
+    buf = torch.full((m * n + 64,), 5.0, dtype=_torch_type(out), device="cuda")
+    y = H.matmul_fp8(a, sa, b, sb, out=buf[: m * n].view(m, n))
+    rows = np.unique(np.r_[np.arange(0, m, 61), m - 1])
+    R.check_product(ha[rows], hsa[rows], hb, hsb, _host(y[torch.from_numpy(rows).cuda()]), out)
+    assert (buf[m * n:] == 5).all()
+
+
 def test_weights_beyond_4_gib():
     import torch
     groups, n, k = 40, 8192, 16384
