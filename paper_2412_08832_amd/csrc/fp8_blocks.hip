@@ -624,8 +624,12 @@ __device__ __forceinline__ void store_row(void *out, int64_t at, const float (&v
       bits = u4{pack2<OUT>(v[0], v[1]), pack2<OUT>(v[2], v[3]), pack2<OUT>(v[4], v[5]),
                 pack2<OUT>(v[6], v[7])};
     char *to = static_cast<char *>(out) + at * (OUT == HADACORE_FP32 ? 4 : 2);
-    if (nt)  // in asm: the compiler would make one ordinary store of the two branches
-      asm volatile("global_store_dwordx4 %0, %1, off sc1 nt" ::"v"(to), "v"(bits) : "memory");
+    // In asm, since the compiler would make one ordinary store of the two branches; with the
+    // wait state that a store of more than 8 bytes needs before its data may be overwritten,
+    // which the compiler does not see to here.
+    if (nt)
+      asm volatile("global_store_dwordx4 %0, %1, off sc1 nt\n\ts_nop 1" ::"v"(to), "v"(bits)
+                   : "memory");
     else
       *reinterpret_cast<u4_any *>(to) = bits;
   } else {
