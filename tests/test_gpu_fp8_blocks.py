@@ -226,6 +226,30 @@ def test_tiles_zero_and_padding():
     assert H.quantize_fp8_tiles(w[:0])[0].shape == (0, 200)
 
 
+@pytest.mark.parametrize("m,k", [(1031, 4096), (8195, 4097), (8200, 4224)])
+def test_large_quantizers(m, k):
+    """Sizes whose input and codes take other cache policies, on sampled rows."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(m)
+    x = torch.randn((m, k), generator=gen, device="cuda").to(torch.bfloat16)
+    rows = np.unique(np.r_[np.arange(0, m, 37), m - 1])
+    pick = torch.from_numpy(rows).cuda()
+    for n in (1, 64, 128) if k % 128 == 0 else (1,):
+        codes, scales = H.transform_fp8_blocks(x, n=n)
+        y = _hadamard_rows(x[pick].double().cpu().numpy() * W.default_scale(n), n)
+        R.check_rows(y, codes[pick].cpu().numpy(), scales[pick].cpu().numpy(), f"rows n={n}")
+    codes, scales, codes_t = H.quantize_fp8_tiles(x, transposed=True)
+    assert torch.equal(codes.t(), codes_t)
+    cut = slice(m // 128 * 128 - 256, m)
+    R.check_tiles(x[cut].double().cpu().numpy(), codes[cut].cpu().numpy(),
+                  scales[m // 128 - 2:].cpu().numpy(), "tiles")
+    codes, scales = H.quantize_fp8_columns(x)
+    cols = np.unique(np.r_[np.arange(0, k, 41), k - 1])
+    pick = torch.from_numpy(cols).cuda()
+    y = R.pad_to(x[:, pick].double().cpu().numpy().T, 1, 128)
+    R.check_rows(y, codes[pick].cpu().numpy(), scales[pick].cpu().numpy(), "columns")
+
+
 # ---- products --------------------------------------------------------------------
 
 
