@@ -893,23 +893,24 @@ __device__ __forceinline__ void sum_tiles(const ProductArgs &p, uint8_t *tiles, 
   };
 
   // One of a thread's kLoads loads of block kb.  In the last, partial block (TAIL) chunks
-  // wholly past k may lie past the matrix: the row's first one is loaded instead.
+  // wholly past k may lie past the matrix: the row's first one is loaded instead, so the
+  // block's offset is the lane's there.
   const auto load_piece = [&](int kb, int stage, int i, auto is_tail) {
     if (i >= kTiles) {
       load_word_to_lds(scale_at[i - kTiles] + kb,
                        lds_address(&scales[stage][(i - kTiles) * kThreads + wave * kWave]));
       return;
     }
-    int from = off[i];
+    int from = off[i], at = kb * kBlock;
     if constexpr (decltype(is_tail)::value) {
       const int s = (i < kLoadsA ? i : i - kLoadsA) * kThreads + t;
       const int c = ((s & 7) ^ ((s >> 4) & 7)) << 4;
-      if (c >= tail) from -= c + kb * kBlock;
+      from = c < tail ? from + at : from - c;
+      at = 0;
     }
     // A's rows and then B's
     load_to_lds(i < kLoadsA ? ra : rb,
-                lds_address(ring + stage * kStageBytes) + (i * kThreads + wave * kWave) * 16, from,
-                kb * kBlock);
+                lds_address(ring + stage * kStageBytes) + (i * kThreads + wave * kWave) * 16, from, at);
   };
 
   f4 acc[TM][TN];
@@ -1264,13 +1265,18 @@ __global__ __launch_bounds__(W *kWave) void few_rows_kernel(ProductArgs p) {
     for (int i = 0; i < 2 * (MT + RB); ++i) {
       const bool of_b = i >= 2 * MT;
       int off = of_b ? off_b[of_b ? i - 2 * MT : 0] : off_a[of_b ? 0 : i];
-      // chunks wholly past k may lie past the matrix: the row's first one instead
-      const int c = chunk((of_b ? i - 2 * MT : i) * kWave + lane);
-      if (kb == kb_tail && c >= tail) off -= c + kb * kBlock;
+      int at = kb * kBlock;
+      if (kb == kb_tail) {
+        // chunks wholly past k may lie past the matrix: the row's first one instead, so the
+        // block's offset is the lane's
+        const int c = chunk((of_b ? i - 2 * MT : i) * kWave + lane);
+        off = c < tail ? off + at : off - c;
+        at = 0;
+      }
       if (of_b)
-        load_to_lds<NT>(rb, to + i * kWave * 16, off, kb * kBlock);
+        load_to_lds<NT>(rb, to + i * kWave * 16, off, at);
       else
-        load_to_lds(ra, to + i * kWave * 16, off, kb * kBlock);
+        load_to_lds(ra, to + i * kWave * 16, off, at);
     }
 #pragma unroll
     for (int i = 0; i < kScaleLoads; ++i)
