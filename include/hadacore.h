@@ -53,7 +53,8 @@
  * choice.  For 2^16 < n < 2^20 "passes" and "parts" force one of the two ways of
  * hadamard_transform_ws, and "parts-defer" also sets the waits of an in-place
  * call to zero, so that its parts go through the workspace; "parts-wait-N" to at
- * most N polls.
+ * most N polls.  "tiles-64", "tiles-64x128", "tiles-128" and "tiles-256" force the
+ * tile of the FP8 products (the last not for 32-bit outputs).
  *
  * Launches: a call is one kernel launch, or up to two for n > 2^16; m so
  * large that a launch would exceed 2^31 work-items (2^33 elements) is split
@@ -305,7 +306,8 @@ int64_t hadacore_padded_tokens(int64_t tokens, int64_t groups);
  * hadacore_padded_tokens(m, groups), get zero codes and scales.  Rows after the last end
  * are left out.
  *   in          m rows of k 16-bit values, any stride >= k (<= 2^26), 2-byte aligned
- *   ends        the groups' ends; NULL with groups = 1: one group of all rows
+ *   ends        the groups' ends; NULL with groups = 1: one group of all rows; not read
+ *               with groups = 0
  *   out_codes   k rows of hadacore_padded_tokens(m, groups) bytes
  *   out_scales  k rows of a 128th of that
  * Ranges must not overlap.  m is at most 2^22 by the stride of the codes.

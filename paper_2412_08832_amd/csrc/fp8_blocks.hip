@@ -285,6 +285,7 @@ constexpr int kTurns = 2;
 // Rows rotated by 2^L <= 64 values: 16 lanes hold a block of 128, 8 consecutive values
 // each, so the stages on index bits 0-2 are in registers and those on bits 3-5 between
 // lanes.  HBM-bound; a group of lanes takes kTurns blocks, whose loads go out together.
+// 8192 bf16 rows of 8192 without rotation: 34 us, 5.9 TB/s.
 template <int DT, int L, int POLICY>
 __global__ __launch_bounds__(256) void short_rotation_kernel(
     const uint16_t *in, int64_t in_stride, uint8_t *codes, int64_t codes_stride, float *scales,
@@ -387,7 +388,9 @@ hipError_t short_rotations(const uint16_t *in, int64_t in_stride, uint8_t *codes
 // column and 128 rows, transposed codes only).  A workgroup takes one tile: thread t
 // holds the 8 x 8 square of rows 8 * (t / 16) and columns 8 * (t % 16), whose codes it
 // transposes in registers; the transposed tile goes through LDS so that its rows leave
-// as whole 128-byte lines.  HBM-bound.
+// as whole 128-byte lines.  HBM-bound: 8 bf16 weights of 2048 x 4096 to both orders 42 us,
+// 6.4 TB/s; 8191 rows of 4096 in 8 groups to columns 18.6 us, 5.7 TB/s.  All of a thread's
+// loads go out before anything uses one; before they did, 52 and 26 us.
 struct TileArgs {
   const uint16_t *in;
   int64_t in_stride, in_batch;
@@ -427,7 +430,7 @@ __global__ __launch_bounds__(256) void tile_kernel(TileArgs p) {
   const int out_block = blockIdx.y;  // block of rows of the output (a padded one for columns)
   int row0 = out_block * kBlock, row_end = p.m;
   if constexpr (COLUMNS) {
-    if (p.ends != nullptr) {
+    if (p.ends != nullptr || p.groups == 0) {
       const Piece piece = find_piece(p.ends, p.groups, p.m, kBlock, out_block, false);
       row0 = piece.low;
       row_end = piece.group < 0 ? 0 : piece.high;
@@ -761,6 +764,16 @@ __device__ __forceinline__ int tile_column(int j, int i) {
 //
 // LDS rows are 128 bytes; chunk c of row r lies at c ^ ((r >> 1) & 7), which the loads
 // obey by choosing their global chunk, since LDS addresses of a load run with the lane.
+//
+// Both operands go through LDS: a step of 256 x 256 reads 1536 cycles of it and writes 512,
+// as many as its MFMAs take, so the two bound it together, at the clock that the card's
+// power leaves (1.83 GHz of 2.4).  Loading B to registers in the MFMA's order touches 64
+// lines an instruction and was 3 times slower, weights laid out for it beforehand reached
+// 2.14 PFLOP/s, MFMAs of 32 x 32 x 64 spilled (2.2).  Measured: 16384 x 4096 x 4096 with tile
+// scales to bf16 230 us, 2.39 PFLOP/s; 4001 tokens' gradient of 4096 x 4096, scales of both
+// rows, 73 us, 1.85 PFLOP/s (a scale of B costs 8 VALU operations a product more); to 32
+// bits, 8 gradients of 2048 x 4096 from 8191 tokens, 179 us, 0.77 PFLOP/s (half the MFMA rate,
+// the widening, and a 256 MiB store).
 // A tile's rows and columns, where its outputs start, and its blocks of k.
 struct Tile {
   int m0, n0, m_end, kb0, kb1;
@@ -1164,7 +1177,8 @@ __device__ __forceinline__ void sum_tiles(const ProductArgs &p, uint8_t *tiles, 
 // One tile to a workgroup, or (LOOP) as many workgroups as run together, each going through
 // tiles.  SPLIT: the tiles of the last turn, if they would leave half of the workgroups or
 // more without one, are cut into quarters: a turn of quarters with k = 4096 takes 21 us
-// where one of whole tiles takes 60 (16384 tokens over 16 experts: 181 us instead of 191).
+// where one of whole tiles takes 60 (16384 tokens over 16 experts of 2048 x 4096: 180 us
+// instead of 189).
 template <int BM, int BN, int WM, int WN, int D, int KS, bool LOOP, bool SPLIT, bool BROWS, bool FULL>
 __global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs p) {
   using S = Shape<BM, BN, WM, WN, D, KS, BROWS>;
@@ -1201,6 +1215,10 @@ __global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs 
 // D stages of LDS of its own, so there is no barrier before the sums: with its loads D - 1
 // stages ahead it waits for the oldest only.  Loads of 16 bytes a lane straight to
 // registers in the MFMA's order would touch 64 cache lines an instruction, in LDS order 8.
+// Measured: one row by 4096 x 4096 5.7 us and by 8192 x 8192 13.4 (5.0 TB/s, of which 2.5 us
+// are the start), 64 tokens over 28 of 32 experts of 2048 x 4096 36 us (6.5 TB/s).  Tiles of
+// 64 x 32 and 32 x 64 gained 11% at 64 rows by 8192 x 8192 (22.8 us instead of 25.7), and lost
+// 30% at 4096 x 4096; three stages and other orders of k changed nothing.
 template <int MT, int RB, int W, int D, bool NT, bool FULL>
 __global__ __launch_bounds__(W *kWave) void few_rows_kernel(ProductArgs p) {
   constexpr int kRowsA = 16 * MT, kRowsB = 16 * RB;
@@ -1486,8 +1504,8 @@ int tile_override() {
 hipError_t launch_product(ProductArgs p, bool b_rows, hipStream_t stream) {
   // Outputs of this size do not stay in the last-level cache for their reader, and push out
   // of the L2s what other tiles still read.  With the policy SC1 | NT, us: 128 MiB of 16384
-  // x 4096 bf16 outputs 240 instead of 264 (k = 4096), 74.7 instead of 82.9 (k = 1024), 256
-  // MiB of gradients 182 instead of 200; 64 MiB by expert 193 instead of 190.
+  // x 4096 bf16 outputs 233 instead of 259 (k = 4096), 72.3 instead of 82.8 (k = 1024), 256
+  // MiB of gradients 178 instead of 197; but 64 MiB by expert 185 instead of 179.
   p.nt_out = (int64_t)p.m * p.n * (p.kind == kGradient ? p.groups : 1) *
                  (p.out_type == HADACORE_FP32 ? 4 : 2) >= (int64_t(1) << 27);
   int best = -1;
@@ -1506,7 +1524,7 @@ hipError_t launch_product(ProductArgs p, bool b_rows, hipStream_t stream) {
     }
   }
   // weights of this size that are read once do not stay in the last-level cache beside
-  // others: streamed, 64 tokens over 32 experts of 2048 x 4096 take 40.6 us instead of 46.8
+  // others: streamed, 64 tokens over 32 experts of 2048 x 4096 take 40.4 us instead of 46.4
   // and 16 rows by 8192 x 8192 13.9 instead of 14.8; but 4096 x 4096 6.3 instead of 5.8, and
   // 64 rows by 8192 x 8192, which two workgroups read, 29.6 instead of 25.7
   const int64_t read = p.kind == kGroups ? (p.groups < p.m ? p.groups : p.m) : 1;
@@ -1680,7 +1698,7 @@ extern "C" hadacore_status hadacore_quantize_fp8_columns(
     const void *in, int64_t in_row_stride, const int32_t *ends, int64_t groups, void *out_codes,
     int64_t out_row_stride, float *out_scales, int64_t scales_row_stride, int64_t m, int64_t k,
     hadacore_dtype dtype, void *stream) {
-  if (m < 0 || k < 0 || groups < 0 || (ends == nullptr && groups != 1))
+  if (m < 0 || k < 0 || groups < 0 || (ends == nullptr && groups > 1))
     return HADACORE_ERROR_INVALID_VALUE;
   if (dtype != HADACORE_FP16 && dtype != HADACORE_BF16) return HADACORE_ERROR_INVALID_DTYPE;
   if (m >= kMaxDim || k >= kMaxDim || groups >= kMaxDim) return HADACORE_ERROR_TOO_LARGE;
@@ -1851,7 +1869,7 @@ extern "C" hadacore_status hadacore_weight_gradient_fp8_grouped(
     const int32_t *ends, int64_t groups, void *out, int64_t out_row_stride,
     int64_t out_batch_stride, hadacore_dtype out_dtype, int64_t places, int64_t n, int64_t k,
     void *stream) {
-  if (places < 0 || n < 0 || k < 0 || groups < 0 || (ends == nullptr && groups != 1))
+  if (places < 0 || n < 0 || k < 0 || groups < 0 || (ends == nullptr && groups > 1))
     return HADACORE_ERROR_INVALID_VALUE;
   if (places % kBlock != 0) return HADACORE_ERROR_INVALID_SIZE;
   if (places >= kMaxDim || n >= kMaxDim || k >= kMaxDim || groups >= kMaxDim)

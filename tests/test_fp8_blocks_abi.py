@@ -99,6 +99,15 @@ def test_matmul_refusals(change, status):
     assert _status(H.hadacore_matmul_fp8, MATMUL, **change) == status
 
 
+@cpu_only
+def test_no_groups_need_no_ends():
+    """An empty tensor of ends has no address."""
+    assert _status(H.hadacore_quantize_fp8_columns, COLUMNS, ends=0, groups=0, m=100) == "SUCCESS"
+    assert _status(H.hadacore_matmul_fp8_grouped, GROUPED, ends=0, groups=0, m=0) == "SUCCESS"
+    assert _status(H.hadacore_weight_gradient_fp8_grouped, GRADIENT, ends=0, groups=0) == "SUCCESS"
+    assert _status(H.hadacore_weight_gradient_fp8_grouped, GRADIENT, ends=0, groups=2) == "INVALID_VALUE"
+
+
 GROUPED = dict(a=X, a_stride=304, sa=S, sa_stride=3, b=C, b_stride=304, b_batch=304 * 40, sb=S + 4096,
                sb_stride=3, sb_batch=3, ends=E, groups=4, out=O, out_stride=40, dtype=H.FP16, m=7, n=40,
                k=300, stream=0)

@@ -331,6 +331,25 @@ def test_matmul_nothing_to_add(variant):
     assert H.matmul_fp8(b, z((9, 1), device="cuda"), a, z((0, 1), device="cuda")).shape == (9, 0)
 
 
+@pytest.mark.parametrize("m", [1, 20, 1000])
+@pytest.mark.parametrize("out", OUTS)
+def test_no_groups_at_all(m, out, variant):
+    """Without a group every row comes after the last end: zeros."""
+    import torch
+    z = torch.zeros
+    a, sa = z((m, 256), dtype=torch.uint8, device="cuda"), z((m, 2), device="cuda")
+    b, sb = z((0, 200, 256), dtype=torch.uint8, device="cuda"), z((0, 2, 2), device="cuda")
+    ends = z(0, dtype=torch.int32, device="cuda")
+    y = H.grouped_matmul_fp8(a, sa, b, sb, ends,
+                             out=torch.full((m, 200), 3.0, dtype=_torch_type(out), device="cuda"))
+    assert (y == 0).all()
+    x = torch.ones((m, 200), dtype=torch.float16, device="cuda")
+    codes, scales = H.quantize_fp8_columns(x, ends)
+    assert codes.shape == (200, H.hadacore_padded_tokens(m, 0))
+    assert (codes == 0).all() and (scales == 0).all()
+    assert H.grouped_weight_gradient_fp8(codes, scales, codes, scales, ends).shape == (0, 200, 200)
+
+
 @pytest.mark.parametrize("m", [1, 20, 200])
 @pytest.mark.parametrize("out", OUTS)
 def test_matmul_nan_and_inf_stay_in_their_row(m, out, variant):
