@@ -468,13 +468,16 @@ def _stream_of(stream, device: int):
 
 def _padded_rows(shape: tuple, device):
     """A uint8 tensor whose rows start on 16-byte boundaries and are readable up to the
-    next one (what lies there is ignored): what the quantizers write and the products read."""
-    pitch = (shape[-1] + 15) & ~15
+    next one (what lies there is ignored): what the quantizers write and the products read.
+    Returns it and its row stride."""
+    k = shape[-1]
+    pitch = (k + 15) & ~15
     if len(shape) == 2:
-        if pitch == shape[1]:
-            return _torch.empty_strided(shape, (pitch, 1), dtype=_torch.uint8, device=device)
-        return _torch.empty((shape[0], pitch), dtype=_torch.uint8, device=device)[:, : shape[1]]
-    return _torch.empty((*shape[:-1], pitch), dtype=_torch.uint8, device=device)[..., : shape[-1]]
+        padded, steps = (shape[0], pitch), (pitch, 1)
+    else:
+        padded, steps = (shape[0], shape[1], pitch), (shape[1] * pitch, pitch, 1)
+    codes = _torch.empty_strided(padded, steps, dtype=_torch.uint8, device=device)
+    return codes if pitch == k else codes.narrow(-1, 0, k), pitch
 
 
 def _operand(name: str, codes, scales, rows: int, device: int):
@@ -511,13 +514,6 @@ def _row_stride(t, least: int) -> int:
     return t.stride(-2) if t.shape[-2] > 1 else least
 
 
-def _pitch(codes) -> int:
-    """The row stride of codes (of a single row: its padded length; of empty rows 0)."""
-    if codes.shape[-1] == 0:
-        return 0
-    return codes.stride(-2) if codes.shape[-2] > 1 else (codes.shape[-1] + 15) & ~15
-
-
 def _new_scales(scales, shape: tuple, device):
     if scales is None:
         return _torch.empty_strided(shape, (shape[1], 1), dtype=_float32, device=device)
@@ -528,12 +524,14 @@ def _new_scales(scales, shape: tuple, device):
 
 
 def _new_codes(codes, shape: tuple, device):
+    """The codes' tensor and row stride (of a single row: its padded length; of empty rows 0)."""
     if codes is None:
         return _padded_rows(shape, device)
     if codes.dtype not in _code_types or tuple(codes.shape) != shape or codes.device != device \
             or (shape[-1] > 1 and codes.stride(-1) != 1):
         raise ValueError(f"codes must be a {shape} uint8 tensor with contiguous rows")
-    return codes
+    k = shape[-1]
+    return codes, 0 if k == 0 else codes.stride(-2) if shape[-2] > 1 else (k + 15) & ~15
 
 
 def transform_fp8_blocks(x, n: int | None = None, codes=None, scales=None,
@@ -559,10 +557,10 @@ def transform_fp8_blocks(x, n: int | None = None, codes=None, scales=None,
     n = max(k, 1) if n is None else int(n)
     blocks = (k + 127) >> 7
     where = x.device
-    codes = _new_codes(codes, (m, k), where)
+    codes, pitch = _new_codes(codes, (m, k), where)
     scales = _new_scales(scales, (m, blocks), where)
     _call("hadamard_transform_fp8_blocks", device, x.data_ptr(), in_stride if m > 1 else k,
-          codes.data_ptr(), _pitch(codes), scales.data_ptr(), _row_stride(scales, blocks), m, k, n,
+          codes.data_ptr(), pitch, scales.data_ptr(), _row_stride(scales, blocks), m, k, n,
           code, _default_scale(n) if scale is None else scale, _stream_of(stream, device))
     return codes, scales
 
@@ -600,10 +598,10 @@ def quantize_fp8_columns(x, ends=None, codes=None, scales=None, stream=None):
         groups, ends_ptr = ends.shape[0], ends.data_ptr()
     blocks = (m + 127 * min(groups, m)) >> 7  # hadacore_padded_tokens
     where = x.device
-    codes = _new_codes(codes, (k, blocks << 7), where)
+    codes, pitch = _new_codes(codes, (k, blocks << 7), where)
     scales = _new_scales(scales, (k, blocks), where)
     _call("hadacore_quantize_fp8_columns", device, x.data_ptr(), in_stride if m > 1 else k, ends_ptr,
-          groups, codes.data_ptr(), _pitch(codes), scales.data_ptr(), _row_stride(scales, blocks), m,
+          groups, codes.data_ptr(), pitch, scales.data_ptr(), _row_stride(scales, blocks), m,
           k, code, _stream_of(stream, device))
     return codes, scales
 
@@ -627,18 +625,21 @@ def quantize_fp8_tiles(w, transposed: bool = False, stream=None):
     if steps[-1] != 1 and k > 1:
         raise ValueError("rows must be contiguous (column stride 1)")
     code = _dtype_code(w)
-    codes = _padded_rows((*lead, n, k), where)
-    codes_t = _padded_rows((*lead, k, n), where) if transposed else None
-    scales = _torch.empty((*lead, (n + 127) >> 7, (k + 127) >> 7), dtype=_float32, device=where)
+    rows, blocks = (n + 127) >> 7, (k + 127) >> 7
+    batch = lead[0] if lead else 1
+    codes, pitch = _padded_rows((batch, n, k) if lead else (n, k), where)
+    scales = _torch.empty_strided((batch, rows, blocks) if lead else (rows, blocks),
+                                  (rows * blocks, blocks, 1) if lead else (blocks, 1),
+                                  dtype=_float32, device=where)
+    codes_t, address_t, pitch_t = None, None, 0
+    if transposed:
+        codes_t, pitch_t = _padded_rows((batch, k, n) if lead else (k, n), where)
+        address_t = codes_t.data_ptr()
     # the steps from one matrix to the next are not used for a single one
-    batch, in_step, step, t_step, scales_step = 1, 0, 0, 0, 0
-    if lead:
-        batch, in_step, step, scales_step = lead[0], steps[0], codes.stride(0), scales.stride(0)
-        t_step = codes_t.stride(0) if transposed else 0
-    _call("hadacore_quantize_fp8_tiles", device, w.data_ptr(), steps[-2] if n > 1 else k, in_step,
-          codes.data_ptr(), _pitch(codes), step, codes_t.data_ptr() if transposed else None,
-          _pitch(codes_t) if transposed else 0, t_step, scales.data_ptr(), scales.stride(-2),
-          scales_step, batch, n, k, code, _stream_of(stream, device))
+    _call("hadacore_quantize_fp8_tiles", device, w.data_ptr(), steps[-2] if n > 1 else k,
+          steps[0] if lead else 0, codes.data_ptr(), pitch, n * pitch, address_t, pitch_t,
+          k * pitch_t, scales.data_ptr(), blocks, rows * blocks, batch, n, k, code,
+          _stream_of(stream, device))
     return (codes, scales, codes_t) if transposed else (codes, scales)
 
 
