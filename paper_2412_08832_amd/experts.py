@@ -74,6 +74,18 @@ def linear(x: torch.Tensor, weights: Weights, ends: torch.Tensor | None = None) 
     return _product(a, a_scales, weights.codes, weights.scales, ends, x.dtype)
 
 
+class _NoSecondDerivative(torch.autograd.Function):
+    """The identity, whose gradient raises."""
+    @staticmethod
+    def forward(ctx, g):
+        return g.view_as(g)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("the FP8 linear layers have no second derivative: a gradient taken with "
+                           "create_graph=True is not to be differentiated")
+
+
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, ends, rotate):
@@ -84,6 +96,16 @@ class _Linear(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy):
+        with torch.no_grad():
+            grads = _Linear.gradients(ctx, dy)
+        if torch.is_grad_enabled():
+            # create_graph=True: the gradients depend on dy and on w or x, through calls that
+            # autograd does not see.  once_differentiable would mark them for dy's sake only.
+            grads = [g if g is None else _NoSecondDerivative.apply(g.requires_grad_()) for g in grads]
+        return *grads, None, None
+
+    @staticmethod
+    def gradients(ctx, dy):
         x, ends, codes_t, scales_t = ctx.saved_tensors
         dy = dy.contiguous()
         dx = dw = None
@@ -96,13 +118,13 @@ class _Linear(torch.autograd.Function):
             a, a_scales = hadacore.quantize_fp8_columns(rotate_rows(x.contiguous(), ctx.rotate), ends)
             dw = hadacore.grouped_weight_gradient_fp8(d, d_scales, a, a_scales, ends, dtype=x.dtype)
             dw = rotate_rows(dw, ctx.rotate, out=dw)
-        return dx, dw, None, None
+        return dx, dw
 
 
 def train_linear(x: torch.Tensor, w: torch.Tensor, ends: torch.Tensor | None = None,
                  rotate: int | None = None) -> torch.Tensor:
     """``linear`` with gradients of ``x`` and ``w`` (both float16 or both bfloat16), whose
-    codes are made anew."""
+    codes are made anew.  First derivatives only: to differentiate a gradient raises."""
     return _Linear.apply(x, w, ends, rotate)
 
 
