@@ -14,7 +14,11 @@ example below is 0.029 off without the rotation and 0.037 with it.)  Forward:
 Backward, for the output's gradient dy:
 
     dx = (dy (w H)) H          the product with b's transposed codes, then transform
-    dw = (dy^T (x H)) H        quantize_fp8_columns, grouped_weight_gradient_fp8, transform
+    dw = dy^T x                quantize_fp8_columns, grouped_weight_gradient_fp8
+
+The weight gradient is that of w itself: dw = (dy^T (x H)) H, in which the rotations cancel,
+so neither is made.  Between them the values would be held in 16 bits, and those of a row of
+one sign are up to sqrt(rotate) times its largest, past fp16's range.
 
 ``python -m paper_2412_08832_amd.experts`` runs a small layer of experts forward and
 backward on the GPU and prints its errors against 32 bits, with and without the rotation.
@@ -74,6 +78,16 @@ def linear(x: torch.Tensor, weights: Weights, ends: torch.Tensor | None = None) 
     return _product(a, a_scales, weights.codes, weights.scales, ends, x.dtype)
 
 
+def weight_gradient(dy: torch.Tensor, x: torch.Tensor, ends: torch.Tensor | None = None,
+                    dtype: torch.dtype | None = None) -> torch.Tensor:
+    """dy^T x in FP8 (tokens x n, tokens x k), with ``ends`` for each group of rows: the gradient
+    of the layer's weights in ``dtype`` (default: x's), float32 for an optimizer that keeps 32 bits."""
+    d, d_scales = hadacore.quantize_fp8_columns(dy, ends)
+    a, a_scales = hadacore.quantize_fp8_columns(x, ends)
+    return hadacore.grouped_weight_gradient_fp8(d, d_scales, a, a_scales, ends,
+                                                dtype=x.dtype if dtype is None else dtype)
+
+
 class _NoSecondDerivative(torch.autograd.Function):
     """The identity, whose gradient raises."""
     @staticmethod
@@ -90,7 +104,7 @@ class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, ends, rotate):
         q = quantize_weights(w, rotate, backward=ctx.needs_input_grad[0])
-        ctx.rotate = q.rotate
+        ctx.rotate, ctx.weight_dtype = q.rotate, w.dtype
         ctx.save_for_backward(x, ends, q.codes_t, q.scales_t)
         return linear(x, q, ends)
 
@@ -114,10 +128,7 @@ class _Linear(torch.autograd.Function):
             dx = _product(d, d_scales, codes_t, scales_t, ends, x.dtype)
             dx = rotate_rows(dx, ctx.rotate, out=dx)
         if ctx.needs_input_grad[1]:
-            d, d_scales = hadacore.quantize_fp8_columns(dy, ends)
-            a, a_scales = hadacore.quantize_fp8_columns(rotate_rows(x.contiguous(), ctx.rotate), ends)
-            dw = hadacore.grouped_weight_gradient_fp8(d, d_scales, a, a_scales, ends, dtype=x.dtype)
-            dw = rotate_rows(dw, ctx.rotate, out=dw)
+            dw = weight_gradient(dy, x, ends, ctx.weight_dtype)
         return dx, dw
 
 
