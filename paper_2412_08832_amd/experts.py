@@ -13,12 +13,13 @@ example below is 0.029 off without the rotation and 0.037 with it.)  Forward:
 
 Backward, for the output's gradient dy:
 
-    dx = (dy (w H)) H          the product with b's transposed codes, then transform
+    dx = dy w                  transform_fp8_blocks(n=1), the product with w's transposed codes
     dw = dy^T x                quantize_fp8_columns, grouped_weight_gradient_fp8
 
-The weight gradient is that of w itself: dw = (dy^T (x H)) H, in which the rotations cancel,
-so neither is made.  Between them the values would be held in 16 bits, and those of a row of
-one sign are up to sqrt(rotate) times its largest, past fp16's range.
+In dx = (dy (w H)) H and dw = (dy^T (x H)) H the rotations cancel, so neither is made: each
+gradient is one product, rounded once.  Between two rotations it would be held in 16 bits,
+and values of one sign are up to sqrt(rotate) times larger there, past fp16's range.  The
+backward's codes of w are its own (of w H only without a rotation), one pass more over w.
 
 ``python -m paper_2412_08832_amd.experts`` runs a small layer of experts forward and
 backward on the GPU and prints its errors against 32 bits, with and without the rotation.
@@ -33,7 +34,7 @@ from . import hadacore
 
 
 class Weights(NamedTuple):
-    """Weights laid out for the products: codes of w H, and transposed for the backward."""
+    """Weights laid out for the products: codes of w H, and of w, transposed, for the backward."""
     codes: torch.Tensor
     scales: torch.Tensor
     codes_t: torch.Tensor | None
@@ -46,23 +47,24 @@ def default_rotation(k: int) -> int:
     return min(k & -k, 1 << 15)
 
 
-def rotate_rows(x: torch.Tensor, rotate: int, out: torch.Tensor | None = None) -> torch.Tensor:
+def rotate_rows(x: torch.Tensor, rotate: int) -> torch.Tensor:
     """Each ``rotate`` values of the contiguous tensor ``x`` times H / sqrt(rotate)."""
     if rotate == 1 or x.numel() == 0:
-        return x if out is None or out is x else out.copy_(x)
-    y = hadacore.transform(x.view(-1, rotate), out=None if out is None else out.view(-1, rotate))
-    return y.view(x.shape)
+        return x
+    return hadacore.transform(x.view(-1, rotate)).view(x.shape)
 
 
 def quantize_weights(w: torch.Tensor, rotate: int | None = None, backward: bool = True) -> Weights:
     """Weights (n x k, or experts x n x k; float16 or bfloat16) as codes; once for serving,
     every step for training.  ``backward=False`` leaves the transposed codes out."""
     rotate = default_rotation(w.shape[-1]) if rotate is None else rotate
-    rotated = rotate_rows(w.contiguous(), rotate)
-    if not backward:
-        return Weights(*hadacore.quantize_fp8_tiles(rotated), None, None, rotate)
-    codes, scales, codes_t = hadacore.quantize_fp8_tiles(rotated, transposed=True)
-    return Weights(codes, scales, codes_t, scales.transpose(-1, -2).contiguous(), rotate)
+    w, codes_t, scales_t = w.contiguous(), None, None
+    if backward:
+        codes, scales, codes_t = hadacore.quantize_fp8_tiles(w, transposed=True)
+        scales_t = scales.transpose(-1, -2).contiguous()
+    if rotate != 1 or not backward:
+        codes, scales = hadacore.quantize_fp8_tiles(rotate_rows(w, rotate))
+    return Weights(codes, scales, codes_t, scales_t, rotate)
 
 
 def _product(a, a_scales, b, b_scales, ends, dtype):
@@ -104,7 +106,7 @@ class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, ends, rotate):
         q = quantize_weights(w, rotate, backward=ctx.needs_input_grad[0])
-        ctx.rotate, ctx.weight_dtype = q.rotate, w.dtype
+        ctx.weight_dtype = w.dtype
         ctx.save_for_backward(x, ends, q.codes_t, q.scales_t)
         return linear(x, q, ends)
 
@@ -126,7 +128,6 @@ class _Linear(torch.autograd.Function):
         if ctx.needs_input_grad[0]:
             d, d_scales = hadacore.transform_fp8_blocks(dy, n=1)
             dx = _product(d, d_scales, codes_t, scales_t, ends, x.dtype)
-            dx = rotate_rows(dx, ctx.rotate, out=dx)
         if ctx.needs_input_grad[1]:
             dw = weight_gradient(dy, x, ends, ctx.weight_dtype)
         return dx, dw

@@ -92,6 +92,15 @@ def test_inputs_of_one_sign():
     _check(*r["dw"], REL)
 
 
+@pytest.mark.parametrize("ends", [None, [100, 100, 130]])
+def test_input_gradients_of_one_sign(ends):
+    """dx = 1100 everywhere."""
+    import torch
+    w = torch.full((*([3] if ends else []), 2200, K), 0.5, device="cuda")
+    r = _run(_normal(4, 130, K) * 0.1, w, torch.ones((130, 2200), device="cuda"), _ends(ends))
+    _check(*r["dx"], ONE_SIGN)
+
+
 @pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
 @pytest.mark.parametrize("scale", [1e-4, 1.0])
 def test_small_values_keep_their_precision(dtype, scale):
