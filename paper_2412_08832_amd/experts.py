@@ -63,6 +63,11 @@ def quantize_weights(w: torch.Tensor, rotate: int | None = None, backward: bool 
         codes, scales, codes_t = hadacore.quantize_fp8_tiles(w, transposed=True)
         scales_t = scales.transpose(-1, -2).contiguous()
     if rotate != 1 or not backward:
+        # between the rotation and its codes float16 weights are bfloat16, which holds whatever
+        # the rotation of finite weights gives (up to sqrt(rotate) times the largest) for two
+        # roundings of 2^-9, each a thirtieth of the codes' own
+        if rotate != 1 and w.dtype is torch.float16:
+            w = w.bfloat16()
         codes, scales = hadacore.quantize_fp8_tiles(rotate_rows(w, rotate))
     return Weights(codes, scales, codes_t, scales_t, rotate)
 

@@ -101,6 +101,18 @@ def test_input_gradients_of_one_sign(ends):
     _check(*r["dx"], ONE_SIGN)
 
 
+@pytest.mark.parametrize("backward", [False, True])
+def test_weights_of_one_sign(backward):
+    """Weights of 1100, whose rotation is 70400: the layer's outputs stay finite."""
+    import torch
+    from paper_2412_08832_amd import experts as E
+    w = torch.full((130, K), 1100.0, device="cuda").half()
+    w[7] *= -1
+    x = (_normal(5, 50, K) * 0.05).half()
+    want = x.double() @ w.double().t()
+    _check(E.linear(x, E.quantize_weights(w, backward=backward)), want, REL)
+
+
 @pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
 @pytest.mark.parametrize("scale", [1e-4, 1.0])
 def test_small_values_keep_their_precision(dtype, scale):
