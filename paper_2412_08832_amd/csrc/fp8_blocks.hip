@@ -12,7 +12,8 @@
 //   - 16-bit outputs: one MFMA 16x16x128 on the codes.  Its products are exact, but its
 //     adder keeps about 17 bits below the largest of the products it adds: measured on
 //     N(0, 1) operands 1.3e-5 of the result, a twentieth of fp16's rounding and a hundredth
-//     of bf16's.  (The older MFMA 16x16x32 for FP8 measures the same.)
+//     of bf16's.  (The older MFMA 16x16x32 for FP8 measures the same.)  At most a sum is
+//     128 * 2^-16 = 2^-9 of that largest product off, which shows where large products cancel.
 //   - 32-bit outputs: the codes widened to bf16, exactly, and four MFMA 16x16x32 for bf16,
 //     which add in full fp32 (1e-8 for 128 products) at half the rate.
 
