@@ -293,7 +293,8 @@ hadacore_status hadamard_transform_fp8_blocks(const void *in, int64_t in_row_str
 /*
  * hadacore_padded_tokens -- the places that `tokens` tokens in `groups` groups may
  * take when each group is padded to a multiple of 128, whatever the groups:
- * floor((tokens + 127 min(groups, tokens)) / 128) * 128.  0 for negative arguments.
+ * floor((tokens + 127 min(groups, tokens)) / 128) * 128.  0 for negative arguments; the largest
+ * multiple of 128 where the places pass int64.
  */
 int64_t hadacore_padded_tokens(int64_t tokens, int64_t groups);
 

@@ -1692,7 +1692,11 @@ using namespace hadacore;
 
 extern "C" int64_t hadacore_padded_tokens(int64_t tokens, int64_t groups) {
   if (tokens < 0 || groups < 0) return 0;
-  return (tokens + (kBlock - 1) * (groups < tokens ? groups : tokens)) / kBlock * kBlock;
+  int64_t places;
+  if (__builtin_mul_overflow(kBlock - 1, groups < tokens ? groups : tokens, &places) ||
+      __builtin_add_overflow(places, tokens, &places))
+    places = INT64_MAX;
+  return places / kBlock * kBlock;
 }
 
 extern "C" hadacore_status hadacore_quantize_fp8_columns(
@@ -1895,7 +1899,8 @@ extern "C" hadacore_status hadacore_weight_gradient_fp8_grouped(
   p.groups = (int)groups;
   p.kind = kGradient;
   p.out_type = out_dtype;
-  if (groups > 1 && out_batch_stride < (n - 1) * out_row_stride + k)
+  if (groups > 1 && (out_row_stride < k || out_row_stride > kMaxPitch ||
+                     out_batch_stride < (n - 1) * out_row_stride + k))
     return HADACORE_ERROR_INVALID_STRIDE;
   const hadacore_status st = check_product(p, n, k, places, groups, k);
   if (st != HADACORE_SUCCESS || n == 0 || k == 0 || groups == 0) return st;

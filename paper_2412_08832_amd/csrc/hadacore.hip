@@ -2792,7 +2792,7 @@ extern "C" hadacore_status hadamard_transform_fp8_blocks(
   if (dtype != HADACORE_FP16 && dtype != HADACORE_BF16) return HADACORE_ERROR_INVALID_DTYPE;
   if (!isfinite(scale)) return HADACORE_ERROR_INVALID_VALUE;
   const bool wide = n >= 128;  // the transform's kernels, with their rules for the input
-  const int64_t blocks = (k + 127) / 128;
+  const int64_t blocks = k / 128 + (k % 128 != 0);
   if (in_row_stride < k || (wide && in_row_stride % 8 != 0) || out_row_stride < k ||
       out_row_stride % 16 != 0 || scales_row_stride < blocks || in_row_stride > kMaxStride ||
       out_row_stride > kMaxStride || scales_row_stride > kMaxStride)
