@@ -1191,8 +1191,10 @@ __global__ __launch_bounds__(KS *WM *WN *kWave) void product_kernel(ProductArgs 
   Tiles which{BM, BN, p.tiles_m, p.tiles, 0, p.tiles, 0, blockIdx.x};
   if constexpr (LOOP && SPLIT) {
     if (p.kind == kGroups) {
-      // ragged groups: the tiles that there are, not those that there may be
-      which.tiles_m = count_pieces(p.ends, p.groups, p.m, BM, true);
+      // ragged groups: the tiles that there are, not those that there may be (p.tiles_m), which
+      // ends that go down can pass by any number, up to a count that does not fit
+      const uint32_t count = (uint32_t)count_pieces(p.ends, p.groups, p.m, BM, true);
+      which.tiles_m = count < (uint32_t)p.tiles_m ? (int)count : p.tiles_m;
       which.total = (uint32_t)which.tiles_m * (uint32_t)p.tiles_n;
     }
     const uint32_t rest = which.total % gridDim.x;
