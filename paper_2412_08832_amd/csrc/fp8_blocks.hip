@@ -161,15 +161,24 @@ __device__ __forceinline__ void widen8(u4 raw, float (&v)[8]) {
   }
 }
 
-// Cache policy of a quantizer by its size, measured with buffers that are not in the
-// last-level cache (us, plain / kStreamOut / kStreamIn):
-//   8 weights of 2048 x 4096 as tiles 50.2 / 50.7 / 43.7; 8191 x 4096 as columns 21.5 / 18.5 /
-//   22.8; 8192 rows of 8192 without rotation 38.2 / 35.2 / 33.9.
-// So large calls stream their input and store with SC1, and those whose input a later reader
-// may still find in the cache store with SC1 | NT, if the codes are whole lines.  Small calls,
-// whose codes the next product reads from the L2, and others keep the plain policy (8192 rows
-// of 8191: 40 us, streamed 60), and rows off 16 bytes, whose loads share lines, are not
-// streamed in.
+// Cache policy of a quantizer by its size.  Which one is fastest depends on whether the input
+// lies in the last-level cache (256 MB), which a call cannot know; us, plain / kStreamOut /
+// kStreamIn, on inputs in the cache and not:
+//   columns of 2048 x 4096        8.1 /  7.4 /  7.3     7.9 /  7.2 /  7.1
+//              8320 x 4096       22.4 / 22.3 / 24.9    21.2 / 23.4 / 21.8
+//             16384 x 4096       36.7 / 36.6 / 40.3    44.0 / 43.3 / 38.1
+//   tiles of   2048 x 4096        9.4 /  7.6 /  8.7     9.2 /  8.4 /  8.6   (both orders)
+//              8320 x 4096       26.2 / 26.8 / 27.7    25.4 / 28.0 / 24.9
+//          4 x 4096 x 4096       45.3 / 45.2 / 46.5    48.7 / 50.1 / 43.0
+//   rows of    2048 x 4096        7.0 /  6.5 /  7.0     7.1 /  7.0 /  6.7   (not rotated)
+//              8320 x 4096       23.2 / 22.7 / 21.0    19.7 / 19.8 / 19.1
+//             16384 x 4096       37.1 / 37.6 / 39.0    37.2 / 36.2 / 35.4
+// From 2^22 elements codes of whole lines are stored with SC1 | NT, which an input in the
+// cache gains from.  Inputs of more than 64 MiB (2^25 elements) are taken not to be there:
+// they are streamed in, with SC1 stores, which gains up to a seventh if so and costs up to an
+// eighth if not.  Below 2^22 the three are alike, and the next product reads the codes from the
+// L2: plain.  So are codes that are not whole lines (8192 rows of 8191: 40 us, streamed 60),
+// and rows off 16 bytes, whose loads share lines, are not streamed in.
 constexpr int kPlain = 0, kStreamOut = 1, kStreamIn = 2;
 
 int quantizer_policy(int64_t elements, const void *in, int64_t in_stride, const void *codes,
