@@ -265,8 +265,13 @@ hadacore_status hadamard_transform_int8(const void *in, int64_t in_row_stride, v
  * go down give unspecified outputs, but no access out of bounds.  The host does not read
  * them: no call waits for the GPU.
  *
- * Streams, ownership, errors and graph capture are as for the transforms.  Sizes are below
- * 2^30 (HADACORE_ERROR_TOO_LARGE), batches and groups too.
+ * Streams, ownership, errors and graph capture are as for the transforms.
+ *
+ * HADACORE_ERROR_TOO_LARGE: sizes, batches and groups of 2^30 and more (rows of
+ * hadamard_transform_fp8_blocks: 2^31); rows times their stride, or matrices times theirs,
+ * past 2^42 (2^40 there); for hadacore_quantize_fp8_tiles more than 65535 matrices, or more than
+ * 65535 * 128 rows; for the products tiles that take 2^32 work-items or more (at most 512 for
+ * each 16 x 16 outputs).
  */
 
 /*
@@ -344,7 +349,9 @@ hadacore_status hadacore_quantize_fp8_tiles(const void *in, int64_t in_row_strid
 /*
  * hadacore_matmul_fp8 -- out = A B^T for codes A (m x k) and B (n x k):
  *     out[i][j] = sum_b a_scales[i][b] * b_scales[j'][b] * sum_{c in block b} A[i][c] B[j][c],
- * j' = j for b_scale_rows = 1 and j / 128 for b_scale_rows = 128 (weights in tiles).
+ * j' = j for b_scale_rows = 1 and j / 128 for b_scale_rows = 128 (weights in tiles).  The two
+ * scales are multiplied first, in fp32: their product has to be in its range (one that passes it
+ * gives NaN even with zero codes, one below it 0).
  * The products of codes are exact, the blocks are joined in fp32, and the result is
  * rounded once, to nearest even.  The 128 products inside a block
  *   - are added in fp32 for outputs of HADACORE_FP32;

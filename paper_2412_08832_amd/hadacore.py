@@ -667,7 +667,8 @@ def matmul_fp8(a, a_scales, b, b_scales, out=None, dtype=None, stream=None):
 
     ``a`` (m x k) and ``a_scales`` (m x ceil(k / 128)) are as ``transform_fp8_blocks`` gives
     them.  ``b`` (n x k) has a scale per tile of 128 x 128 (``quantize_fp8_tiles``) or one per
-    row and 128 columns, told apart by the rows of ``b_scales``.  ``dtype`` is the output's:
+    row and 128 columns, told apart by the rows of ``b_scales``.  The product of two scales
+    has to be in fp32's range: they are multiplied first.  ``dtype`` is the output's:
     bfloat16 (default), float16 or float32.  Blocks are added in 32 bits and the result is
     rounded once; inside a block a float32 output's sums are fp32, and a 16-bit output's
     are within 2^-9 of the block's largest product (about 17 bits below it are kept), which
