@@ -43,8 +43,8 @@ class Weights(NamedTuple):
 
 
 def default_rotation(k: int) -> int:
-    """The largest power of two that divides k, at most 32768."""
-    return min(k & -k, 1 << 15)
+    """The largest power of two that divides k, at most 32768 (1 for no columns)."""
+    return min(k & -k, 1 << 15) or 1
 
 
 def rotate_rows(x: torch.Tensor, rotate: int) -> torch.Tensor:

@@ -112,3 +112,19 @@ def test_one_gradient_alone(wanted):
     E.train_linear(x, w).backward(dy)
     want = dy @ w if wanted == "x" else dy.t() @ x
     assert torch.allclose(leaf.grad, want.detach(), rtol=1e-12, atol=1e-12)
+
+
+@pytest.mark.parametrize("k,rotate", [(0, 1), (1, 1), (7, 1), (96, 32), (4096, 4096), (3 << 20, 1 << 15)])
+def test_default_rotation(k, rotate):
+    assert E.default_rotation(k) == rotate
+
+
+@pytest.mark.parametrize("ends", [None, [4, 4, 11]])
+def test_nothing_to_multiply(ends):
+    """Rows without columns: zeros, and empty gradients."""
+    x, w, dy, ends = _make(ends)
+    x, w = (t.detach()[..., :0].requires_grad_() for t in (x, w))
+    y = E.train_linear(x, w, ends)
+    assert y.shape == dy.shape and (y == 0).all()
+    y.backward(dy)
+    assert x.grad.shape == x.shape and w.grad.shape == w.shape

@@ -146,3 +146,19 @@ def test_weight_gradient_in_32_bits(ends):
     want = want[0] if ends is None else want
     assert got.dtype == torch.float32 and got.shape == want.shape and float(got.max()) > 65504
     _check(got, want, ONE_SIGN)
+
+
+@pytest.mark.parametrize("tokens,n,k", [(5, 4, 0), (0, 4, 256), (5, 0, 256)])
+@pytest.mark.parametrize("groups", [0, 2])
+def test_empty_layers(tokens, n, k, groups):
+    """No tokens, no outputs or no columns: zeros, and gradients of the operands' shapes."""
+    import torch
+    from paper_2412_08832_amd import experts as E
+    x = torch.ones((tokens, k), dtype=torch.float16, device="cuda", requires_grad=True)
+    w = torch.ones((*([groups] if groups else []), n, k), dtype=torch.float16, device="cuda",
+                   requires_grad=True)
+    y = E.train_linear(x, w, _ends([tokens // 2, tokens]) if groups else None)
+    assert y.shape == (tokens, n) and (y == 0).all()
+    y.backward(torch.ones_like(y))
+    assert x.grad.shape == x.shape and (x.grad == 0).all()
+    assert w.grad.shape == w.shape and (w.grad == 0).all()
