@@ -732,7 +732,8 @@ struct Operand<true> {
 // Which tile a workgroup takes.  Workgroups go to the 8 XCDs in turn, each with an L2 of
 // its own: of 256 that run together (one to a CU), each XCD takes 32 consecutive tiles, and
 // tiles are numbered in bands of kBand rows, down the band first, so that 32 tiles read
-// 4 strips of A and 8 of B.
+// 4 strips of A and 8 of B.  (On a part of a card the numbering is as complete, only the strips
+// are shared less.)
 struct TileAt {
   int matrix, m, n;
 };
@@ -782,7 +783,7 @@ __device__ __forceinline__ int tile_column(int j, int i) {
 // 2.14 PFLOP/s, MFMAs of 32 x 32 x 64 spilled (2.2).  Measured: 16384 x 4096 x 4096 with tile
 // scales to bf16 230 us, 2.39 PFLOP/s; 4001 tokens' gradient of 4096 x 4096, scales of both
 // rows, 73 us, 1.85 PFLOP/s (a scale of B costs 8 VALU operations a product more); to 32
-// bits, 8 gradients of 2048 x 4096 from 8191 tokens, 179 us, 0.77 PFLOP/s (half the MFMA rate,
+// bits, 8 gradients of 2048 x 4096 from 8191 tokens, 179-197 us, 0.70-0.77 PFLOP/s (half the MFMA rate,
 // the widening, and a 256 MiB store).
 // A tile's rows and columns, where its outputs start, and its blocks of k.
 struct Tile {
@@ -1451,7 +1452,9 @@ hipError_t launch_few(ProductArgs p, bool stream_b, hipStream_t stream) {
 // a wave has blocks of k, and few rows at least the time of reading B.  The times are
 // measured (us; a step with one workgroup to a CU at most, and with all slots taken), for
 // 16-bit outputs of tiles of B scales; rows of scales and 32-bit outputs take the factors.
-// Over 60 random calls the choice was within a tenth of the best for all but a few.
+// Over 80 random calls the choice was within 8% of the best tile for all but three (11, 14 and
+// 24% over it).  The slots are those of a whole card: on a part of one the estimates are off, and
+// the choice may be, not the results.
 struct KernelTime {
   int bm, bn, slots, shares;  // tile, workgroups that run together, shares of k
   float start, alone, full;
