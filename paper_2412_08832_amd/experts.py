@@ -19,7 +19,8 @@ Backward, for the output's gradient dy:
 In dx = (dy (w H)) H and dw = (dy^T (x H)) H the rotations cancel, so neither is made: each
 gradient is one product, rounded once.  Between two rotations it would be held in 16 bits,
 and values of one sign are up to sqrt(rotate) times larger there, past fp16's range.  The
-backward's codes of w are its own (of w H only without a rotation), one pass more over w.
+backward's codes are of w, for which quantize_weights takes one pass more over the weights
+(without a rotation they are the forward's).
 
 ``python -m paper_2412_08832_amd.experts`` runs a small layer of experts forward and
 backward on the GPU and prints its errors against 32 bits, with and without the rotation.
