@@ -82,12 +82,12 @@
 extern "C" {
 #endif
 
-#define HADACORE_VERSION 10300 /* 1.3.0: codes with a scale per block of 128, their products */
+#define HADACORE_VERSION 10400 /* 1.4.0: routing, the exchange by expert, low-rank adapters */
 
 typedef int32_t hadacore_dtype;
 #define HADACORE_FP16 0 /* IEEE binary16 */
 #define HADACORE_BF16 1 /* bfloat16 */
-#define HADACORE_FP32 2 /* IEEE binary32: output of the FP8 products only */
+#define HADACORE_FP32 2 /* IEEE binary32: outputs of the FP8 products; logits, exchange, adapters */
 
 typedef int32_t hadacore_status;
 #define HADACORE_SUCCESS 0
@@ -405,6 +405,174 @@ hadacore_status hadacore_weight_gradient_fp8_grouped(
     const int32_t *ends, int64_t groups, void *out, int64_t out_row_stride,
     int64_t out_batch_stride, hadacore_dtype out_dtype, int64_t places, int64_t n, int64_t k,
     void *stream);
+
+/*
+ * Tokens and weights of their own: routing, the exchange by expert, low-rank adapters.
+ *
+ * A router gives each of m tokens k of its experts.  A slot is a (token, choice) pair, t * k + j.
+ * hadacore_group_tokens sorts slots by group (expert, adapter): `ends` as above, `rows` the place of
+ * each slot and `slots` the slot of each place.  hadacore_dispatch_rows copies the tokens' rows to
+ * their places, where the products by expert take them, and hadacore_combine_rows joins the
+ * products' rows by weight.  The adapters take tokens in place, by `ends` and `slots` (k = 1).
+ *
+ * Values are fp16, bf16 or fp32 (HADACORE_FP32) where a dtype is named; rows start at any
+ * value's address, `*_row_stride` elements apart (at least their width, at most 2^26).  Arrays of
+ * int32 and fp32 are dense.  All sums are fp32 or wider, joined in an order that the sizes fix, and
+ * rounded once: results repeat to the bit.  Wrong ends, rows and slots give unspecified
+ * results, but no access out of bounds.  Outputs must not overlap each other or an input unless
+ * stated.  Workspaces are scratch: two calls in flight at once need two (a captured graph keeps its
+ * own as long as it may run).  Streams, ownership, errors and graph capture are as for the
+ * transforms.
+ *
+ * HADACORE_ERROR_TOO_LARGE: 2^30 slots and more; rows times their stride past 2^42; for the
+ * exchange 2^32 work-items (256 for each token of a gradient, and for each 16 KiB copied or 2048
+ * values, 1024 of fp32, joined); for the adapters 2^27 tokens, or rows of more than 2^22
+ * values, or more than HADACORE_MAX_GROUPS adapters.
+ */
+#define HADACORE_MAX_EXPERTS 1024
+#define HADACORE_MAX_CHOICES 32
+#define HADACORE_MAX_GROUPS 4095
+#define HADACORE_MAX_RANK 256
+
+/* Bytes of workspace of hadacore_route (0 for arguments that it rejects). */
+int64_t hadacore_route_workspace_size(int64_t m, int64_t experts);
+
+/*
+ * hadacore_route -- the k largest logits of each token, their softmax weights, how many
+ * tokens each expert got, and the balance loss.  With p_t the softmax of token t's logits,
+ * c_e how often expert e was chosen, and T the tokens that have an expert:
+ *     loss = experts * sum_e (c_e / sum c) * (sum_t p_te / T),
+ *     out_slopes[e] = d loss / d p_te = experts * c_e / (sum c * T)   (c has no gradient).
+ * Equal logits: the lower index first (-0 is 0; NaN is above all).  An expert whose logit is -Inf is
+ * never chosen, and a token without enough of others gets -1 and weight 0 there; so does a token
+ * whose `valid` is 0, which counts nowhere.  A NaN or +Inf logit makes its token's p NaN.
+ * Weights are p of the chosen, divided by their sum if `renormalize`.  Without any
+ * choice (m = 0 included) counts, slopes and loss are 0.
+ *   logits      m rows of `experts` (1 to HADACORE_MAX_EXPERTS) values
+ *   valid       m bytes, or NULL: all are valid
+ *   k           1 to HADACORE_MAX_CHOICES and at most `experts` (INVALID_SIZE otherwise)
+ *   out_experts, out_weights  m * k values, in falling order of the logits
+ *   workspace   hadacore_route_workspace_size(m, experts) bytes, 4-byte aligned
+ */
+hadacore_status hadacore_route(const void *logits, int64_t logits_row_stride, hadacore_dtype dtype,
+                               const uint8_t *valid, int64_t m, int64_t experts, int64_t k,
+                               int32_t renormalize, int32_t *out_experts, float *out_weights,
+                               int32_t *out_counts, float *out_loss, float *out_slopes,
+                               void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * hadacore_route_gradient -- the gradient of the logits for those of the weights (m * k, or NULL)
+ * and of the loss (one value on the device, or NULL), from what hadacore_route took and gave.
+ * Rows of tokens without an expert get zeros.
+ */
+hadacore_status hadacore_route_gradient(const void *logits, int64_t logits_row_stride,
+                                        hadacore_dtype dtype, const int32_t *chosen,
+                                        const float *weights, const float *slopes,
+                                        const float *dweights, const float *dloss, int64_t m,
+                                        int64_t experts, int64_t k, int32_t renormalize, void *out,
+                                        int64_t out_row_stride, void *stream);
+
+/* Bytes of workspace of hadacore_group_tokens (0 for few slots, and for arguments it rejects). */
+int64_t hadacore_group_workspace_size(int64_t slots, int64_t groups);
+
+/*
+ * hadacore_group_tokens -- slots sorted by group, in their own order inside a group.
+ *   ids        `slots` int32; one outside [0, groups) is of no group
+ *   out_ends   `groups` (at most HADACORE_MAX_GROUPS) values: the end of each group's places
+ *   out_rows   `slots` values: the place of each slot, -1 for a slot of no group
+ *   out_slots  `slots` values: the slot of each place; behind the last end the slots of no group
+ */
+hadacore_status hadacore_group_tokens(const int32_t *ids, int64_t slots, int64_t groups,
+                                      int32_t *out_ends, int32_t *out_rows, int32_t *out_slots,
+                                      void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * hadacore_dispatch_rows -- row t of `in` (m rows of `width` values of 1, 2 or 4 bytes, codes and
+ * their scales as well) copied to the places rows[t * k + j] of `out` (m * k rows).  Places behind the
+ * last end get zeros.  Its gradient is hadacore_combine_rows without weights.  Each place is to be
+ * the row of one slot at most (as hadacore_group_tokens gives them).
+ */
+hadacore_status hadacore_dispatch_rows(const void *in, int64_t in_row_stride, int32_t value_bytes,
+                                       const int32_t *rows, const int32_t *ends, int64_t groups,
+                                       void *out, int64_t out_row_stride, int64_t m, int64_t k,
+                                       int64_t width, void *stream);
+
+/*
+ * hadacore_combine_rows -- out[t] = sum_j weights[t * k + j] * in[rows[t * k + j]], `in` of `places`
+ * rows.  weights = NULL: the sum.  A row outside [0, places) adds nothing, whatever its weight.
+ */
+hadacore_status hadacore_combine_rows(const void *in, int64_t in_row_stride, int64_t places,
+                                      hadacore_dtype dtype, const int32_t *rows,
+                                      const float *weights, void *out, int64_t out_row_stride,
+                                      int64_t m, int64_t k, int64_t width, void *stream);
+
+/*
+ * hadacore_combine_gradient -- the gradients of such a join of m * k rows y:
+ *     dy[rows[t * k + j]] = weights[t * k + j] * dout[t]   (zeros behind the last end),
+ *     dweights[t * k + j] = <dout[t], y[rows[t * k + j]]>  (0 for a slot of no group).
+ * dy or dweights may be NULL; y is read for dweights only.
+ */
+hadacore_status hadacore_combine_gradient(const void *dout, int64_t dout_row_stride, const void *y,
+                                          int64_t y_row_stride, hadacore_dtype dtype,
+                                          const int32_t *rows, const int32_t *ends, int64_t groups,
+                                          const float *weights, void *dy, int64_t dy_row_stride,
+                                          float *dweights, int64_t m, int64_t k, int64_t width,
+                                          void *stream);
+
+/* Bytes of workspace of hadacore_adapters (0 for arguments that it rejects). */
+int64_t hadacore_adapters_workspace_size(int64_t m, int64_t k, int64_t n, int64_t rank,
+                                         int64_t groups);
+
+/*
+ * hadacore_adapters -- out[t] = y[t] + scales[g] * up[g]^T (down[g] x[t]) for the tokens t of each
+ * group g; tokens of no group (behind the last end) get y[t].
+ *   x           m rows of k values of `dtype` (HADACORE_FP16 or _BF16)
+ *   down, up    `groups` matrices of `rank` (1 to HADACORE_MAX_RANK) rows of k, of n values of
+ *               `dtype`: both rank-major; batch strides in elements, not used for one group.
+ *               Adapters of different ranks: zero rows behind the smaller one's
+ *   scales      one fp32 for each group, or NULL: 1
+ *   ends        the groups' ends among the places; NULL with groups = 1: all rows, with 0: none
+ *   slots       the token of each place (hadacore_group_tokens with k = 1), each token once; NULL:
+ *               the tokens themselves are sorted
+ *   y, out      m rows of n values of out_dtype (`dtype` or HADACORE_FP32); y may be out (in place),
+ *               or NULL: zeros
+ *   hidden      NULL, or m rows of fp32 (16-byte aligned, a stride of a multiple of 4 and at least
+ *               rank rounded up to 16): down[g] x[t] by place, zeros up to that width; places behind
+ *               the last end are left as they were.  The gradient of the weights takes it
+ * The gradients of x are the same call on dout with `down` and `up` exchanged and y = NULL.
+ * Between the products h is fp32; the second takes it in parts of 16 bits that sum up to 16 bits of
+ * it for 16-bit outputs (22 for fp16) and to 24 for fp32 (22 for fp16, of the row's largest).  Inf
+ * may give NaN.
+ */
+hadacore_status hadacore_adapters(const void *x, int64_t x_row_stride, const void *down,
+                                  int64_t down_row_stride, int64_t down_batch_stride,
+                                  const void *up, int64_t up_row_stride, int64_t up_batch_stride,
+                                  const float *scales, const int32_t *ends, const int32_t *slots,
+                                  int64_t groups, const void *y, int64_t y_row_stride, void *out,
+                                  int64_t out_row_stride, hadacore_dtype dtype,
+                                  hadacore_dtype out_dtype, float *hidden,
+                                  int64_t hidden_row_stride, int64_t m, int64_t k, int64_t n,
+                                  int64_t rank, void *workspace, int64_t workspace_bytes,
+                                  void *stream);
+
+/* Bytes of workspace of hadacore_adapter_gradient (0 where it needs none, or rejects). */
+int64_t hadacore_adapter_gradient_workspace_size(int64_t m, int64_t width, int64_t rank,
+                                                 int64_t groups);
+
+/*
+ * hadacore_adapter_gradient -- out[g] (rank x width) = scales[g] * sum over the places p of g of
+ * hidden[p] x[token of p]^T: the gradient of `up` from hidden and dout, and that of `down` from the
+ * hidden of the gradient's call (dout, roles exchanged) and x.  A group without tokens gets
+ * zeros.  out_dtype is `dtype` or HADACORE_FP32; other arguments as for hadacore_adapters.
+ */
+hadacore_status hadacore_adapter_gradient(const float *hidden, int64_t hidden_row_stride,
+                                          const void *x, int64_t x_row_stride,
+                                          hadacore_dtype dtype, const float *scales,
+                                          const int32_t *ends, const int32_t *slots,
+                                          int64_t groups, void *out, int64_t out_row_stride,
+                                          int64_t out_batch_stride, hadacore_dtype out_dtype,
+                                          int64_t m, int64_t width, int64_t rank,
+                                          void *workspace, int64_t workspace_bytes, void *stream);
 
 /*
  * hadacore_stream_copy -- copies `bytes` bytes from device pointer `src` to

@@ -12,7 +12,8 @@ from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
 ROOT = PKG.parent
-SOURCES = [PKG / "csrc" / "hadacore.hip", PKG / "csrc" / "fp8_blocks.hip"]
+SOURCES = [PKG / "csrc" / name for name in
+           ("hadacore.hip", "fp8_blocks.hip", "routing.hip", "adapters.hip")]
 INCLUDE = ROOT / "include"
 LIBRARY = PKG / "libhadacore.so"
 ARCH = "gfx950"

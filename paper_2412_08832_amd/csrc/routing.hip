@@ -1,0 +1,1200 @@
+// routing.hip -- from a router's logits to rows sorted by expert, and back.
+//
+//   route     the k experts of each token with their weights, how many tokens each expert
+//             got, the balance loss; its gradient
+//   group     the stable order of (token, choice) slots by group: ends, places, slots
+//   dispatch  rows of tokens copied to the places of their slots
+//   combine   the rows of a token's slots joined by weight; its gradient
+//
+// All of it moves few bytes (or each byte once): what bounds the large calls is HBM, and the small
+// ones their launches, so every call is one launch where a workgroup can do it and two otherwise.
+// No result depends on the order of atomics: the only ones count, in LDS.
+
+#include <hip/hip_runtime.h>
+
+#include <math.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "groups.h"
+#include "hadacore.h"
+#include "internal.h"
+
+namespace hadacore {
+namespace {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+
+constexpr int kMaxChoices = HADACORE_MAX_CHOICES;
+constexpr int kMaxExperts = HADACORE_MAX_EXPERTS;
+
+template <int DT>
+struct Stored {
+  using type = uint16_t;
+};
+template <>
+struct Stored<HADACORE_FP32> {
+  using type = float;
+};
+
+template <int DT>
+__device__ __forceinline__ float widen(typename Stored<DT>::type h) {
+  if constexpr (DT == HADACORE_FP32)
+    return h;
+  else if constexpr (DT == HADACORE_FP16)
+    return (float)__builtin_bit_cast(_Float16, h);
+  else
+    return __builtin_bit_cast(float, (uint32_t)h << 16);
+}
+
+// One rounding, to nearest even.
+template <int DT>
+__device__ __forceinline__ typename Stored<DT>::type narrow(float v) {
+  if constexpr (DT == HADACORE_FP32)
+    return v;
+  else if constexpr (DT == HADACORE_FP16)
+    return __builtin_bit_cast(uint16_t, (_Float16)v);
+  else
+    return __builtin_bit_cast(uint16_t, (__bf16)v);
+}
+
+// N consecutive values, of which the first `valid` exist (the others are `rest`).  Rows may start
+// at any value's address; the hardware takes wide loads and stores from there.
+template <int DT, int N>
+__device__ __forceinline__ void load_row(const typename Stored<DT>::type *p, int valid, float rest,
+                                         float (&v)[N]) {
+  using T = typename Stored<DT>::type;
+  struct __attribute__((packed, aligned(sizeof(T)))) Raw {
+    T v[N];
+  };
+  if (valid >= N) {
+    const Raw raw = *reinterpret_cast<const Raw *>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = widen<DT>(raw.v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = i < valid ? widen<DT>(p[i]) : rest;
+  }
+}
+
+template <int DT, int N>
+__device__ __forceinline__ void store_row(typename Stored<DT>::type *p, int valid, const float (&v)[N]) {
+  using T = typename Stored<DT>::type;
+  struct __attribute__((packed, aligned(sizeof(T)))) Raw {
+    T v[N];
+  };
+  if (valid >= N) {
+    Raw raw;
+#pragma unroll
+    for (int i = 0; i < N; ++i) raw.v[i] = narrow<DT>(v[i]);
+    *reinterpret_cast<Raw *>(p) = raw;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < valid) p[i] = narrow<DT>(v[i]);
+  }
+}
+
+// ---- reductions over the L lanes (a power of two, at least 8) that share a row ----------
+
+template <class F>
+__device__ __forceinline__ uint32_t across(uint32_t x, int lanes, F f) {
+  const auto dpp = [](uint32_t v, auto ctrl) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xF, 0xF, false);
+  };
+  x = f(x, dpp(x, std::integral_constant<int, 0xB1>{}));   // quad_perm: xor 1
+  x = f(x, dpp(x, std::integral_constant<int, 0x4E>{}));   // quad_perm: xor 2
+  x = f(x, dpp(x, std::integral_constant<int, 0x141>{}));  // row_half_mirror
+  if (lanes >= 16) x = f(x, dpp(x, std::integral_constant<int, 0x140>{}));  // row_mirror
+  if (lanes >= 32) {
+    const auto s = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = f(s[0], s[1]);
+  }
+  if (lanes >= 64) {
+    const auto s = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    x = f(s[0], s[1]);
+  }
+  return x;
+}
+
+template <int L>
+__device__ __forceinline__ uint32_t max_across(uint32_t x) {
+  return across(x, L, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+
+// In an order of its own for every L, the same in every lane.
+template <int L>
+__device__ __forceinline__ float sum_across(float x) {
+  return __builtin_bit_cast(
+      float, across(__builtin_bit_cast(uint32_t, x), L, [](uint32_t a, uint32_t b) {
+        return __builtin_bit_cast(uint32_t,
+                                  __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b));
+      }));
+}
+
+// Sum over a workgroup of THREADS, in every thread; `room` holds a value for each wave.
+template <int THREADS, class T>
+__device__ __forceinline__ T sum_workgroup(T x, T *room) {
+#pragma unroll
+  for (int step = 1; step < kWave; step *= 2) x += __shfl_xor(x, step);
+  __syncthreads();
+  if (threadIdx.x % kWave == 0) room[threadIdx.x / kWave] = x;
+  __syncthreads();
+  x = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / kWave; ++w) x += room[w];
+  return x;
+}
+
+// What one lane of a wave wrote to LDS is there for its others: LDS works through a wave's
+// accesses in order, and the compiler may not move them over this.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// ---- choice of experts --------------------------------------------------------------
+//
+// p = softmax(l), S the k largest logits, f_e the share of expert e in all choices, T the tokens:
+//   loss = E sum_e f_e (1/T) sum_t p_te,   slopes_e = d loss / d p_te = E f_e / T.
+// L lanes share a row, V consecutive experts in each, so that an equal logit's lower index is in the
+// lower lane: a choice is one maximum over the lanes and one ballot.  Sums of p stay in the lanes'
+// registers over a workgroup's rows; workgroups leave theirs and their counts in the workspace,
+// and a workgroup joins them in order.
+
+struct RouteArgs {
+  const void *logits;
+  int64_t stride;
+  const uint8_t *valid;
+  int m, experts, k, renormalize;
+  int32_t *chosen;
+  float *weights;
+  int32_t *counts;
+  float *loss, *slopes;
+  // of each workgroup: sums of p, counts, and how many tokens have an expert
+  float *part_p;
+  int32_t *part_counts, *part_tokens;
+};
+
+constexpr int kRouteThreads = 1024;
+
+// Larger logits have larger keys, NaN the largest, and -0 is 0.  0: no logit.
+__device__ __forceinline__ uint32_t order_key(float x) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);
+  if (x != x) return 0xFFFFFFFFu;
+  return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+constexpr uint32_t kNone = 0x007FFFFFu;  // -inf, which is never chosen
+
+__device__ __forceinline__ float from_key(uint32_t k) {
+  return __builtin_bit_cast(float, (k & 0x80000000u) ? k ^ 0x80000000u : ~k);
+}
+
+__device__ void join_routes(const RouteArgs &p, int parts) {
+  constexpr int kWaves = kRouteThreads / kWave;
+  __shared__ float sum_p[kRouteThreads];
+  __shared__ int sum_c[kRouteThreads];
+  __shared__ int room_i[kWaves];
+  __shared__ double room_d[kWaves];
+  const int tid = threadIdx.x;
+  int wide = kWave;
+  while (wide < p.experts) wide *= 2;
+  const int e = tid % wide, rank = tid / wide, ranks = kRouteThreads / wide;
+  float a = 0.0f;
+  int c = 0;
+  if (e < p.experts) {
+#pragma unroll 4
+    for (int b = rank; b < parts; b += ranks) {
+      a += p.part_p[(int64_t)b * p.experts + e];
+      c += p.part_counts[(int64_t)b * p.experts + e];
+    }
+  }
+  int tokens = 0;
+  for (int b = tid; b < parts; b += kRouteThreads) tokens += p.part_tokens[b];
+  sum_p[tid] = a;
+  sum_c[tid] = c;
+  __syncthreads();
+  for (int half = ranks / 2; half > 0; half /= 2) {
+    if (rank < half) {
+      sum_p[tid] += sum_p[tid + half * wide];
+      sum_c[tid] += sum_c[tid + half * wide];
+    }
+    __syncthreads();
+  }
+  const bool mine = rank == 0 && e < p.experts;
+  const int count = mine ? sum_c[e] : 0;
+  tokens = sum_workgroup<kRouteThreads>(tokens, room_i);
+  const int all = sum_workgroup<kRouteThreads>(count, room_i);
+  const double slope =
+      all > 0 ? (double)p.experts * count / ((double)all * tokens) : 0.0;
+  const double loss = sum_workgroup<kRouteThreads>(mine ? slope * sum_p[e] : 0.0, room_d);
+  if (mine) {
+    p.counts[e] = count;
+    p.slopes[e] = (float)slope;
+  }
+  if (tid == 0) *p.loss = (float)loss;
+}
+
+__global__ __launch_bounds__(kRouteThreads) void join_routes_kernel(RouteArgs p, int parts) {
+  join_routes(p, parts);
+}
+
+template <int DT, int L, int V>
+__global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs p) {
+  constexpr int kRows = kRouteThreads / L;
+  struct Pick {
+    int expert;
+    float logit;
+  };
+  __shared__ Pick picks[kRows][kMaxChoices];
+  __shared__ int hist[L * V];
+  __shared__ float sums[kRows / 8][L * V];
+  __shared__ int routed;
+  const int tid = threadIdx.x, q = tid % L, row = tid / L;
+  const int lane = tid % kWave, first = lane - q;
+  for (int i = tid; i < L * V; i += kRouteThreads) hist[i] = 0;
+  if (tid == 0) routed = 0;
+  __syncthreads();
+  float acc[V] = {};
+  int mine_routed = 0;
+  const auto *logits = static_cast<const typename Stored<DT>::type *>(p.logits);
+  const int left = p.experts - q * V;
+  for (int base = blockIdx.x * kRows; base < p.m; base += gridDim.x * kRows) {
+    const int t = base + row;
+    const bool on = t < p.m && (p.valid == nullptr || p.valid[t] != 0);
+    float l[V];
+    load_row<DT, V>(logits + (on ? t : 0) * p.stride + q * V, on ? left : 0, 0.0f, l);
+    uint32_t key[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) key[v] = on && v < left ? order_key(l[v]) : 0;
+    uint32_t top = 0;
+    for (int j = 0; j < p.k; ++j) {
+      uint32_t best = 0;
+#pragma unroll
+      for (int v = 0; v < V; ++v) best = key[v] > best ? key[v] : best;
+      const uint32_t most = max_across<L>(best);
+      if (j == 0) top = most;
+      const uint64_t have = __ballot(best == most) >> first;
+      const bool there = most > kNone;
+      if (q == __builtin_ctzll(have)) {
+        Pick pick{-1, 0.0f};
+        bool open = there;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          if (open && key[v] == most) {
+            pick = {q * V + v, l[v]};
+            key[v] = 0;
+            open = false;
+          }
+        }
+        picks[row][j] = pick;
+      }
+    }
+    wave_sync();
+    const bool any = top > kNone;
+    const float high = from_key(top);
+    float sum = 0.0f, ex[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      ex[v] = any && v < left ? expf(l[v] - high) : 0.0f;
+      sum += ex[v];
+    }
+    sum = sum_across<L>(sum);
+#pragma unroll
+    for (int v = 0; v < V; ++v) acc[v] += any ? ex[v] / sum : 0.0f;
+    mine_routed += any && q == 0;
+    float below = sum;
+    if (p.renormalize) {
+      below = 0.0f;
+      for (int j = q; j < p.k; j += L)
+        below += picks[row][j].expert < 0 ? 0.0f : expf(picks[row][j].logit - high);
+      below = sum_across<L>(below);
+    }
+    if (t < p.m) {
+      for (int j = q; j < p.k; j += L) {
+        const Pick pick = picks[row][j];
+        p.chosen[(int64_t)t * p.k + j] = pick.expert;
+        p.weights[(int64_t)t * p.k + j] = pick.expert < 0 ? 0.0f : expf(pick.logit - high) / below;
+        if (pick.expert >= 0) atomicAdd(&hist[pick.expert], 1);
+      }
+    }
+    wave_sync();
+  }
+  if (mine_routed > 0) atomicAdd(&routed, mine_routed);
+  // an eighth of the rows at a time, in order
+  for (int part = 0; part < 8; ++part) {
+    if (row % 8 == part) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float *to = &sums[row / 8][q * V + v];
+        *to = part == 0 ? acc[v] : *to + acc[v];
+      }
+    }
+    __syncthreads();
+  }
+  for (int e = tid; e < p.experts; e += kRouteThreads) {
+    float a = 0.0f;
+    for (int r = 0; r < kRows / 8; ++r) a += sums[r][e];
+    p.part_p[(int64_t)blockIdx.x * p.experts + e] = a;
+    p.part_counts[(int64_t)blockIdx.x * p.experts + e] = hist[e];
+  }
+  if (tid == 0) p.part_tokens[blockIdx.x] = routed;
+  if (gridDim.x == 1) {
+    __threadfence_block();
+    __syncthreads();
+    join_routes(p, 1);
+  }
+}
+
+struct RouteGradArgs {
+  const void *logits;
+  int64_t stride;
+  const int32_t *chosen;
+  const float *weights, *slopes, *dweights, *dloss;
+  int m, experts, k, renormalize;
+  void *out;
+  int64_t out_stride;
+};
+
+// u_e = dloss slopes_e (and, not renormalized, dw_j at the chosen e): dl = p (u - sum p u);
+// renormalized, dl_e gets w_j (dw_j - sum_S w dw) besides, the softmax over the chosen.
+// p is made again from the logits, which is less to read than p would be.
+template <int DT, int L, int V>
+__global__ __launch_bounds__(256) void route_gradient_kernel(RouteGradArgs p) {
+  constexpr int kRows = 256 / L;
+  __shared__ float extra[kRows][L * V];
+  const int tid = threadIdx.x, q = tid % L, row = tid / L;
+  const int left = p.experts - q * V;
+  const auto *logits = static_cast<const typename Stored<DT>::type *>(p.logits);
+  auto *out = static_cast<typename Stored<DT>::type *>(p.out);
+  float slope[V];
+  load_row<HADACORE_FP32, V>(p.slopes + q * V, p.dloss != nullptr ? left : 0, 0.0f, slope);
+  const float g = p.dloss != nullptr ? *p.dloss : 0.0f;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    slope[v] *= g;
+    extra[row][q * V + v] = 0.0f;
+  }
+  wave_sync();
+  for (int base = blockIdx.x * kRows; base < p.m; base += gridDim.x * kRows) {
+    const int t = base + row;
+    const bool on = t < p.m && p.chosen[(int64_t)(t < p.m ? t : 0) * p.k] >= 0;
+    float l[V];
+    load_row<DT, V>(logits + (on ? t : 0) * p.stride + q * V, on ? left : 0, -INFINITY, l);
+    uint32_t best = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const uint32_t key = v < left ? order_key(l[v]) : 0;
+      best = key > best ? key : best;
+    }
+    const uint32_t top = max_across<L>(best);
+    const float high = from_key(top);
+    float sum = 0.0f, pr[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      pr[v] = on && v < left ? expf(l[v] - high) : 0.0f;
+      sum += pr[v];
+    }
+    sum = sum_across<L>(sum);
+    if (p.dweights != nullptr) {
+      float wd = 0.0f;
+      if (p.renormalize) {
+        for (int j = q; on && j < p.k; j += L)
+          wd += p.weights[(int64_t)t * p.k + j] * p.dweights[(int64_t)t * p.k + j];
+        wd = sum_across<L>(wd);
+      }
+      for (int j = q; on && j < p.k; j += L) {
+        const int64_t at = (int64_t)t * p.k + j;
+        const int e = p.chosen[at];
+        const float dw = p.dweights[at];
+        if (e >= 0 && e < p.experts) extra[row][e] = p.renormalize ? p.weights[at] * (dw - wd) : dw;
+      }
+      wave_sync();
+    }
+    float pu = 0.0f, u[V], add[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      pr[v] = on ? pr[v] / sum : 0.0f;
+      add[v] = 0.0f;
+      if (p.dweights != nullptr) {
+        add[v] = extra[row][q * V + v];
+        extra[row][q * V + v] = 0.0f;
+      }
+      u[v] = slope[v] + (p.renormalize ? 0.0f : add[v]);
+      pu += pr[v] * u[v];
+    }
+    pu = sum_across<L>(pu);
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      u[v] = on ? pr[v] * (u[v] - pu) + (p.renormalize ? add[v] : 0.0f) : 0.0f;
+    if (t < p.m && left > 0) store_row<DT, V>(out + t * p.out_stride + q * V, left, u);
+    wave_sync();
+  }
+}
+
+// Lanes to a row and experts to a lane: four experts in a lane until a row takes the wave.
+template <class F>
+void for_experts(int64_t experts, F f) {
+  using std::integral_constant;
+  if (experts <= 32)
+    f(integral_constant<int, 8>{}, integral_constant<int, 4>{});
+  else if (experts <= 64)
+    f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+  else if (experts <= 128)
+    f(integral_constant<int, 32>{}, integral_constant<int, 4>{});
+  else if (experts <= 256)
+    f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  else if (experts <= 512)
+    f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+  else
+    f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
+}
+
+template <class F>
+void for_type(hadacore_dtype dtype, F f) {
+  if (dtype == HADACORE_FP16)
+    f(std::integral_constant<int, HADACORE_FP16>{});
+  else if (dtype == HADACORE_BF16)
+    f(std::integral_constant<int, HADACORE_BF16>{});
+  else
+    f(std::integral_constant<int, HADACORE_FP32>{});
+}
+
+// Workgroups of a route: one for each set of rows, at most 256, and no more than the joining
+// workgroup reads in a few microseconds (2^16 sums and counts).
+int64_t route_parts(int64_t m, int64_t experts) {
+  int64_t rows = 0;
+  for_experts(experts, [&](auto l, auto) { rows = kRouteThreads / decltype(l)::value; });
+  int64_t parts = (m + rows - 1) / rows;
+  const int64_t most = (1 << 16) / experts < 256 ? (1 << 16) / experts : 256;
+  if (parts > most) parts = most;
+  return parts > 0 ? parts : 1;
+}
+
+// ---- slots by group ------------------------------------------------------------------
+//
+// A stable counting sort.  A wave takes a run of slots of its workgroup's, counts its groups, and
+// gives places 64 slots at a time: lanes of the same group find each other by a ballot for each
+// bit of the id, and rank themselves by their lanes.  A workgroup starts from the slots of earlier
+// groups, and of its own group in earlier workgroups, which it adds up from all counts.
+
+struct GroupArgs {
+  const int32_t *ids;
+  int slots, groups;
+  int32_t *ends, *rows, *order;
+  int32_t *parts;  // counts of each workgroup's slots, groups + 1 each
+  int per_block;   // slots of a workgroup, a multiple of 64 for each wave
+};
+
+constexpr int kGroupThreads = 1024;
+constexpr int kGroupWaves = kGroupThreads / kWave;
+
+__device__ __forceinline__ int group_of(const GroupArgs &p, int slot) {
+  const int id = p.ids[slot];
+  return (uint32_t)id < (uint32_t)p.groups ? id : p.groups;
+}
+
+__global__ __launch_bounds__(kGroupThreads) void count_groups_kernel(GroupArgs p) {
+  extern __shared__ int hist[];
+  const int bins = p.groups + 1;
+  for (int g = threadIdx.x; g < bins; g += kGroupThreads) hist[g] = 0;
+  __syncthreads();
+  const int low = blockIdx.x * p.per_block;
+  const int high = low + p.per_block < p.slots ? low + p.per_block : p.slots;
+  for (int s = low + threadIdx.x; s < high; s += kGroupThreads) atomicAdd(&hist[group_of(p, s)], 1);
+  __syncthreads();
+  for (int g = threadIdx.x; g < bins; g += kGroupThreads)
+    p.parts[(int64_t)blockIdx.x * bins + g] = hist[g];
+}
+
+// W: how many waves share the slots (fewer where the counts of 16 would not fit 64 KiB of LDS).
+template <int W>
+__global__ __launch_bounds__(kGroupThreads) void place_groups_kernel(GroupArgs p) {
+  extern __shared__ int counts[];  // [W][bins], then the base of each group
+  __shared__ int wave_sums[kGroupWaves];
+  const int bins = p.groups + 1, tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
+  int *base = counts + W * bins;
+  for (int i = tid; i < W * bins; i += kGroupThreads) counts[i] = 0;
+  __syncthreads();
+  const int low = blockIdx.x * p.per_block;
+  const int high = low + p.per_block < p.slots ? low + p.per_block : p.slots;
+  const int run = p.per_block / W;
+  const int from = low + wave * run, to = from + run < high ? from + run : high;
+  if (wave < W)
+    for (int s = from + lane; s < to; s += kWave) atomicAdd(&counts[wave * bins + group_of(p, s)], 1);
+  __syncthreads();
+  // slots of each group: in all, and before this workgroup
+  const int each = (bins + kGroupThreads - 1) / kGroupThreads;
+  int sum = 0;
+  for (int i = 0; i < each; ++i) {
+    const int g = tid * each + i;
+    int all = 0, before = 0;
+    if (g < bins) {
+      if (gridDim.x == 1) {
+        for (int w = 0; w < W; ++w) all += counts[w * bins + g];
+      } else {
+#pragma unroll 4
+        for (int b = 0; b < (int)gridDim.x; ++b) {
+          const int c = p.parts[(int64_t)b * bins + g];
+          all += c;
+          before += b < (int)blockIdx.x ? c : 0;
+        }
+      }
+      base[g] = sum + before;
+    }
+    sum += all;
+  }
+  // the groups before this thread's
+  const int upto = prefix_sum(sum);
+  if (lane == kWave - 1) wave_sums[wave] = upto;
+  __syncthreads();
+  int start = upto - sum;
+  for (int w = 0; w < wave; ++w) start += wave_sums[w];
+  for (int i = 0; i < each; ++i) {
+    const int g = tid * each + i;
+    if (g >= bins) break;
+    int at = base[g] + start;
+    // a group's end is where the next one starts: group 0's start is 0
+    if (blockIdx.x == 0 && g > 0) p.ends[g - 1] = at;
+    for (int w = 0; w < W; ++w) {
+      const int c = counts[w * bins + g];
+      counts[w * bins + g] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+  if (wave >= W) return;
+  int bits = 0;
+  while ((1 << bits) < bins) ++bits;
+  for (int s0 = from; s0 < to; s0 += kWave) {
+    const int s = s0 + lane;
+    const bool on = s < to;
+    const int g = on ? group_of(p, s) : 0;
+    uint64_t same = __ballot(on);
+    for (int b = 0; b < bits; ++b) {
+      const uint64_t one = __ballot((g >> b) & 1);
+      same &= (g >> b) & 1 ? one : ~one;
+    }
+    const int ahead = __popcll(same & ((1ull << lane) - 1));
+    int *next = &counts[wave * bins + g];
+    const int at = on ? *next + ahead : 0;
+    wave_sync();
+    if (on && ahead == 0) *next = at + __popcll(same);
+    wave_sync();
+    if (on) {
+      p.rows[s] = g < p.groups ? at : -1;
+      p.order[at] = s;
+    }
+  }
+}
+
+// How many waves of a workgroup share its slots: their counts and the bases fit 64 KiB of LDS.
+int group_waves(int64_t groups) { return groups <= 900 ? 16 : groups <= 3200 ? 4 : 2; }
+
+// Workgroups: one for 4096 slots, where a second launch costs more than it gains (measured at
+// the calls of few slots); their counts at most 2^15, since each workgroup reads them all.
+int64_t group_blocks_of(int64_t slots, int64_t groups) {
+  int64_t blocks = (slots + 4095) / 4096;
+  const int64_t most = (1 << 15) / (groups + 1) < 256 ? (1 << 15) / (groups + 1) : 256;
+  if (blocks > most) blocks = most;
+  return blocks > 0 ? blocks : 1;
+}
+
+// ---- rows to their places, and back --------------------------------------------------
+
+struct DispatchArgs {
+  const uint8_t *in;
+  int64_t in_stride, out_stride;  // bytes
+  const int32_t *rows, *ends;
+  uint8_t *out;
+  int m, k, groups, bytes, size;  // bytes of a row, of a value
+  int chunks;
+};
+
+typedef u4 u4_any __attribute__((aligned(1)));
+
+// One wave copies 4 KiB of a token's row to the places of its slots: the row is read once.  It also
+// clears that part of those of its own slots' places that lie behind the last end.
+constexpr int kDispatchLoads = 4;
+constexpr int kDispatchChunk = kWave * 16 * kDispatchLoads;
+
+__global__ __launch_bounds__(256) void dispatch_kernel(DispatchArgs p) {
+  const int lane = threadIdx.x % kWave;
+  const int64_t id = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+  const int t = (int)(id / p.chunks), chunk = (int)(id % p.chunks);
+  if (t >= p.m) return;
+  const int slots = p.m * p.k;
+  const int used = p.groups > 0 ? clamp_end(p.ends[p.groups - 1], slots) : 0;
+  const int start = chunk * kDispatchChunk + lane * 16;
+  const uint8_t *from = p.in + t * p.in_stride;
+  u4 v[kDispatchLoads];
+#pragma unroll
+  for (int i = 0; i < kDispatchLoads; ++i) {
+    const int at = start + i * kWave * 16;
+    v[i] = u4{0, 0, 0, 0};
+    if (at + 16 <= p.bytes) v[i] = *reinterpret_cast<const u4_any *>(from + at);
+  }
+  const auto put = [&](int row, bool zero) {
+    uint8_t *to = p.out + row * p.out_stride;
+#pragma unroll
+    for (int i = 0; i < kDispatchLoads; ++i) {
+      const int at = start + i * kWave * 16;
+      if (at + 16 <= p.bytes) {
+        *reinterpret_cast<u4_any *>(to + at) = zero ? u4{0, 0, 0, 0} : v[i];
+      } else {
+        // the row's last bytes, value by value
+        for (int b = at; b < p.bytes; b += p.size) {
+          if (p.size == 1)
+            to[b] = zero ? 0 : from[b];
+          else if (p.size == 2)
+            *reinterpret_cast<uint16_t *>(to + b) =
+                zero ? 0 : *reinterpret_cast<const uint16_t *>(from + b);
+          else
+            *reinterpret_cast<uint32_t *>(to + b) =
+                zero ? 0 : *reinterpret_cast<const uint32_t *>(from + b);
+        }
+      }
+    }
+  };
+  for (int j = 0; j < p.k; ++j) {
+    const int slot = t * p.k + j;
+    const int row = __builtin_amdgcn_readfirstlane(p.rows[slot]);
+    if ((uint32_t)row < (uint32_t)used) put(row, false);
+    if (slot >= used) put(slot, true);
+  }
+}
+
+struct CombineArgs {
+  const void *in;
+  int64_t in_stride, out_stride;
+  const int32_t *rows;
+  const float *weights;
+  void *out;
+  int places, m, k, width, chunks;
+};
+
+// One wave joins 64 * N * U columns of a token's rows: the loads of four slots before their sums.
+template <int DT, int N, int U>
+__global__ __launch_bounds__(256) void combine_kernel(CombineArgs p) {
+  using T = typename Stored<DT>::type;
+  const int lane = threadIdx.x % kWave;
+  const int64_t id = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+  const int t = (int)(id / p.chunks), chunk = (int)(id % p.chunks);
+  if (t >= p.m) return;
+  const int col = chunk * (kWave * N * U) + lane * N;
+  const T *in = static_cast<const T *>(p.in);
+  float acc[U][N] = {};
+  const int32_t *rows = p.rows + (int64_t)t * p.k;
+  const float *weights = p.weights != nullptr ? p.weights + (int64_t)t * p.k : nullptr;
+  constexpr int kAhead = 4;
+  for (int j0 = 0; j0 < p.k; j0 += kAhead) {
+    float v[kAhead][U][N], w[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int row = j0 + j < p.k ? __builtin_amdgcn_readfirstlane(rows[j0 + j]) : -1;
+      const bool there = (uint32_t)row < (uint32_t)p.places;
+      w[j] = !there ? 0.0f : weights != nullptr ? weights[j0 + j] : 1.0f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int at = col + u * kWave * N;
+        // a row that is not there adds nothing, whatever its weight: zeros times 0
+        load_row<DT, N>(in + (there ? row : 0) * p.in_stride + at, there ? p.width - at : 0, 0.0f, v[j][u]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[u][i] = fmaf(w[j], v[j][u][i], acc[u][i]);
+  }
+  T *out = static_cast<T *>(p.out) + t * p.out_stride;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int at = col + u * kWave * N;
+    store_row<DT, N>(out + at, p.width - at, acc[u]);
+  }
+}
+
+struct CombineGradArgs {
+  const void *dout, *y;
+  int64_t dout_stride, y_stride, dy_stride;
+  const int32_t *rows, *ends;
+  const float *weights;
+  void *dy;
+  float *dweights;
+  int groups, m, k, width;
+};
+
+// dy[rows[t,j]] = w_tj dout[t], dw_tj = <dout[t], y[rows[t,j]]>; places behind the last end get zeros.
+// W waves go through a token's row together, K slots at a time: dout is read once for them.
+template <int DT, int N, int W, int K>
+__global__ __launch_bounds__(256) void combine_gradient_kernel(CombineGradArgs p) {
+  using T = typename Stored<DT>::type;
+  __shared__ float parts[4][K];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int64_t id = (int64_t)blockIdx.x * (4 / W) + (W == 1 ? wave : 0);
+  if (W == 1 && id >= p.m) return;
+  const int t = (int)id, slots = p.m * p.k;
+  const int used = p.groups > 0 ? clamp_end(p.ends[p.groups - 1], slots) : 0;
+  const T *dout = static_cast<const T *>(p.dout) + t * p.dout_stride;
+  const T *y = static_cast<const T *>(p.y);
+  T *dy = static_cast<T *>(p.dy);
+  const int first = (W == 1 ? 0 : wave) * kWave * N + lane * N;
+  for (int j0 = 0; j0 < p.k; j0 += K) {
+    int row[K];
+    float w[K], dot[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      const int64_t at = (int64_t)t * p.k + (j0 + j < p.k ? j0 + j : 0);
+      row[j] = __builtin_amdgcn_readfirstlane(p.rows[at]);
+      if (j0 + j >= p.k || (uint32_t)row[j] >= (uint32_t)used) row[j] = -1;
+      w[j] = p.weights != nullptr ? p.weights[at] : 1.0f;
+      dot[j] = 0.0f;
+    }
+    for (int at = first; at < p.width; at += W * kWave * N) {
+      const int valid = p.width - at;
+      float d[N], v[K][N];
+      load_row<DT, N>(dout + at, valid, 0.0f, d);
+      if (p.dweights != nullptr) {
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+          if (row[j] >= 0) load_row<DT, N>(y + row[j] * p.y_stride + at, valid, 0.0f, v[j]);
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+          if (row[j] >= 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) dot[j] = fmaf(d[i], v[j][i], dot[j]);
+          }
+      }
+      if (dy != nullptr) {
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+          if (row[j] >= 0) {
+            float s[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) s[i] = w[j] * d[i];
+            store_row<DT, N>(dy + row[j] * p.dy_stride + at, valid, s);
+          }
+          const int slot = t * p.k + j0 + j;
+          if (j0 + j < p.k && slot >= used) {
+            const float zero[N] = {};
+            store_row<DT, N>(dy + slot * p.dy_stride + at, valid, zero);
+          }
+        }
+      }
+    }
+    if (p.dweights == nullptr) continue;
+#pragma unroll
+    for (int j = 0; j < K; ++j) dot[j] = sum_across<kWave>(dot[j]);
+    if constexpr (W > 1) {
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+        if (lane == 0) parts[wave][j] = dot[j];
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < K; ++j) dot[j] = ((parts[0][j] + parts[1][j]) + parts[2][j]) + parts[3][j];
+      __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+      if (threadIdx.x % (W * kWave) == 0 && j0 + j < p.k)
+        p.dweights[(int64_t)t * p.k + j0 + j] = row[j] >= 0 ? dot[j] : 0.0f;
+  }
+}
+
+// ---- arguments -----------------------------------------------------------------------
+
+constexpr int64_t kMaxPitch = int64_t(1) << 26;
+constexpr int64_t kMaxBytes = int64_t(1) << 42;
+constexpr int64_t kMaxDim = int64_t(1) << 30;
+
+bool aligned_to(const void *p, uintptr_t bytes) {
+  return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0;
+}
+
+bool is_type(hadacore_dtype t) {
+  return t == HADACORE_FP16 || t == HADACORE_BF16 || t == HADACORE_FP32;
+}
+
+int64_t size_of(hadacore_dtype t) { return t == HADACORE_FP32 ? 4 : 2; }
+
+hadacore_status status_of(hipError_t e) {
+  return e == hipSuccess ? HADACORE_SUCCESS : HADACORE_ERROR_LAUNCH;
+}
+
+// A matrix of `rows` rows: its stride, size and address.
+hadacore_status check_rows(const void *p, int64_t rows, int64_t pitch, int64_t width, int64_t size) {
+  if (pitch < width || pitch > kMaxPitch) return HADACORE_ERROR_INVALID_STRIDE;
+  if (rows == 0 || width == 0) return HADACORE_SUCCESS;
+  if (pitch > kMaxBytes / rows) return HADACORE_ERROR_TOO_LARGE;
+  if (p == nullptr) return HADACORE_ERROR_INVALID_VALUE;
+  return aligned_to(p, size) ? HADACORE_SUCCESS : HADACORE_ERROR_MISALIGNED;
+}
+
+// An array of `n` values of 4 bytes that has to be there where n > 0.
+hadacore_status check_words(const void *p, int64_t n) {
+  if (n > 0 && p == nullptr) return HADACORE_ERROR_INVALID_VALUE;
+  return aligned_to(p, 4) ? HADACORE_SUCCESS : HADACORE_ERROR_MISALIGNED;
+}
+
+template <int N>
+hadacore_status first_error(const hadacore_status (&st)[N]) {
+  for (hadacore_status s : st)
+    if (s != HADACORE_SUCCESS) return s;
+  return HADACORE_SUCCESS;
+}
+
+// Whether one of the outputs overlaps another or an input.
+template <int O, int I>
+bool any_overlap(const Span (&out)[O], const Span (&in)[I]) {
+  for (int i = 0; i < O; ++i) {
+    for (int j = 0; j < i; ++j)
+      if (spans_overlap(out[i], out[j])) return true;
+    for (const Span &s : in)
+      if (spans_overlap(out[i], s)) return true;
+  }
+  return false;
+}
+
+Span words(const void *p, int64_t n) { return span(p, p != nullptr, n, n, 4); }
+
+hadacore_status check_choices(int64_t m, int64_t experts, int64_t k, hadacore_dtype dtype) {
+  if (m < 0) return HADACORE_ERROR_INVALID_VALUE;
+  if (experts < 1 || experts > kMaxExperts || k < 1 || k > experts || k > kMaxChoices)
+    return HADACORE_ERROR_INVALID_SIZE;
+  if (!is_type(dtype)) return HADACORE_ERROR_INVALID_DTYPE;
+  return m * k >= kMaxDim || m >= kMaxDim ? HADACORE_ERROR_TOO_LARGE : HADACORE_SUCCESS;
+}
+
+// Tokens, choices and columns of the exchange.
+hadacore_status check_exchange(int64_t m, int64_t k, int64_t width, int64_t groups) {
+  if (m < 0 || k < 1 || width < 0 || groups < 0) return HADACORE_ERROR_INVALID_VALUE;
+  if (m >= kMaxDim || k >= kMaxDim || m * k >= kMaxDim || width > kMaxPitch || groups >= kMaxDim)
+    return HADACORE_ERROR_TOO_LARGE;
+  return HADACORE_SUCCESS;
+}
+
+}  // namespace
+}  // namespace hadacore
+
+using namespace hadacore;
+
+extern "C" int64_t hadacore_route_workspace_size(int64_t m, int64_t experts) {
+  if (m < 0 || m >= kMaxDim || experts < 1 || experts > kMaxExperts) return 0;
+  return route_parts(m, experts) * (2 * experts + 1) * 4;
+}
+
+extern "C" hadacore_status hadacore_route(const void *logits, int64_t logits_row_stride,
+                                          hadacore_dtype dtype, const uint8_t *valid, int64_t m,
+                                          int64_t experts, int64_t k, int32_t renormalize,
+                                          int32_t *out_experts, float *out_weights,
+                                          int32_t *out_counts, float *out_loss, float *out_slopes,
+                                          void *workspace, int64_t workspace_bytes, void *stream) {
+  hadacore_status st = check_choices(m, experts, k, dtype);
+  if (st != HADACORE_SUCCESS) return st;
+  st = check_rows(logits, m, logits_row_stride, experts, size_of(dtype));
+  if (st != HADACORE_SUCCESS) return st;
+  st = first_error({check_words(out_experts, m * k), check_words(out_weights, m * k),
+                    check_words(out_counts, experts), check_words(out_loss, 1),
+                    check_words(out_slopes, experts)});
+  if (st != HADACORE_SUCCESS) return st;
+  const int64_t need = hadacore_route_workspace_size(m, experts);
+  if (workspace == nullptr || workspace_bytes < need) return HADACORE_ERROR_WORKSPACE;
+  if (!aligned_to(workspace, 4)) return HADACORE_ERROR_MISALIGNED;
+  if (any_overlap({words(out_experts, m * k), words(out_weights, m * k), words(out_counts, experts),
+                   words(out_loss, 1), words(out_slopes, experts), span(workspace, 1, need, need, 1)},
+                  {span(logits, m, logits_row_stride, experts, size_of(dtype)),
+                   span(valid, valid != nullptr, m, m, 1)}))
+    return HADACORE_ERROR_OVERLAP;
+  st = check_device();
+  if (st != HADACORE_SUCCESS) return st;
+  const int64_t parts = route_parts(m, experts);
+  RouteArgs p{};
+  p.logits = logits;
+  p.stride = logits_row_stride;
+  p.valid = valid;
+  p.m = (int)m;
+  p.experts = (int)experts;
+  p.k = (int)k;
+  p.renormalize = renormalize != 0;
+  p.chosen = out_experts;
+  p.weights = out_weights;
+  p.counts = out_counts;
+  p.loss = out_loss;
+  p.slopes = out_slopes;
+  p.part_p = static_cast<float *>(workspace);
+  p.part_counts = static_cast<int32_t *>(workspace) + parts * experts;
+  p.part_tokens = p.part_counts + parts * experts;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  for_type(dtype, [&](auto dt) {
+    for_experts(experts, [&](auto l, auto v) {
+      hipLaunchKernelGGL((route_kernel<decltype(dt)::value, decltype(l)::value, decltype(v)::value>),
+                         dim3((uint32_t)parts), dim3(kRouteThreads), 0, s, p);
+    });
+  });
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && parts > 1) {
+    hipLaunchKernelGGL(join_routes_kernel, dim3(1), dim3(kRouteThreads), 0, s, p, (int)parts);
+    e = hipGetLastError();
+  }
+  return status_of(e);
+}
+
+extern "C" hadacore_status hadacore_route_gradient(
+    const void *logits, int64_t logits_row_stride, hadacore_dtype dtype, const int32_t *chosen,
+    const float *weights, const float *slopes, const float *dweights, const float *dloss, int64_t m,
+    int64_t experts, int64_t k, int32_t renormalize, void *out, int64_t out_row_stride,
+    void *stream) {
+  hadacore_status st = check_choices(m, experts, k, dtype);
+  if (st != HADACORE_SUCCESS) return st;
+  const int64_t size = size_of(dtype);
+  st = first_error({check_rows(logits, m, logits_row_stride, experts, size),
+                    check_rows(out, m, out_row_stride, experts, size)});
+  if (st != HADACORE_SUCCESS || m == 0) return st;
+  st = first_error({check_words(chosen, m * k), check_words(weights, dweights != nullptr ? m * k : 0),
+                    check_words(slopes, dloss != nullptr ? experts : 0), check_words(dweights, 0),
+                    check_words(dloss, 0)});
+  if (st != HADACORE_SUCCESS) return st;
+  if (any_overlap({span(out, m, out_row_stride, experts, size)},
+                  {span(logits, m, logits_row_stride, experts, size), words(chosen, m * k),
+                   words(weights, m * k), words(slopes, experts), words(dweights, m * k),
+                   words(dloss, 1)}))
+    return HADACORE_ERROR_OVERLAP;
+  st = check_device();
+  if (st != HADACORE_SUCCESS) return st;
+  RouteGradArgs p{};
+  p.logits = logits;
+  p.stride = logits_row_stride;
+  p.chosen = chosen;
+  p.weights = weights;
+  p.slopes = slopes;
+  p.dweights = dweights;
+  p.dloss = dloss;
+  p.m = (int)m;
+  p.experts = (int)experts;
+  p.k = (int)k;
+  p.renormalize = renormalize != 0;
+  p.out = out;
+  p.out_stride = out_row_stride;
+  for_type(dtype, [&](auto dt) {
+    for_experts(experts, [&](auto l, auto v) {
+      constexpr int kRows = 256 / decltype(l)::value;
+      const int64_t blocks = (m + kRows - 1) / kRows, most = (int64_t)device_cus() * 8;
+      hipLaunchKernelGGL(
+          (route_gradient_kernel<decltype(dt)::value, decltype(l)::value, decltype(v)::value>),
+          dim3((uint32_t)(blocks < most ? blocks : most)), dim3(256), 0,
+          static_cast<hipStream_t>(stream), p);
+    });
+  });
+  return status_of(hipGetLastError());
+}
+
+extern "C" int64_t hadacore_group_workspace_size(int64_t slots, int64_t groups) {
+  if (slots < 0 || slots >= kMaxDim || groups < 0 || groups > HADACORE_MAX_GROUPS) return 0;
+  const int64_t blocks = group_blocks_of(slots, groups);
+  return blocks > 1 ? blocks * (groups + 1) * 4 : 0;
+}
+
+extern "C" hadacore_status hadacore_group_tokens(const int32_t *ids, int64_t slots, int64_t groups,
+                                                 int32_t *out_ends, int32_t *out_rows,
+                                                 int32_t *out_slots, void *workspace,
+                                                 int64_t workspace_bytes, void *stream) {
+  if (slots < 0 || groups < 0) return HADACORE_ERROR_INVALID_VALUE;
+  if (groups > HADACORE_MAX_GROUPS) return HADACORE_ERROR_INVALID_SIZE;
+  if (slots >= kMaxDim) return HADACORE_ERROR_TOO_LARGE;
+  hadacore_status st = first_error({check_words(ids, slots), check_words(out_ends, groups),
+                                    check_words(out_rows, slots), check_words(out_slots, slots)});
+  if (st != HADACORE_SUCCESS) return st;
+  const int64_t need = hadacore_group_workspace_size(slots, groups);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return HADACORE_ERROR_WORKSPACE;
+  if (!aligned_to(workspace, 4)) return HADACORE_ERROR_MISALIGNED;
+  if (any_overlap({words(out_ends, groups), words(out_rows, slots), words(out_slots, slots),
+                   span(workspace, need > 0, need, need, 1)},
+                  {words(ids, slots)}))
+    return HADACORE_ERROR_OVERLAP;
+  if (groups == 0 && slots == 0) return HADACORE_SUCCESS;
+  st = check_device();
+  if (st != HADACORE_SUCCESS) return st;
+  const int64_t blocks = group_blocks_of(slots, groups);
+  const int waves = group_waves(groups);
+  GroupArgs p{};
+  p.ids = ids;
+  p.slots = (int)slots;
+  p.groups = (int)groups;
+  p.ends = out_ends;
+  p.rows = out_rows;
+  p.order = out_slots;
+  p.parts = static_cast<int32_t *>(workspace);
+  const int64_t unit = kWave * waves;
+  p.per_block = (int)(((slots + blocks - 1) / blocks + unit - 1) / unit * unit);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const size_t bins = (size_t)(groups + 1) * 4;
+  if (blocks > 1) {
+    hipLaunchKernelGGL(count_groups_kernel, dim3((uint32_t)blocks), dim3(kGroupThreads), bins, s, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return status_of(e);
+  }
+  if (waves == 16)
+    hipLaunchKernelGGL(place_groups_kernel<16>, dim3((uint32_t)blocks), dim3(kGroupThreads),
+                       17 * bins, s, p);
+  else if (waves == 4)
+    hipLaunchKernelGGL(place_groups_kernel<4>, dim3((uint32_t)blocks), dim3(kGroupThreads), 5 * bins,
+                       s, p);
+  else
+    hipLaunchKernelGGL(place_groups_kernel<2>, dim3((uint32_t)blocks), dim3(kGroupThreads), 3 * bins,
+                       s, p);
+  return status_of(hipGetLastError());
+}
+
+extern "C" hadacore_status hadacore_dispatch_rows(const void *in, int64_t in_row_stride,
+                                                  int32_t value_bytes, const int32_t *rows,
+                                                  const int32_t *ends, int64_t groups, void *out,
+                                                  int64_t out_row_stride, int64_t m, int64_t k,
+                                                  int64_t width, void *stream) {
+  hadacore_status st = check_exchange(m, k, width, groups);
+  if (st != HADACORE_SUCCESS) return st;
+  if (value_bytes != 1 && value_bytes != 2 && value_bytes != 4) return HADACORE_ERROR_INVALID_DTYPE;
+  st = first_error({check_rows(in, m, in_row_stride, width, value_bytes),
+                    check_rows(out, m * k, out_row_stride, width, value_bytes),
+                    check_words(rows, m * k), check_words(ends, groups)});
+  if (st != HADACORE_SUCCESS || m == 0 || width == 0) return st;
+  if (any_overlap({span(out, m * k, out_row_stride, width, value_bytes)},
+                  {span(in, m, in_row_stride, width, value_bytes), words(rows, m * k),
+                   words(ends, groups)}))
+    return HADACORE_ERROR_OVERLAP;
+  DispatchArgs p{};
+  p.in = static_cast<const uint8_t *>(in);
+  p.in_stride = in_row_stride * value_bytes;
+  p.out_stride = out_row_stride * value_bytes;
+  p.rows = rows;
+  p.ends = ends;
+  p.out = static_cast<uint8_t *>(out);
+  p.m = (int)m;
+  p.k = (int)k;
+  p.groups = (int)groups;
+  p.bytes = (int)(width * value_bytes);
+  p.size = value_bytes;
+  p.chunks = (p.bytes + kDispatchChunk - 1) / kDispatchChunk;
+  const int64_t blocks = (m * p.chunks + 3) / 4;
+  if (blocks * 256 >= (int64_t(1) << 32)) return HADACORE_ERROR_TOO_LARGE;
+  st = check_device();
+  if (st != HADACORE_SUCCESS) return st;
+  hipLaunchKernelGGL(dispatch_kernel, dim3((uint32_t)blocks), dim3(256), 0,
+                     static_cast<hipStream_t>(stream), p);
+  return status_of(hipGetLastError());
+}
+
+extern "C" hadacore_status hadacore_combine_rows(const void *in, int64_t in_row_stride,
+                                                 int64_t places, hadacore_dtype dtype,
+                                                 const int32_t *rows, const float *weights,
+                                                 void *out, int64_t out_row_stride, int64_t m,
+                                                 int64_t k, int64_t width, void *stream) {
+  hadacore_status st = check_exchange(m, k, width, 0);
+  if (st != HADACORE_SUCCESS) return st;
+  if (places < 0) return HADACORE_ERROR_INVALID_VALUE;
+  if (!is_type(dtype)) return HADACORE_ERROR_INVALID_DTYPE;
+  if (places >= kMaxDim) return HADACORE_ERROR_TOO_LARGE;
+  const int64_t size = size_of(dtype);
+  st = first_error({check_rows(in, places, in_row_stride, width, size),
+                    check_rows(out, m, out_row_stride, width, size), check_words(rows, m * k),
+                    check_words(weights, 0)});
+  if (st != HADACORE_SUCCESS || m == 0 || width == 0) return st;
+  if (any_overlap({span(out, m, out_row_stride, width, size)},
+                  {span(in, places, in_row_stride, width, size), words(rows, m * k),
+                   words(weights, m * k)}))
+    return HADACORE_ERROR_OVERLAP;
+  CombineArgs p{};
+  p.in = in;
+  p.in_stride = in_row_stride;
+  p.out_stride = out_row_stride;
+  p.rows = rows;
+  p.weights = weights;
+  p.out = out;
+  p.places = (int)places;
+  p.m = (int)m;
+  p.k = (int)k;
+  p.width = (int)width;
+  hadacore_status result = HADACORE_SUCCESS;
+  for_type(dtype, [&](auto dt) {
+    constexpr int DT = decltype(dt)::value, N = DT == HADACORE_FP32 ? 4 : 8, U = 1;
+    p.chunks = (p.width + kWave * N * U - 1) / (kWave * N * U);
+    const int64_t blocks = (m * p.chunks + 3) / 4;
+    if (blocks * 256 >= (int64_t(1) << 32)) {
+      result = HADACORE_ERROR_TOO_LARGE;
+      return;
+    }
+    result = check_device();
+    if (result != HADACORE_SUCCESS) return;
+    hipLaunchKernelGGL((combine_kernel<DT, N, U>), dim3((uint32_t)blocks), dim3(256), 0,
+                       static_cast<hipStream_t>(stream), p);
+    result = status_of(hipGetLastError());
+  });
+  return result;
+}
+
+extern "C" hadacore_status hadacore_combine_gradient(
+    const void *dout, int64_t dout_row_stride, const void *y, int64_t y_row_stride,
+    hadacore_dtype dtype, const int32_t *rows, const int32_t *ends, int64_t groups,
+    const float *weights, void *dy, int64_t dy_row_stride, float *dweights, int64_t m, int64_t k,
+    int64_t width, void *stream) {
+  hadacore_status st = check_exchange(m, k, width, groups);
+  if (st != HADACORE_SUCCESS) return st;
+  if (!is_type(dtype)) return HADACORE_ERROR_INVALID_DTYPE;
+  const int64_t size = size_of(dtype);
+  const bool want_w = dweights != nullptr, want_y = dy != nullptr;
+  st = first_error({check_rows(dout, m, dout_row_stride, width, size), check_words(rows, m * k),
+                    check_words(ends, groups), check_words(weights, 0), check_words(dweights, 0)});
+  if (st == HADACORE_SUCCESS && want_w) st = check_rows(y, m * k, y_row_stride, width, size);
+  if (st == HADACORE_SUCCESS && want_y) st = check_rows(dy, m * k, dy_row_stride, width, size);
+  if (st != HADACORE_SUCCESS || m == 0 || (!want_w && !want_y)) return st;
+  if (any_overlap({span(dy, want_y ? m * k : 0, dy_row_stride, width, size), words(dweights, m * k)},
+                  {span(dout, m, dout_row_stride, width, size),
+                   span(y, want_w ? m * k : 0, y_row_stride, width, size), words(rows, m * k),
+                   words(ends, groups), words(weights, m * k)}))
+    return HADACORE_ERROR_OVERLAP;
+  CombineGradArgs p{};
+  p.dout = dout;
+  p.y = y;
+  p.dout_stride = dout_row_stride;
+  p.y_stride = y_row_stride;
+  p.dy_stride = dy_row_stride;
+  p.rows = rows;
+  p.ends = ends;
+  p.weights = weights;
+  p.dy = dy;
+  p.dweights = dweights;
+  p.groups = (int)groups;
+  p.m = (int)m;
+  p.k = (int)k;
+  p.width = (int)width;
+  if (m * 256 >= (int64_t(1) << 32)) return HADACORE_ERROR_TOO_LARGE;
+  st = check_device();
+  if (st != HADACORE_SUCCESS) return st;
+  for_type(dtype, [&](auto dt) {
+    constexpr int DT = decltype(dt)::value, N = DT == HADACORE_FP32 ? 4 : 8;
+    const auto go = [&](auto waves, auto slots) {
+      constexpr int W = decltype(waves)::value;
+      hipLaunchKernelGGL((combine_gradient_kernel<DT, N, W, decltype(slots)::value>),
+                         dim3((uint32_t)((m * W + 3) / 4)), dim3(256), 0,
+                         static_cast<hipStream_t>(stream), p);
+    };
+    const auto by_slots = [&](auto waves) {
+      if (k == 1)
+        go(waves, std::integral_constant<int, 1>{});
+      else if (k == 2)
+        go(waves, std::integral_constant<int, 2>{});
+      else
+        go(waves, std::integral_constant<int, 4>{});
+    };
+    if (width <= kWave * N)
+      by_slots(std::integral_constant<int, 1>{});
+    else
+      by_slots(std::integral_constant<int, 4>{});
+  });
+  return status_of(hipGetLastError());
+}

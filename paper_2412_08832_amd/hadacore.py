@@ -9,24 +9,31 @@ The raw entry points take device addresses as integers and keep the C names:
 ``hadamard_transform_ws_noalloc``, ``hadamard_transform_workspace_size``, ``hadamard_transform_fp8``,
 ``hadamard_transform_int8``, ``hadamard_transform_fp8_blocks``, ``hadacore_padded_tokens``,
 ``hadacore_quantize_fp8_columns``, ``hadacore_quantize_fp8_tiles``, ``hadacore_matmul_fp8``,
-``hadacore_matmul_fp8_grouped``, ``hadacore_weight_gradient_fp8_grouped``,
+``hadacore_matmul_fp8_grouped``, ``hadacore_weight_gradient_fp8_grouped``, ``hadacore_route``,
+``hadacore_route_gradient``, ``hadacore_group_tokens``, ``hadacore_dispatch_rows``,
+``hadacore_combine_rows``, ``hadacore_combine_gradient``, ``hadacore_adapters``,
+``hadacore_adapter_gradient`` and their ``*_workspace_size``,
 ``hadacore_stream_copy``, ``hadacore_status_string``, ``hadacore_version``.  ``transform``,
 ``transform_fp8`` and ``transform_int8`` are convenience wrappers for 2-D torch tensors on a
 ROCm device, and so are, for codes with a scale per block of 128, ``transform_fp8_blocks``,
 ``quantize_fp8_columns``, ``quantize_fp8_tiles``, ``matmul_fp8``, ``grouped_matmul_fp8`` and
-``grouped_weight_gradient_fp8``.
+``grouped_weight_gradient_fp8``; for tokens and weights of their own ``route_tokens``,
+``route_tokens_gradient``, ``group_tokens``, ``dispatch_rows``, ``combine_rows``,
+``combine_rows_gradient``, ``adapt_rows`` and ``adapter_gradient``.
 """
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 from pathlib import Path
+from typing import NamedTuple
 
 LIBRARY = Path(__file__).resolve().parent / "libhadacore.so"
 
 FP16 = 0
 BF16 = 1
-FP32 = 2  # output of the FP8 products only
+FP32 = 2  # outputs of the FP8 products; logits, exchange, adapters
 BLOCK = 128  # values that share a scale in the block quantizers and the products
 SUCCESS = 0
 STATUS_NAMES = {
@@ -40,6 +47,10 @@ EXPORTS = ("hadamard_transform", "hadamard_transform_strided", "hadamard_transfo
            "hadamard_transform_int8", "hadamard_transform_fp8_blocks", "hadacore_padded_tokens",
            "hadacore_quantize_fp8_columns", "hadacore_quantize_fp8_tiles", "hadacore_matmul_fp8",
            "hadacore_matmul_fp8_grouped", "hadacore_weight_gradient_fp8_grouped",
+           "hadacore_route_workspace_size", "hadacore_route", "hadacore_route_gradient",
+           "hadacore_group_workspace_size", "hadacore_group_tokens", "hadacore_dispatch_rows",
+           "hadacore_combine_rows", "hadacore_combine_gradient", "hadacore_adapters_workspace_size",
+           "hadacore_adapters", "hadacore_adapter_gradient_workspace_size", "hadacore_adapter_gradient",
            "hadacore_stream_copy", "hadacore_status_string", "hadacore_version")
 
 
@@ -114,6 +125,36 @@ def library() -> ctypes.CDLL:
                                                              i64, vp, i64, i64, i32, i64, i64, i64,
                                                              vp]
         lib.hadacore_weight_gradient_fp8_grouped.restype = i32
+        lib.hadacore_route_workspace_size.argtypes = [i64, i64]
+        lib.hadacore_route_workspace_size.restype = i64
+        lib.hadacore_route.argtypes = [vp, i64, i32, vp, i64, i64, i64, i32, vp, vp, vp, vp, vp, vp,
+                                       i64, vp]
+        lib.hadacore_route.restype = i32
+        lib.hadacore_route_gradient.argtypes = [vp, i64, i32, vp, vp, vp, vp, vp, i64, i64, i64, i32,
+                                                vp, i64, vp]
+        lib.hadacore_route_gradient.restype = i32
+        lib.hadacore_group_workspace_size.argtypes = [i64, i64]
+        lib.hadacore_group_workspace_size.restype = i64
+        lib.hadacore_group_tokens.argtypes = [vp, i64, i64, vp, vp, vp, vp, i64, vp]
+        lib.hadacore_group_tokens.restype = i32
+        lib.hadacore_dispatch_rows.argtypes = [vp, i64, i32, vp, vp, i64, vp, i64, i64, i64, i64, vp]
+        lib.hadacore_dispatch_rows.restype = i32
+        lib.hadacore_combine_rows.argtypes = [vp, i64, i64, i32, vp, vp, vp, i64, i64, i64, i64, vp]
+        lib.hadacore_combine_rows.restype = i32
+        lib.hadacore_combine_gradient.argtypes = [vp, i64, vp, i64, i32, vp, vp, i64, vp, vp, i64, vp,
+                                                  i64, i64, i64, vp]
+        lib.hadacore_combine_gradient.restype = i32
+        lib.hadacore_adapters_workspace_size.argtypes = [i64, i64, i64, i64, i64]
+        lib.hadacore_adapters_workspace_size.restype = i64
+        lib.hadacore_adapters.argtypes = [vp, i64, vp, i64, i64, vp, i64, i64, vp, vp, vp, i64, vp,
+                                          i64, vp, i64, i32, i32, vp, i64, i64, i64, i64, i64, vp,
+                                          i64, vp]
+        lib.hadacore_adapters.restype = i32
+        lib.hadacore_adapter_gradient_workspace_size.argtypes = [i64, i64, i64, i64]
+        lib.hadacore_adapter_gradient_workspace_size.restype = i64
+        lib.hadacore_adapter_gradient.argtypes = [vp, i64, vp, i64, i32, vp, vp, vp, i64, vp, i64, i64,
+                                                  i32, i64, i64, i64, vp, i64, vp]
+        lib.hadacore_adapter_gradient.restype = i32
         lib.hadacore_stream_copy.argtypes = [vp, vp, i64, vp]
         lib.hadacore_stream_copy.restype = i32
         lib.hadacore_status_string.argtypes = [i32]
@@ -276,6 +317,120 @@ def hadacore_weight_gradient_fp8_grouped(a_ptr: int, a_row_stride: int, a_scales
         out_dtype, places, n, k, stream)
     if check:
         _check(st, "hadacore_weight_gradient_fp8_grouped")
+    return st
+
+
+def hadacore_route_workspace_size(m: int, experts: int) -> int:
+    return int(library().hadacore_route_workspace_size(m, experts))
+
+
+def hadacore_route(logits_ptr: int, logits_row_stride: int, dtype: int, valid_ptr: int, m: int,
+                   experts: int, k: int, renormalize: int, experts_ptr: int, weights_ptr: int,
+                   counts_ptr: int, loss_ptr: int, slopes_ptr: int, workspace_ptr: int,
+                   workspace_bytes: int, stream: int = 0, check: bool = True) -> int:
+    st = library().hadacore_route(logits_ptr, logits_row_stride, dtype, valid_ptr, m, experts, k,
+                                  renormalize, experts_ptr, weights_ptr, counts_ptr, loss_ptr,
+                                  slopes_ptr, workspace_ptr, workspace_bytes, stream)
+    if check:
+        _check(st, "hadacore_route")
+    return st
+
+
+def hadacore_route_gradient(logits_ptr: int, logits_row_stride: int, dtype: int, chosen_ptr: int,
+                            weights_ptr: int, slopes_ptr: int, dweights_ptr: int, dloss_ptr: int,
+                            m: int, experts: int, k: int, renormalize: int, out_ptr: int,
+                            out_row_stride: int, stream: int = 0, check: bool = True) -> int:
+    st = library().hadacore_route_gradient(logits_ptr, logits_row_stride, dtype, chosen_ptr,
+                                           weights_ptr, slopes_ptr, dweights_ptr, dloss_ptr, m,
+                                           experts, k, renormalize, out_ptr, out_row_stride, stream)
+    if check:
+        _check(st, "hadacore_route_gradient")
+    return st
+
+
+def hadacore_group_workspace_size(slots: int, groups: int) -> int:
+    return int(library().hadacore_group_workspace_size(slots, groups))
+
+
+def hadacore_group_tokens(ids_ptr: int, slots: int, groups: int, ends_ptr: int, rows_ptr: int,
+                          slots_ptr: int, workspace_ptr: int, workspace_bytes: int, stream: int = 0,
+                          check: bool = True) -> int:
+    st = library().hadacore_group_tokens(ids_ptr, slots, groups, ends_ptr, rows_ptr, slots_ptr,
+                                         workspace_ptr, workspace_bytes, stream)
+    if check:
+        _check(st, "hadacore_group_tokens")
+    return st
+
+
+def hadacore_dispatch_rows(in_ptr: int, in_row_stride: int, value_bytes: int, rows_ptr: int,
+                           ends_ptr: int, groups: int, out_ptr: int, out_row_stride: int, m: int,
+                           k: int, width: int, stream: int = 0, check: bool = True) -> int:
+    st = library().hadacore_dispatch_rows(in_ptr, in_row_stride, value_bytes, rows_ptr, ends_ptr,
+                                          groups, out_ptr, out_row_stride, m, k, width, stream)
+    if check:
+        _check(st, "hadacore_dispatch_rows")
+    return st
+
+
+def hadacore_combine_rows(in_ptr: int, in_row_stride: int, places: int, dtype: int, rows_ptr: int,
+                          weights_ptr: int, out_ptr: int, out_row_stride: int, m: int, k: int,
+                          width: int, stream: int = 0, check: bool = True) -> int:
+    st = library().hadacore_combine_rows(in_ptr, in_row_stride, places, dtype, rows_ptr, weights_ptr,
+                                         out_ptr, out_row_stride, m, k, width, stream)
+    if check:
+        _check(st, "hadacore_combine_rows")
+    return st
+
+
+def hadacore_combine_gradient(dout_ptr: int, dout_row_stride: int, y_ptr: int, y_row_stride: int,
+                              dtype: int, rows_ptr: int, ends_ptr: int, groups: int,
+                              weights_ptr: int, dy_ptr: int, dy_row_stride: int, dweights_ptr: int,
+                              m: int, k: int, width: int, stream: int = 0,
+                              check: bool = True) -> int:
+    st = library().hadacore_combine_gradient(dout_ptr, dout_row_stride, y_ptr, y_row_stride, dtype,
+                                             rows_ptr, ends_ptr, groups, weights_ptr, dy_ptr,
+                                             dy_row_stride, dweights_ptr, m, k, width, stream)
+    if check:
+        _check(st, "hadacore_combine_gradient")
+    return st
+
+
+def hadacore_adapters_workspace_size(m: int, k: int, n: int, rank: int, groups: int) -> int:
+    return int(library().hadacore_adapters_workspace_size(m, k, n, rank, groups))
+
+
+def hadacore_adapters(x_ptr: int, x_row_stride: int, down_ptr: int, down_row_stride: int,
+                      down_batch_stride: int, up_ptr: int, up_row_stride: int, up_batch_stride: int,
+                      scales_ptr: int, ends_ptr: int, slots_ptr: int, groups: int, y_ptr: int,
+                      y_row_stride: int, out_ptr: int, out_row_stride: int, dtype: int,
+                      out_dtype: int, hidden_ptr: int, hidden_row_stride: int, m: int, k: int, n: int,
+                      rank: int, workspace_ptr: int, workspace_bytes: int, stream: int = 0,
+                      check: bool = True) -> int:
+    st = library().hadacore_adapters(
+        x_ptr, x_row_stride, down_ptr, down_row_stride, down_batch_stride, up_ptr, up_row_stride,
+        up_batch_stride, scales_ptr, ends_ptr, slots_ptr, groups, y_ptr, y_row_stride, out_ptr,
+        out_row_stride, dtype, out_dtype, hidden_ptr, hidden_row_stride, m, k, n, rank,
+        workspace_ptr, workspace_bytes, stream)
+    if check:
+        _check(st, "hadacore_adapters")
+    return st
+
+
+def hadacore_adapter_gradient_workspace_size(m: int, width: int, rank: int, groups: int) -> int:
+    return int(library().hadacore_adapter_gradient_workspace_size(m, width, rank, groups))
+
+
+def hadacore_adapter_gradient(hidden_ptr: int, hidden_row_stride: int, x_ptr: int, x_row_stride: int,
+                              dtype: int, scales_ptr: int, ends_ptr: int, slots_ptr: int, groups: int,
+                              out_ptr: int, out_row_stride: int, out_batch_stride: int,
+                              out_dtype: int, m: int, width: int, rank: int, workspace_ptr: int,
+                              workspace_bytes: int, stream: int = 0, check: bool = True) -> int:
+    st = library().hadacore_adapter_gradient(
+        hidden_ptr, hidden_row_stride, x_ptr, x_row_stride, dtype, scales_ptr, ends_ptr, slots_ptr,
+        groups, out_ptr, out_row_stride, out_batch_stride, out_dtype, m, width, rank, workspace_ptr,
+        workspace_bytes, stream)
+    if check:
+        _check(st, "hadacore_adapter_gradient")
     return st
 
 
@@ -754,4 +909,359 @@ def grouped_weight_gradient_fp8(dy, dy_scales, x, x_scales, ends=None, out=None,
           dy_scales.data_ptr(), sdy_stride, x.data_ptr(), x_stride, x_scales.data_ptr(), sx_stride,
           ends_ptr, groups, out.data_ptr(), out_stride, out.stride(0) if groups > 1 else 0, code,
           places, n, k, _stream_of(stream, device))
+    return out
+
+
+# ---- tokens and weights of their own: routing, the exchange by expert, adapters ----------
+
+
+class Routes(NamedTuple):
+    """What ``route_tokens`` gives: the experts of each token (m x k, -1: none), their weights
+    (m x k), how many tokens each expert got, the balance loss (a scalar), and its derivative to
+    each token's probability of an expert."""
+    experts: "torch.Tensor"  # noqa: F821
+    weights: "torch.Tensor"  # noqa: F821
+    counts: "torch.Tensor"  # noqa: F821
+    loss: "torch.Tensor"  # noqa: F821
+    slopes: "torch.Tensor"  # noqa: F821
+    renormalize: bool
+
+
+class Groups(NamedTuple):
+    """What ``group_tokens`` gives: the ends of the groups, the place of each slot (in the ids'
+    shape, -1: none) and the slot of each place."""
+    ends: "torch.Tensor"  # noqa: F821
+    rows: "torch.Tensor"  # noqa: F821
+    slots: "torch.Tensor"  # noqa: F821
+
+
+_route_workspace = functools.lru_cache(maxsize=1024)(hadacore_route_workspace_size)
+_group_workspace = functools.lru_cache(maxsize=1024)(hadacore_group_workspace_size)
+_adapters_workspace = functools.lru_cache(maxsize=1024)(hadacore_adapters_workspace_size)
+_adapter_gradient_workspace = functools.lru_cache(maxsize=1024)(
+    hadacore_adapter_gradient_workspace_size)
+
+
+def _words(n: int, device, dtype=None):
+    return _torch.empty_strided((n,), (1,), dtype=dtype or _torch.int32, device=device)
+
+
+def _matrix(name: str, t, device: int, dims: int = 2):
+    """Checks of a tensor with contiguous rows; the row stride (one that passes for a single row)."""
+    if t.dim() != dims:
+        raise ValueError(f"{name}: expected {dims} dimensions, got {t.dim()}")
+    if t.get_device() != device or device < 0:
+        raise ValueError(f"{name}: all tensors must be on the same ROCm device")
+    shape, steps = t.shape, t.stride()
+    width = shape[-1]
+    if steps[-1] != 1 and width > 1:
+        raise ValueError(f"{name}: rows must be contiguous (column stride 1)")
+    return steps[-2] if shape[-2] > 1 else width
+
+
+def _dense(name: str, t, dtype, shape, device: int):
+    """Checks of a dense tensor of `shape`; its address."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected the shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: all tensors must be on the same ROCm device")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor")
+    return t.data_ptr()
+
+
+def _value_code(name: str, t) -> int:
+    code = _out_codes.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name}: expected float16, bfloat16 or float32, got {t.dtype}")
+    return code
+
+
+def _output(out, shape: tuple, dtype, device):
+    if out is None:
+        return _torch.empty_strided(shape, (shape[1], 1), dtype=dtype, device=device)
+    if out.shape != shape or out.dtype is not dtype or out.device != device \
+            or (out.stride(1) != 1 and shape[1] > 1):
+        raise ValueError(f"out must be a {shape} {dtype} tensor with contiguous rows")
+    return out
+
+
+def route_tokens(logits, k: int, renormalize: bool = True, valid=None, stream=None) -> Routes:
+    """The ``k`` experts with the largest logits for each token (m x experts; float16, bfloat16 or
+    float32), their softmax weights, the number of tokens that each got, and the balance loss
+    experts * sum_e f_e P_e of the shares f of the choices and the mean probabilities P.
+
+    Equal logits go to the lower index.  An expert at -inf is never chosen; a token with too few
+    others gets -1 and weight 0 there, as does one whose ``valid`` (m truth values) is false, which
+    counts nowhere.  Weights are probabilities, over their sum with ``renormalize``.
+    """
+    if _torch is None:
+        _init_torch()
+    device = logits.get_device()
+    stride = _matrix("logits", logits, device)
+    code = _value_code("logits", logits)
+    m, experts = logits.shape
+    valid_ptr = None
+    if valid is not None:
+        valid_ptr = _dense("valid", valid, _torch.bool, (m,), device)
+    where = logits.device
+    chosen = _torch.empty_strided((m, k), (k, 1), dtype=_torch.int32, device=where)
+    weights = _torch.empty_strided((m, k), (k, 1), dtype=_float32, device=where)
+    counts = _words(experts, where)
+    slopes = _words(experts, where, _float32)
+    loss = _torch.empty_strided((), (), dtype=_float32, device=where)
+    need = _route_workspace(m, experts)
+    workspace = _words(need >> 2, where)
+    _call("hadacore_route", device, logits.data_ptr(), stride, code, valid_ptr, m, experts, k,
+          renormalize, chosen.data_ptr(), weights.data_ptr(), counts.data_ptr(), loss.data_ptr(),
+          slopes.data_ptr(), workspace.data_ptr(), need, _stream_of(stream, device))
+    return Routes(chosen, weights, counts, loss, slopes, renormalize)
+
+
+def route_tokens_gradient(logits, routes: Routes, dweights=None, dloss=None, out=None, stream=None):
+    """The logits' gradient, in their type, for the gradients of ``routes.weights`` (m x k) and of
+    ``routes.loss`` (a scalar tensor); None is no gradient."""
+    if _torch is None:
+        _init_torch()
+    device = logits.get_device()
+    stride = _matrix("logits", logits, device)
+    code = _value_code("logits", logits)
+    m, experts = logits.shape
+    k = routes.experts.shape[-1]
+    chosen = _dense("routes.experts", routes.experts, _torch.int32, (m, k), device)
+    weights = _dense("routes.weights", routes.weights, _float32, (m, k), device)
+    slopes = _dense("routes.slopes", routes.slopes, _float32, (experts,), device)
+    dw = dl = None
+    if dweights is not None:
+        dw = _dense("dweights", dweights, _float32, (m, k), device)
+    if dloss is not None:
+        dl = _dense("dloss", dloss, _float32, (), device)
+    out = _output(out, (m, experts), logits.dtype, logits.device)
+    _call("hadacore_route_gradient", device, logits.data_ptr(), stride, code, chosen, weights, slopes,
+          dw, dl, m, experts, k, routes.renormalize, out.data_ptr(), _row_stride(out, experts),
+          _stream_of(stream, device))
+    return out
+
+
+def group_tokens(ids, groups: int, stream=None) -> Groups:
+    """Slots sorted by group: ``ids`` (tokens, or tokens x choices; int32) holds each slot's group,
+    anything outside [0, groups) for none.
+
+    Returns (ends, rows, slots): ``ends`` as the products by expert take them, ``rows`` the place of
+    each slot (-1 without a group) and ``slots`` the slot of each place, those without a
+    group behind the last end.  Slots of a group keep their order.
+    """
+    if _torch is None:
+        _init_torch()
+    device = ids.get_device()
+    if device < 0 or ids.dim() not in (1, 2) or ids.dtype is not _torch.int32 or not ids.is_contiguous():
+        raise ValueError("ids must be a contiguous 1-D or 2-D int32 tensor on a ROCm device")
+    n, where = ids.numel(), ids.device
+    ends, slots = _words(groups, where), _words(n, where)
+    rows = _torch.empty_strided(ids.shape, ids.stride(), dtype=_torch.int32, device=where)
+    need, workspace = _group_workspace(n, groups), None
+    if need:
+        workspace = _words(need >> 2, where)
+    _call("hadacore_group_tokens", device, ids.data_ptr(), n, groups, ends.data_ptr(), rows.data_ptr(),
+          slots.data_ptr(), workspace.data_ptr() if need else None, need, _stream_of(stream, device))
+    return Groups(ends, rows, slots)
+
+
+def _slots_of(rows, device: int):
+    """Tokens and choices of ``rows`` (tokens, or tokens x choices), and its address."""
+    if rows.dtype is not _torch.int32 or rows.dim() not in (1, 2) or not rows.is_contiguous():
+        raise ValueError("rows must be a contiguous 1-D or 2-D int32 tensor")
+    if rows.get_device() != device:
+        raise ValueError("rows: all tensors must be on the same ROCm device")
+    shape = rows.shape
+    return shape[0], shape[1] if len(shape) == 2 else 1, rows.data_ptr()
+
+
+def dispatch_rows(x, rows, ends, out=None, stream=None):
+    """The rows of ``x`` (tokens x width, values of 1, 2 or 4 bytes: codes and their scales too) at
+    the places of their slots: (tokens * choices) x width, zeros behind the last end.  ``rows``
+    and ``ends`` are ``group_tokens``'.  Its gradient is ``combine_rows`` without weights."""
+    if _torch is None:
+        _init_torch()
+    device = x.get_device()
+    stride = _matrix("x", x, device)
+    m, k, rows_ptr = _slots_of(rows, device)
+    tokens, width = x.shape
+    if tokens != m:
+        raise ValueError(f"x has {tokens} rows and rows {m} tokens")
+    _check_ends(ends, device)
+    size = x.element_size()
+    if size not in (1, 2, 4):
+        raise TypeError(f"expected values of 1, 2 or 4 bytes, got {x.dtype}")
+    if out is None and size == 1:
+        out, _ = _padded_rows((m * k, width), x.device)
+        if x.dtype is not _torch.uint8:
+            out = out.view(x.dtype)
+    else:
+        out = _output(out, (m * k, width), x.dtype, x.device)
+    _call("hadacore_dispatch_rows", device, x.data_ptr(), stride, size, rows_ptr, ends.data_ptr(),
+          ends.shape[0], out.data_ptr(), _row_stride(out, width), m, k, width,
+          _stream_of(stream, device))
+    return out
+
+
+def combine_rows(y, rows, weights=None, out=None, stream=None):
+    """The rows of each token's slots, added by weight: out[t] = sum_j weights[t, j] * y[rows[t, j]]
+    (tokens x width, in y's type: float16, bfloat16 or float32), summed in 32 bits.  A slot
+    without a row (-1) adds nothing; ``weights`` is float32 of rows' shape, or None for the sum."""
+    if _torch is None:
+        _init_torch()
+    device = y.get_device()
+    stride = _matrix("y", y, device)
+    code = _value_code("y", y)
+    m, k, rows_ptr = _slots_of(rows, device)
+    places, width = y.shape
+    weights_ptr = None if weights is None else _dense("weights", weights, _float32, rows.shape, device)
+    out = _output(out, (m, width), y.dtype, y.device)
+    _call("hadacore_combine_rows", device, y.data_ptr(), stride, places, code, rows_ptr, weights_ptr,
+          out.data_ptr(), _row_stride(out, width), m, k, width, _stream_of(stream, device))
+    return out
+
+
+def combine_rows_gradient(dout, y, rows, ends, weights=None, want_dy: bool = True, stream=None):
+    """(dy, dweights) of ``combine_rows`` for the gradient ``dout`` of its output: dy in dout's type,
+    zeros behind the last end, and dweights in float32 and rows' shape.  ``y=None`` leaves
+    dweights out, ``want_dy=False`` dy: None in their places."""
+    if _torch is None:
+        _init_torch()
+    device = dout.get_device()
+    stride = _matrix("dout", dout, device)
+    code = _value_code("dout", dout)
+    m, k, rows_ptr = _slots_of(rows, device)
+    tokens, width = dout.shape
+    if tokens != m:
+        raise ValueError(f"dout has {tokens} rows and rows {m} tokens")
+    _check_ends(ends, device)
+    weights_ptr = None if weights is None else _dense("weights", weights, _float32, rows.shape, device)
+    y_ptr, y_stride, dweights, dw_ptr = None, width, None, None
+    if y is not None:
+        y_stride = _matrix("y", y, device)
+        if y.dtype is not dout.dtype or y.shape != (m * k, width):
+            raise ValueError(f"y must be a {(m * k, width)} {dout.dtype} tensor")
+        y_ptr = y.data_ptr()
+        dweights = _torch.empty_strided(rows.shape, rows.stride(), dtype=_float32, device=dout.device)
+        dw_ptr = dweights.data_ptr()
+    dy = dy_ptr = None
+    if want_dy:
+        dy = _torch.empty_strided((m * k, width), (width, 1), dtype=dout.dtype, device=dout.device)
+        dy_ptr = dy.data_ptr()
+    _call("hadacore_combine_gradient", device, dout.data_ptr(), stride, y_ptr, y_stride, code, rows_ptr,
+          ends.data_ptr(), ends.shape[0], weights_ptr, dy_ptr, width, dw_ptr, m, k, width,
+          _stream_of(stream, device))
+    return dy, dweights
+
+
+def _plan(ends, slots, scales, m: int, device: int):
+    """Groups of the adapters, and the addresses of ends, slots and scales."""
+    groups, ends_ptr, slots_ptr, scales_ptr = 1, None, None, None
+    if ends is not None:
+        _check_ends(ends, device)
+        groups, ends_ptr = ends.shape[0], ends.data_ptr()
+    if slots is not None:
+        slots_ptr = _dense("slots", slots, _torch.int32, (m,), device)
+    if scales is not None:
+        scales_ptr = _dense("scales", scales, _float32, (groups,), device)
+    return groups, ends_ptr, slots_ptr, scales_ptr
+
+
+def adapt_rows(x, down, up, ends=None, slots=None, y=None, scales=None, out=None, dtype=None,
+               hidden: bool = False, stream=None):
+    """Low-rank adapters, one for each group of tokens: out[t] = y[t] + scales[g] * (x[t] @ down[g]^T)
+    @ up[g] for the tokens of group g, and y[t] for those of none.
+
+    ``x`` is tokens x k, ``down`` groups x rank x k and ``up`` groups x rank x n (float16 or bfloat16):
+    both weights are stored rank by rank.  ``ends`` and ``slots`` are ``group_tokens``' for one id a
+    token; ``slots=None``: the tokens are sorted themselves; ``ends=None``: one adapter (``down``
+    and ``up`` without the first dimension, or with one of 1) for all.  ``y`` (tokens x n, x's
+    type or float32) may be ``out``; without it the output is of ``dtype`` (default x's).  With
+    ``hidden`` returns (out, h), h (tokens x rank, float32) the first products by place, for
+    ``adapter_gradient``; its rows behind the last end are not written.
+    """
+    if _torch is None:
+        _init_torch()
+    device = x.get_device()
+    x_stride = _matrix("x", x, device)
+    code = _dtype_code(x)
+    if ends is None and down.dim() == 2 and up.dim() == 2:
+        down, up = down[None], up[None]
+    down_stride, up_stride = _matrix("down", down, device, 3), _matrix("up", up, device, 3)
+    m, k = x.shape
+    groups, rank, k_down = down.shape
+    n = up.shape[2]
+    if down.dtype is not x.dtype or up.dtype is not x.dtype:
+        raise TypeError(f"down and up must be {x.dtype}, as x, got {down.dtype} and {up.dtype}")
+    count, ends_ptr, slots_ptr, scales_ptr = _plan(ends, slots, scales, m, device)
+    if k_down != k or up.shape[:2] != (groups, rank) or count != groups:
+        raise ValueError(f"x of {tuple(x.shape)}, down of {tuple(down.shape)}, up of {tuple(up.shape)} "
+                         f"and {count} groups do not go together")
+    y_ptr, y_stride, where = None, n, x.device
+    if y is not None:
+        y_stride = _matrix("y", y, device)
+        if y.shape != (m, n) or (dtype is not None and y.dtype is not dtype):
+            raise ValueError(f"y must be a {(m, n)} tensor of the output's type")
+        dtype, y_ptr = y.dtype, y.data_ptr()
+    elif dtype is None:
+        dtype = x.dtype
+    if dtype is not x.dtype and dtype is not _float32:
+        raise TypeError(f"expected an output of {x.dtype} or float32, got {dtype}")
+    if out is None or out is not y:
+        out = _output(out, (m, n), dtype, where)
+    h_ptr, padded = None, (rank + 15) & ~15
+    if hidden:
+        h = _torch.empty_strided((m, padded), (padded, 1), dtype=_float32, device=where)
+        h_ptr = h.data_ptr()
+    need = _adapters_workspace(m, k, n, rank, groups)
+    workspace = _words(need >> 2, where)
+    _call("hadacore_adapters", device, x.data_ptr(), x_stride, down.data_ptr(), down_stride,
+          down.stride(0), up.data_ptr(), up_stride, up.stride(0), scales_ptr, ends_ptr, slots_ptr,
+          groups, y_ptr, y_stride, out.data_ptr(), _row_stride(out, n), code, _out_codes[dtype], h_ptr,
+          padded, m, k, n, rank, workspace.data_ptr(), need, _stream_of(stream, device))
+    if not hidden:
+        return out
+    return out, h if padded == rank else h.narrow(1, 0, rank)
+
+
+def adapter_gradient(h, x, ends=None, slots=None, scales=None, out=None, dtype=None, stream=None):
+    """The gradient of an adapter's weight: scales[g] * sum over the tokens of group g of h x^T, groups x
+    rank x width (rank x width without ``ends``).
+
+    For out = ``adapt_rows(x, down, up, ..., hidden=True)`` with hidden values h and the gradient
+    dout: dx and dh are ``adapt_rows(dout, up, down, ..., hidden=True)`` of the same groups, up's gradient
+    ``adapter_gradient(h, dout, ...)`` and down's ``adapter_gradient(dh, x, ...)``.  ``dtype`` is x's
+    (default) or float32.  A group without tokens gets zeros.
+    """
+    if _torch is None:
+        _init_torch()
+    device = x.get_device()
+    x_stride, h_stride = _matrix("x", x, device), _matrix("h", h, device)
+    code = _dtype_code(x)
+    m, width = x.shape
+    if h.dtype is not _float32 or h.shape[0] != m:
+        raise ValueError(f"h must be a float32 tensor of {m} rows")
+    rank = h.shape[1]
+    groups, ends_ptr, slots_ptr, scales_ptr = _plan(ends, slots, scales, m, device)
+    shape = (rank, width) if ends is None else (groups, rank, width)
+    if out is None:
+        steps = (width, 1) if ends is None else (rank * width, width, 1)
+        dtype = dtype or x.dtype
+        if dtype is not x.dtype and dtype is not _float32:
+            raise TypeError(f"expected an output of {x.dtype} or float32, got {dtype}")
+        out = _torch.empty_strided(shape, steps, dtype=dtype, device=x.device)
+    elif out.shape != shape or out.device != x.device or (width > 1 and out.stride(-1) != 1) \
+            or out.dtype not in (x.dtype, _float32) or (dtype is not None and out.dtype is not dtype):
+        raise ValueError(f"out must be a {shape} tensor of the output's type with contiguous rows")
+    need, workspace = _adapter_gradient_workspace(m, width, rank, groups), None
+    if need:
+        workspace = _words(need >> 2, x.device)
+    _call("hadacore_adapter_gradient", device, h.data_ptr(), h_stride, x.data_ptr(), x_stride, code,
+          scales_ptr, ends_ptr, slots_ptr, groups, out.data_ptr(), _row_stride(out, width),
+          out.stride(0) if ends is not None else 0, _out_codes[out.dtype], m, width, rank,
+          workspace.data_ptr() if need else None, need, _stream_of(stream, device))
     return out
