@@ -31,6 +31,7 @@
 #include "groups.h"
 #include "hadacore.h"
 #include "internal.h"
+#include "lds_loads.h"
 
 namespace hadacore {
 namespace {
@@ -164,7 +165,7 @@ struct AdapterArgs {
   int64_t part_pitch, part_step;
   float *hidden;  // where h goes besides
   int64_t hidden_stride;
-  int m, k, n, rank, padded, groups, splits, unit;  // padded: the rank in whole tiles
+  int m, k, n, rank, padded, groups, splits, unit, chunks;  // padded: the rank in whole tiles
 };
 
 // The token of a place; a wrong slot gives a wrong row, but no access out of bounds.
@@ -181,58 +182,53 @@ __device__ __forceinline__ Piece piece_of(const int32_t *ends, int groups, int m
   return {id * (int64_t)unit < m ? 0 : -1, id * unit, m};
 }
 
-// h for 16 TT tokens of a group, 16 RT of its ranks and one of `splits` shares of k.  Four waves
-// take a quarter of the share each and add up at the end, so that each value of x and of
+// h for 16 TT tokens of a group, 16 RT of its ranks and one of `splits` shares of k.  W waves
+// take a part of the share each and add up at the end, so that each value of x and of
 // the weights is loaded by one wave, straight into the operands of the matrix products: both
 // have k along their rows.  U steps of k are loaded ahead of the U being multiplied.
-template <int DT, int TT, int RT, int U>
-__global__ __launch_bounds__(256) void down_kernel(AdapterArgs p) {
-  constexpr int kWaves = 4;
-  __shared__ f4 sums[kWaves][TT * RT][kWave];
+template <int DT, int TT, int RT, int U, int W>
+__global__ __launch_bounds__(W *kWave) void down_kernel(AdapterArgs p) {
+  constexpr int kTiles = TT * RT;
+  constexpr int kHeld = kTiles * W > 64 ? kTiles / 2 : kTiles;  // tiles in LDS at a time
+  __shared__ f4 sums[W][kHeld][kWave];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int c = lane % kTile, quarter = lane / kTile;
   const Piece piece = piece_of(p.ends, p.groups, p.m, kTile * TT, blockIdx.x, false);
   if (piece.group < 0) return;
   const int rank0 = blockIdx.z * (kTile * RT);
+  // whole steps of k, then (by the last wave) the rest of it
+  const int64_t steps = p.k / kStep;
+  const int shares = p.splits * W, share = blockIdx.y * W + wave;
+  const int from = (int)(steps * share / shares), to = (int)(steps * (share + 1) / shares);
   const uint16_t *xp[TT], *wp[RT];
 #pragma unroll
   for (int t = 0; t < TT; ++t) {
     const int place = piece.low + t * kTile + c;
     xp[t] = p.x + token_of(p.slots, place < piece.high ? place : piece.high - 1, p.m) * p.x_stride +
-            quarter * 8;
+            quarter * 8 + (int64_t)from * kStep;
   }
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const int row = rank0 + r * kTile + c;
     wp[r] = p.down + piece.group * p.down_batch + (row < p.rank ? row : p.rank - 1) * p.down_stride +
-            quarter * 8;
+            quarter * 8 + (int64_t)from * kStep;
   }
-  const int64_t steps = ((int64_t)p.k + kStep - 1) / kStep;
-  const int shares = p.splits * kWaves, share = blockIdx.y * kWaves + wave;
-  const int from = (int)(steps * share / shares), to = (int)(steps * (share + 1) / shares);
   f4 acc[TT][RT] = {};
   u4 xv[2][U][TT], wv[2][U][RT];
-  const auto load = [&](int s0, int buffer) {
-    if (s0 + U <= to && (s0 + U) * kStep <= p.k) {
+  const auto load = [&](int buffer) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int at = (s0 + u) * kStep;
+    for (int u = 0; u < U; ++u) {
 #pragma unroll
-        for (int t = 0; t < TT; ++t) xv[buffer][u][t] = *reinterpret_cast<const u4_any *>(xp[t] + at);
+      for (int t = 0; t < TT; ++t)
+        xv[buffer][u][t] = *reinterpret_cast<const u4_any *>(xp[t] + u * kStep);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) wv[buffer][u][r] = *reinterpret_cast<const u4_any *>(wp[r] + at);
-      }
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int at = (s0 + u) * kStep;
-        const int valid = s0 + u < to ? p.k - at - quarter * 8 : 0;
-#pragma unroll
-        for (int t = 0; t < TT; ++t) xv[buffer][u][t] = load8(xp[t] + at, valid);
-#pragma unroll
-        for (int r = 0; r < RT; ++r) wv[buffer][u][r] = load8(wp[r] + at, valid);
-      }
+      for (int r = 0; r < RT; ++r)
+        wv[buffer][u][r] = *reinterpret_cast<const u4_any *>(wp[r] + u * kStep);
     }
+#pragma unroll
+    for (int t = 0; t < TT; ++t) xp[t] += U * kStep;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) wp[r] += U * kStep;
   };
   const auto multiply = [&](int buffer) {
 #pragma unroll
@@ -243,75 +239,192 @@ __global__ __launch_bounds__(256) void down_kernel(AdapterArgs p) {
         for (int r = 0; r < RT; ++r)
           acc[t][r] = mfma<DT>(wv[buffer][u][r], xv[buffer][u][t], acc[t][r]);
   };
-  if (from < to) load(from, 0);
-  for (int s = from; s < to; s += 2 * U) {
-    if (s + U < to) load(s + U, 1);
+  const int turns = (to - from) / U;
+  if (turns > 0) load(0);
+  for (int s = 0; s < turns; s += 2) {
+    if (s + 1 < turns) load(1);
     multiply(0);
-    if (s + U >= to) break;
-    if (s + 2 * U < to) load(s + 2 * U, 0);
+    if (s + 1 >= turns) break;
+    if (s + 2 < turns) load(0);
     multiply(1);
   }
+  const int left = (to - from) % U + (share == shares - 1 && p.k % kStep != 0);
+  for (int s = 0; s < left; ++s) {
+    const int valid = (from + turns * U + s < to ? kStep : p.k % kStep) - quarter * 8;
 #pragma unroll
-  for (int t = 0; t < TT; ++t)
+    for (int t = 0; t < TT; ++t) xv[0][0][t] = load8(xp[t] + s * kStep, valid);
 #pragma unroll
-    for (int r = 0; r < RT; ++r) sums[wave][t * RT + r][lane] = acc[t][r];
-  __syncthreads();
-  for (int i = wave; i < TT * RT; i += kWaves) {
-    f4 v = sums[0][i][lane];
+    for (int r = 0; r < RT; ++r) wv[0][0][r] = load8(wp[r] + s * kStep, valid);
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) v += sums[w][i][lane];
-    const int place = piece.low + i / RT * kTile + c;
-    const int rank = rank0 + i % RT * kTile + 4 * quarter;
+    for (int t = 0; t < TT; ++t)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (rank + j >= p.rank) v[j] = 0.0f;
-    if (place < piece.high && rank < p.padded)
-      *reinterpret_cast<f4 *>(p.part + blockIdx.y * p.part_step + place * p.part_pitch + rank) = v;
+      for (int r = 0; r < RT; ++r) acc[t][r] = mfma<DT>(wv[0][0][r], xv[0][0][t], acc[t][r]);
+  }
+#pragma unroll
+  for (int first = 0; first < kTiles; first += kHeld) {
+    if (first > 0) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) sums[wave][i][lane] = acc[(first + i) / RT][(first + i) % RT];
+    __syncthreads();
+    for (int i = wave; i < kHeld; i += W) {
+      f4 v = sums[0][i][lane];
+#pragma unroll
+      for (int w = 1; w < W; ++w) v += sums[w][i][lane];
+      const int place = piece.low + (first + i) / RT * kTile + c;
+      const int rank = rank0 + (first + i) % RT * kTile + 4 * quarter;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (rank + j >= p.rank) v[j] = 0.0f;
+      if (place < piece.high && rank < p.padded)
+        *reinterpret_cast<f4 *>(p.part + blockIdx.y * p.part_step + place * p.part_pitch + rank) = v;
+    }
   }
 }
+
+// Values that are read or written once: with the streaming policy they do not push the weights
+// and h out of the L2.
+template <class V>
+__device__ __forceinline__ V stream_in(const void *p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const V *>(p));
+}
+template <class V>
+__device__ __forceinline__ void stream_out(void *p, V v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<V *>(p));
+}
+
+// CT consecutive outputs of a row as words.
+template <int OUT, int CT>
+struct OutRow {
+  static constexpr int kWords = CT * (OUT == HADACORE_FP32 ? 4 : 2) / 4;
+  uint32_t w[kWords];
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = 0;
+  }
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (OUT == HADACORE_FP32)
+      return __builtin_bit_cast(float, w[i]);
+    else
+      return widen<OUT>((uint16_t)(w[i / 2] >> (16 * (i % 2))));
+  }
+  __device__ __forceinline__ void set(const float (&v)[CT]) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      if constexpr (OUT == HADACORE_FP32)
+        w[i] = __builtin_bit_cast(uint32_t, v[i]);
+      else
+        w[i] = narrow<OUT>(v[2 * i]) | (uint32_t)narrow<OUT>(v[2 * i + 1]) << 16;
+    }
+  }
+  // Rows may start at any value's address.
+  __device__ __forceinline__ void load(const uint8_t *p) {
+    if constexpr (kWords == 2) {
+      const u2 v = stream_in<u2_any>(p);
+      w[0] = v[0];
+      w[1] = v[1];
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords / 4; ++i) {
+        const u4 v = stream_in<u4_any>(p + 16 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
+      }
+    }
+  }
+  // the first `valid` of the CT values
+  __device__ __forceinline__ void load(const uint8_t *p, int64_t valid) {
+    if (valid >= CT) return load(p);
+    clear();
+#pragma unroll
+    for (int i = 0; i < CT; ++i) {
+      if (i >= valid) continue;
+      if constexpr (OUT == HADACORE_FP32)
+        w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+      else
+        w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(p)[i] << (16 * (i % 2));
+    }
+  }
+  __device__ __forceinline__ void store(uint8_t *p) const {
+    if constexpr (kWords == 2) {
+      stream_out<u2_any>(p, u2{w[0], w[1]});
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords / 4; ++i)
+        stream_out<u4_any>(p + 16 * i, u4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]});
+    }
+  }
+  __device__ __forceinline__ void store(uint8_t *p, int64_t valid) const {
+    if (valid >= CT) return store(p);
+#pragma unroll
+    for (int i = 0; i < CT; ++i) {
+      if (i >= valid) continue;
+      if constexpr (OUT == HADACORE_FP32)
+        reinterpret_cast<uint32_t *>(p)[i] = w[i];
+      else
+        reinterpret_cast<uint16_t *>(p)[i] = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
+    }
+  }
+};
 
 // out for up to `unit` tokens of a group and 4 * 16 CT columns.  A wave keeps the weights of its
 // 16 CT columns in registers for all these tokens: 8 rows of CT columns a lane, turned in
 // registers so that the ranks lie along an operand.  A lane then has CT consecutive columns of each
-// of four tokens, which it loads and stores whole.  h, joined and split, goes through LDS.
-// Tokens behind the last end get y.
-template <int DT, int OUT, int RB, int CT, int P>
+// of four tokens, which it loads and stores whole, the next four's y under the products of these.
+// h, joined and split, goes through LDS.  Tokens behind the last end get y.
+template <int DT, int OUT, int RB, int CT, int P, int D, bool EVEN>
 __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
   constexpr int kPitch = kStep * RB + 8;
+  constexpr int kSize = OUT == HADACORE_FP32 ? 4 : 2;
   extern __shared__ __attribute__((aligned(16))) uint8_t room[];
   uint16_t *parts = reinterpret_cast<uint16_t *>(room);  // [P][unit][kPitch]
   float *back = reinterpret_cast<float *>(parts + P * p.unit * kPitch);
   int *tokens = reinterpret_cast<int *>(back + p.unit);
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int c = lane % kTile, quarter = lane / kTile;
-  const Piece piece = piece_of(p.ends, p.groups, p.m, p.unit, blockIdx.x, true);
+  const int chunk = blockIdx.x % p.chunks;
+  const Piece piece = piece_of(p.ends, p.groups, p.m, p.unit, blockIdx.x / p.chunks, true);
   if (piece.group < 0) return;
   const bool bare = piece.group == p.groups;  // no adapter
   if (bare && p.y == p.out) return;
   const int count = piece.high - piece.low < p.unit ? piece.high - piece.low : p.unit;
-  const int col = (blockIdx.y * 4 + wave) * (kTile * CT) + c * CT;
-  const int64_t valid = (int64_t)p.n - col;
-  u4 w[RB][CT];
+  const int col = (chunk * 4 + wave) * (kTile * CT) + c * CT;
+  const int64_t valid = EVEN ? CT : (int64_t)p.n - col;
+  uint32_t raw[RB][8][CT / 2];
   if (!bare) {
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      uint32_t raw[8][CT / 2];
+    for (int b = 0; b < RB; ++b)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int row = b * kStep + quarter * 8 + j;
+        // ranks that are not there: any values, cleared below
         load_columns<CT>(p.up + piece.group * p.up_batch + (row < p.rank ? row : 0) * p.up_stride + col,
-                         row < p.rank ? valid : 0, raw[j]);
+                         valid, raw[b][j]);
       }
-      turn<CT>(raw, w[b]);
-    }
   }
+  const uint8_t *y = static_cast<const uint8_t *>(p.y);
+  uint8_t *out = static_cast<uint8_t *>(p.out);
+  using Row = OutRow<OUT, CT>;
+  // Whole tiles of 16 tokens whose columns are all there go without a branch in a lane, so that
+  // loads stay in flight over stores and products.
+  const bool whole = EVEN || (chunk * 4 + wave + 1) * (kTile * CT) <= p.n;
+  const int fast = whole && y != nullptr ? count / kTile * kTile : 0;
+  Row old[D][4];
+#pragma unroll
+  for (int d = 0; d < D; ++d) {
+    if (d * kTile >= fast) break;
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+      old[d][v].load(y + (token_of(p.slots, piece.low + d * kTile + 4 * quarter + v, p.m) * p.y_stride +
+                          col) * kSize);
+  }
+  const float scale = !bare && p.scales != nullptr ? p.scales[piece.group] : 1.0f;
   for (int t0 = 0; t0 < count; t0 += 256 / kTile) {
     const int t = t0 + tid / kTile, q = tid % kTile;
     if (t >= count) continue;
     const int place = piece.low + t;
     if (q == 0) tokens[t] = token_of(p.slots, place, p.m);
     if (bare) continue;
-    const float scale = p.scales != nullptr ? p.scales[piece.group] : 1.0f;
     constexpr int kEach = (kStep * RB + 63) / 64;
     f4 h[kEach];
     float most = 0.0f;
@@ -322,8 +435,17 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
       if (r < p.padded) {
         const float *at = p.part + place * p.part_pitch + r;
         v = *reinterpret_cast<const f4 *>(at);
-        for (int s = 1; s < p.splits; ++s) v += *reinterpret_cast<const f4 *>(at + s * p.part_step);
-        if (p.hidden != nullptr && p.splits > 1 && blockIdx.y == 0)
+        // four shares' loads at a time, joined in order
+        for (int s = 1; s < p.splits; s += 4) {
+          f4 more[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            more[j] = s + j < p.splits ? *reinterpret_cast<const f4 *>(at + (s + j) * p.part_step)
+                                       : f4{0, 0, 0, 0};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v += more[j];
+        }
+        if (p.hidden != nullptr && p.splits > 1 && chunk == 0)
           *reinterpret_cast<f4 *>(p.hidden + place * p.hidden_stride + r) = v;
       }
 #pragma unroll
@@ -352,76 +474,77 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
             u2{v[0][k] | (uint32_t)v[1][k] << 16, v[2][k] | (uint32_t)v[3][k] << 16};
     }
   }
+  u4 w[RB][CT];
+  if (!bare) {
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      if ((b + 1) * kStep > p.rank) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int i = 0; i < CT / 2; ++i)
+            raw[b][j][i] = b * kStep + quarter * 8 + j < p.rank ? raw[b][j][i] : 0;
+      }
+      turn<CT>(raw[b], w[b]);
+    }
+  }
   __syncthreads();
   // whole waves only: a matrix instruction reads the registers of all 64 lanes
-  if ((blockIdx.y * 4 + wave) * (kTile * CT) >= p.n) return;
-  using T = std::conditional_t<OUT == HADACORE_FP32, float, uint16_t>;
-  struct __attribute__((packed, aligned(sizeof(T)))) Row {
-    T v[CT];
+  if ((chunk * 4 + wave) * (kTile * CT) >= p.n) return;
+  const auto multiply = [&](int t0, f4 (&acc)[CT]) {
+    if (bare) return;
+#pragma unroll
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+      for (int k = P - 1; k >= 0; --k) {
+        const u4 a = *reinterpret_cast<const u4 *>(
+            parts + (k * p.unit + t0 + c) * kPitch + b * kStep + quarter * 8);
+#pragma unroll
+        for (int i = 0; i < CT; ++i) acc[i] = mfma<DT>(a, w[b][i], acc[i]);
+      }
   };
-  const T *y = static_cast<const T *>(p.y);
-  T *out = static_cast<T *>(p.out);
-  const auto value = [](T v) {
-    if constexpr (OUT == HADACORE_FP32)
-      return v;
-    else
-      return widen<OUT>(v);
+  const auto add = [&](int t, int v, const f4 (&acc)[CT], Row &row) {
+    const float unshift = DT == HADACORE_FP16 && !bare ? back[t] : 1.0f;
+    float sum[CT];
+#pragma unroll
+    for (int i = 0; i < CT; ++i) sum[i] = fmaf(acc[i][v], unshift, row.get(i));
+    row.set(sum);
   };
-  for (int t0 = 0; t0 < count; t0 += kTile) {
-    const int mine = t0 + 4 * quarter;
-    T old[4][CT];
-    int token[4];
+  for (int t0 = 0; t0 < fast; t0 += D * kTile) {
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+      const int now = t0 + d * kTile, mine = now + 4 * quarter, next = now + D * kTile;
+      if (now >= fast) break;
+      f4 acc[CT] = {};
+      multiply(now, acc);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        add(mine + v, v, acc, old[d][v]);
+        old[d][v].store(out + (tokens[mine + v] * p.out_stride + col) * kSize);
+      }
+      if (next < fast) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          old[d][v].load(y + (tokens[next + 4 * quarter + v] * p.y_stride + col) * kSize);
+      }
+    }
+  }
+  for (int t0 = fast; t0 < count; t0 += kTile) {
+    Row rest[4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      token[v] = tokens[mine + v < count ? mine + v : t0];
-#pragma unroll
-      for (int i = 0; i < CT; ++i) old[v][i] = 0;
-      if (y != nullptr && mine + v < count) {
-        const T *from = y + token[v] * p.y_stride + col;
-        if (valid >= CT) {  // (fewer, or none: value by value)
-          const Row raw = *reinterpret_cast<const Row *>(from);
-#pragma unroll
-          for (int i = 0; i < CT; ++i) old[v][i] = raw.v[i];
-        } else {
-#pragma unroll
-          for (int i = 0; i < CT; ++i)
-            if (i < valid) old[v][i] = from[i];
-        }
-      }
+      const int t = t0 + 4 * quarter + v;
+      rest[v].clear();
+      if (y != nullptr && t < count) rest[v].load(y + (tokens[t] * p.y_stride + col) * kSize, valid);
     }
     f4 acc[CT] = {};
-    if (!bare) {
-#pragma unroll
-      for (int b = 0; b < RB; ++b)
-#pragma unroll
-        for (int k = P - 1; k >= 0; --k) {
-          const u4 a = *reinterpret_cast<const u4 *>(
-              parts + (k * p.unit + t0 + c) * kPitch + b * kStep + quarter * 8);
-#pragma unroll
-          for (int i = 0; i < CT; ++i) acc[i] = mfma<DT>(a, w[b][i], acc[i]);
-        }
-    }
+    multiply(t0, acc);
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      if (mine + v >= count) continue;
-      const float unshift = DT == HADACORE_FP16 && !bare ? back[mine + v] : 1.0f;
-      T *to = out + token[v] * p.out_stride + col;
-      Row row;
-#pragma unroll
-      for (int i = 0; i < CT; ++i) {
-        const float sum = fmaf(acc[i][v], unshift, value(old[v][i]));
-        if constexpr (OUT == HADACORE_FP32)
-          row.v[i] = sum;
-        else
-          row.v[i] = narrow<OUT>(sum);
-      }
-      if (valid >= CT) {
-        *reinterpret_cast<Row *>(to) = row;
-      } else {
-#pragma unroll
-        for (int i = 0; i < CT; ++i)
-          if (i < valid) to[i] = row.v[i];
-      }
+      const int t = t0 + 4 * quarter + v;
+      if (t >= count) continue;
+      add(t, v, acc, rest[v]);
+      rest[v].store(out + (tokens[t] * p.out_stride + col) * kSize, valid);
     }
   }
 }
@@ -448,15 +571,212 @@ __device__ __forceinline__ void store_value(void *out, int64_t at, float v) {
     static_cast<uint16_t *>(out)[at] = narrow<OUT>(v);
 }
 
-constexpr int kGradWaves = 8;
 constexpr int kGradColumns = kTile * 8;
 
+// A step of 32 tokens of dW[g]: their h (hv: rank c of 16 and tokens 8 quarter + j) times their x
+// (raw: the same tokens, 8 columns).  fp16: h is taken times 2^-shift, and `shift` grows with h.
+template <int DT, int RT, int P>
+__device__ __forceinline__ void gradient_step(const uint32_t (&raw)[8][4], const float (&hv)[RT][8],
+                                              int &shift, f4 (&acc)[RT][8]) {
+  float scale = 1.0f;
+  if constexpr (DT == HADACORE_FP16) {
+    float most = 0.0f;
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(hv[r][j]));
+    const int e = scale_exponent(max_lanes(most, kWave));
+    if (e > shift) {
+      const float less = shift - e < -126 ? 0.0f : power_of_two(shift - e);
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[r][i] *= less;
+      shift = e;
+    }
+    scale = power_of_two(-shift);
+  }
+  u4 xc[8];
+  turn<8>(raw, xc);
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    uint16_t v[8][P];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) split<DT, P>(hv[r][j] * scale, v[j]);
+#pragma unroll
+    for (int k = P - 1; k >= 0; --k) {
+      u4 a;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) a[j] = v[2 * j][k] | (uint32_t)v[2 * j + 1][k] << 16;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[r][i] = mfma<DT>(a, xc[i], acc[r][i]);
+    }
+  }
+}
+
+// Adds up the W waves' sums and stores them, or leaves them in the workspace.
+template <int DT, int OUT, int RT, int W>
+__device__ __forceinline__ void store_gradient(const GradientArgs &p, int g, int rank0, int shift,
+                                               const f4 (&acc)[RT][8], f4 (*sums)[8][kWave + 1]) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const float unshift = DT == HADACORE_FP16 ? power_of_two(shift) : 1.0f;
+  const float factor = p.scales != nullptr ? p.scales[g] : 1.0f;
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[wave][i][lane] = acc[r][i] * unshift;
+    __syncthreads();
+    // four ranks of a column for each thread in turn
+    for (int id = threadIdx.x; id < 4 * kGradColumns; id += W * kWave) {
+      const int at = id % kGradColumns, four = id / kGradColumns;  // column: 8 c + i
+      const int64_t column = (int64_t)blockIdx.x * kGradColumns + at;
+      f4 v = sums[0][at % 8][four * kTile + at / 8];
+#pragma unroll
+      for (int w = 1; w < W; ++w) v += sums[w][at % 8][four * kTile + at / 8];
+      if (column >= p.width) continue;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int rank = rank0 + r * kTile + 4 * four + j;
+        if (rank >= p.rank) continue;
+        if (p.splits > 1)
+          p.part[((int64_t)blockIdx.y * p.rank + rank) * p.width + column] = v[j];
+        else
+          store_value<OUT>(p.out, g * p.out_batch + rank * p.out_stride + column, factor * v[j]);
+      }
+    }
+  }
+}
+
 // dW[g] for 16 RT ranks and 128 columns: the sum over a share of the group's tokens, 32 at a time by
-// eight waves in turn.  Both operands have the tokens along their depth: x is turned in registers, h
-// is read as it lies and split.
+// two waves in turn.  Both operands have the tokens along their depth: x is turned in registers, h
+// is split.  Each wave streams its own rows of x and h into a ring in LDS, two steps ahead, and
+// their tokens three: no barriers, and few instructions, which are loaded anew by every call
+// (with the loads in registers, a step ahead, 31 us instead of NEW for 8191 x 4096, rank 16).
+constexpr int kGradWaves = 2;
+constexpr int kGradRing = 3;
+
 template <int DT, int OUT, int RT, int P>
 __global__ __launch_bounds__(kGradWaves *kWave) void gradient_kernel(GradientArgs p) {
-  __shared__ f4 sums[kGradWaves][8][kWave];
+  constexpr int kX = kStep * kGradColumns * 2, kH = RT * kStep * kTile * 4;
+  constexpr int kLoads = 8 + 8 * RT;  // of a step's x and h
+  static_assert(kLoads + 1 < 64, "loads in flight that one wait can count");
+  constexpr int kRing = kGradRing * (kX + kH);
+  constexpr int kSums = kGradWaves * 8 * (kWave + 1) * 16;
+  __shared__ __attribute__((aligned(16))) uint8_t
+      room[kGradWaves * kRing > kSums ? kGradWaves * kRing : kSums];
+  __shared__ int32_t token_room[kGradWaves][5][kWave];
+  const int lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int c = lane % kTile, quarter = lane / kTile;
+  const int g = blockIdx.y % p.groups, share = blockIdx.y / p.groups;
+  const int rank0 = blockIdx.z * (kTile * RT);
+  int col = blockIdx.x * kGradColumns + c * 8;  // a multiple of 8, as the width is
+  col = col < p.width ? col : p.width - 8;
+  const int low = p.ends != nullptr && g > 0 ? clamp_end(p.ends[g - 1], p.m) : 0;
+  const int high = p.ends != nullptr ? clamp_end(p.ends[g], p.m) : p.m;
+  const int stride = kStep * kGradWaves * p.splits;
+  const int first = low + (share * kGradWaves + wave) * kStep;
+  const int steps = first < high ? (high - first + stride - 1) / stride : 0;
+  uint8_t *ring = room + wave * kRing;
+  // places behind the group's end take its last; they are cleared before the products
+  const auto place_of = [&](int i, int t) {
+    const int place = first + i * stride + t;
+    return place < high ? place : high - 1;
+  };
+  const auto load_tokens = [&](int i) {
+    int32_t *to = &token_room[wave][i & 3][0];
+    const int place = place_of(i, lane % kStep);
+    if (p.slots != nullptr) {
+      load_word_to_lds(p.slots + place, lds_address(to));
+    } else {
+      to[lane] = place;
+      load_word_to_lds(p.h, lds_address(&token_room[wave][4][0]));  // for the count of loads
+    }
+  };
+  const auto load_rows = [&](int i, int stage) {
+    uint8_t *to = ring + stage * (kX + kH);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int s = token_room[wave][i & 3][4 * j + quarter];
+      const int token = s < 0 ? 0 : s >= p.m ? p.m - 1 : s;
+      load_lane_to_lds(p.x + token * p.x_stride + col, lds_address(to + j * 1024));
+    }
+    // h so that a lane finds its eight tokens' values at its own place
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const int row = rank0 + r * kTile + c;
+      const float *rank = p.h + (row < p.rank ? row : p.rank - 1);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        load_word_to_lds(rank + place_of(i, 8 * quarter + j) * p.h_stride,
+                         lds_address(to + kX + (r * 8 + j) * 256));
+    }
+  };
+  f4 acc[RT][8] = {};
+  int shift = -100, stage = 1;
+  // Turn i loads the tokens of step i + 3 and the rows of step i + 2, and multiplies step i.
+  // In flight before its wait, in order: the rows of step i, the tokens of i + 2, the rows of i + 1, the
+  // tokens of i + 3; all but the last two have to be there.
+#pragma unroll 1
+  for (int i = -3; i < steps; ++i) {
+    const bool more = i + 3 < steps;
+    if (more) load_tokens(i + 3);
+    if (i == -3) continue;
+    if (i == -2) {
+      if (more)
+        asm volatile("s_waitcnt vmcnt(1)" ::: "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    } else if (more) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads + 1) : "memory");
+    } else if (i + 1 < steps) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    // step i is in `stage`, and step i + 2 goes where i - 1 was
+    const uint8_t *from = ring + stage * (kX + kH);
+    if (i + 2 < steps) load_rows(i + 2, stage == 0 ? kGradRing - 1 : stage - 1);
+    stage = stage == kGradRing - 1 ? 0 : stage + 1;
+    if (i < 0) continue;
+    uint32_t raw[8][4];
+    float hv[RT][8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const u4 v = *reinterpret_cast<const u4 *>(from + (8 * quarter + j) * 256 + c * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) raw[j][e] = v[e];
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+        hv[r][j] = *reinterpret_cast<const float *>(from + kX + (r * 8 + j) * 256 + lane * 4);
+    }
+    // the reads have returned before the next loads go to this stage
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    const int s = first + i * stride;
+    if (s + kStep > high) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const bool on = s + 8 * quarter + j < high;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) raw[j][e] = on ? raw[j][e] : 0;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) hv[r][j] = on ? hv[r][j] : 0.0f;
+      }
+    }
+    gradient_step<DT, RT, P>(raw, hv, shift, acc);
+  }
+  store_gradient<DT, OUT, RT, kGradWaves>(p, g, rank0, shift, acc,
+                                          reinterpret_cast<f4(*)[8][kWave + 1]>(room));
+}
+
+// The same for rows of x off 16 bytes: loads of any address, in registers, by more waves since nothing
+// is loaded ahead.
+constexpr int kAnyWaves = 8;
+
+template <int DT, int OUT, int RT, int P>
+__global__ __launch_bounds__(kAnyWaves *kWave) void gradient_any_kernel(GradientArgs p) {
+  __shared__ f4 sums[kAnyWaves][8][kWave + 1];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int c = lane % kTile, quarter = lane / kTile;
   const int g = blockIdx.y % p.groups, share = blockIdx.y / p.groups;
@@ -466,16 +786,16 @@ __global__ __launch_bounds__(kGradWaves *kWave) void gradient_kernel(GradientArg
   const int low = p.ends != nullptr && g > 0 ? clamp_end(p.ends[g - 1], p.m) : 0;
   const int high = p.ends != nullptr ? clamp_end(p.ends[g], p.m) : p.m;
   f4 acc[RT][8] = {};
-  int shift = -100;  // fp16: h is taken times 2^-shift
-  const int stride = kStep * kGradWaves * p.splits;
-  for (int64_t s = low + (int64_t)(share * kGradWaves + wave) * kStep; s < high; s += stride) {
-    const int place = (int)s + 8 * quarter;
+  int shift = -100;
+  const int stride = kStep * kAnyWaves * p.splits;
+#pragma unroll 1
+  for (int64_t s = low + (int64_t)(share * kAnyWaves + wave) * kStep; s < high; s += stride) {
     uint32_t raw[8][4];
     float hv[RT][8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const bool on = place + j < high;
-      const int at = on ? place + j : high - 1;
+      const bool on = s + 8 * quarter + j < high;
+      const int at = on ? (int)s + 8 * quarter + j : high - 1;
       load_columns<8>(p.x + token_of(p.slots, at, p.m) * p.x_stride + col, on ? valid : 0, raw[j]);
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
@@ -484,69 +804,9 @@ __global__ __launch_bounds__(kGradWaves *kWave) void gradient_kernel(GradientArg
         hv[r][j] = on ? v : 0.0f;
       }
     }
-    float scale = 1.0f;
-    if constexpr (DT == HADACORE_FP16) {
-      float most = 0.0f;
-#pragma unroll
-      for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(hv[r][j]));
-      const int e = scale_exponent(max_lanes(most, kWave));
-      if (e > shift) {
-        const float less = shift - e < -126 ? 0.0f : power_of_two(shift - e);
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) acc[r][i] *= less;
-        shift = e;
-      }
-      scale = power_of_two(-shift);
-    }
-    u4 xc[8];
-    turn<8>(raw, xc);
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      uint16_t v[8][P];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) split<DT, P>(hv[r][j] * scale, v[j]);
-#pragma unroll
-      for (int k = P - 1; k >= 0; --k) {
-        u4 a;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) a[j] = v[2 * j][k] | (uint32_t)v[2 * j + 1][k] << 16;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) acc[r][i] = mfma<DT>(a, xc[i], acc[r][i]);
-      }
-    }
+    gradient_step<DT, RT, P>(raw, hv, shift, acc);
   }
-  const float unshift = DT == HADACORE_FP16 ? power_of_two(shift) : 1.0f;
-  const float factor = p.scales != nullptr ? p.scales[g] : 1.0f;
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    if (r > 0) __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sums[wave][i][lane] = acc[r][i] * unshift;
-    __syncthreads();
-    // wave w: rank w and w + 8 of the 16, 128 columns as two of a lane
-    for (int half = 0; half < 2; ++half) {
-      const int in_tile = wave + half * 8, rank = rank0 + r * kTile + in_tile;
-      if (rank >= p.rank) continue;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int at = lane + e * kWave;  // column: 8 c + i
-        if (blockIdx.x * kGradColumns + at >= p.width) continue;
-        float v = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kGradWaves; ++w)
-          v += sums[w][at % 8][in_tile / 4 * kTile + at / 8][in_tile % 4];
-        const int64_t column = (int64_t)blockIdx.x * kGradColumns + at;
-        if (p.splits > 1)
-          p.part[((int64_t)blockIdx.y * p.rank + rank) * p.width + column] = v;
-        else
-          store_value<OUT>(p.out, g * p.out_batch + rank * p.out_stride + column, factor * v);
-      }
-    }
-  }
+  store_gradient<DT, OUT, RT, kAnyWaves>(p, g, rank0, shift, acc, sums);
 }
 
 template <int OUT>
@@ -560,6 +820,10 @@ __global__ __launch_bounds__(256) void join_gradient_kernel(GradientArgs p) {
     const float factor = p.scales != nullptr ? p.scales[g] : 1.0f;
     store_value<OUT>(p.out, g * p.out_batch + rank * p.out_stride + i % p.width, factor * v);
   }
+}
+
+bool aligned_to(const void *p, uintptr_t bytes) {
+  return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0;
 }
 
 // ---- how a call is cut ---------------------------------------------------------------
@@ -589,7 +853,8 @@ Cut cut_of(int64_t m, int64_t k, int64_t n, int64_t rank, int64_t groups, int pa
   cut.tiles = few ? 1 : cut.ranks == 8 ? 2 : 4;
   const int64_t blocks =
       (divide_up(m, 16 * cut.tiles) + live - 1) * divide_up(rank, 16 * cut.ranks);
-  int64_t splits = divide_up(kBlocksWanted, blocks < 1 ? 1 : blocks);
+  // with four tiles of ranks a wave takes a whole SIMD: a workgroup to a CU
+  int64_t splits = divide_up(cut.ranks == 4 ? kBlocksWanted / 2 : kBlocksWanted, blocks < 1 ? 1 : blocks);
   const int64_t most = k / 512;  // four steps of k for a wave at least
   splits = splits > most ? most : splits;
   cut.splits = (int)(splits < 1 ? 1 : splits > 16 ? 16 : splits);
@@ -604,8 +869,8 @@ Cut cut_of(int64_t m, int64_t k, int64_t n, int64_t rank, int64_t groups, int pa
 int64_t gradient_splits(int64_t m, int64_t width, int64_t rank, int64_t groups) {
   if (groups < 1 || width < 1) return 1;
   const int64_t blocks = divide_up(width, kGradColumns) * groups * divide_up(rank, 64);
-  int64_t splits = divide_up(kBlocksWanted, blocks);
-  // a workgroup goes through 256 tokens in a turn; a share has two turns at least
+  int64_t splits = divide_up(2 * kBlocksWanted, blocks);
+  // a workgroup goes through 64 tokens in a turn; a share has two turns at least
   const int64_t most = m / groups / (2 * kStep * kGradWaves);
   splits = splits > most ? most : splits;
   return splits < 1 ? 1 : splits > 16 ? 16 : splits;
@@ -628,9 +893,11 @@ template <int DT>
 void launch_down(const AdapterArgs &p, const Cut &cut, hipStream_t stream) {
   const int64_t pieces = most_pieces(p.m, p.groups, 16 * cut.tiles);
   const dim3 grid((uint32_t)pieces, (uint32_t)cut.splits, (uint32_t)divide_up(p.rank, 16 * cut.ranks));
-  const auto go = [&](auto tt, auto rt, auto u) {
-    hipLaunchKernelGGL((down_kernel<DT, decltype(tt)::value, decltype(rt)::value, decltype(u)::value>),
-                       grid, dim3(256), 0, stream, p);
+  const auto go = [&](auto tt, auto rt, auto u, auto w) {
+    constexpr int W = decltype(w)::value;
+    hipLaunchKernelGGL(
+        (down_kernel<DT, decltype(tt)::value, decltype(rt)::value, decltype(u)::value, W>), grid,
+        dim3(W * kWave), 0, stream, p);
   };
   using std::integral_constant;
   const integral_constant<int, 1> one{};
@@ -639,35 +906,40 @@ void launch_down(const AdapterArgs &p, const Cut &cut, hipStream_t stream) {
   const integral_constant<int, 8> eight{};
   if (cut.tiles == 1) {
     if (cut.ranks == 1)
-      go(one, one, four);
+      go(one, one, four, four);
     else if (cut.ranks == 2)
-      go(one, two, four);
+      go(one, two, four, four);
     else if (cut.ranks == 4)
-      go(one, four, two);
+      go(one, four, two, four);
     else
-      go(one, eight, two);
+      go(one, eight, two, four);
   } else if (cut.ranks == 1) {
-    go(four, one, two);
+    go(four, one, two, four);
   } else if (cut.ranks == 2) {
-    go(four, two, two);
+    go(four, two, two, four);
   } else if (cut.ranks == 4) {
-    go(four, four, one);
+    go(four, four, two, four);
   } else {
-    go(two, eight, one);
+    go(two, eight, one, four);
   }
 }
 
 template <int DT, int OUT>
-void launch_up(const AdapterArgs &p, hipStream_t stream) {
+void launch_up(AdapterArgs p, hipStream_t stream) {
   constexpr int P = parts_of(DT, OUT);
   const int64_t pieces = most_pieces(p.m, p.groups, p.unit);
+  constexpr int kAhead = 2;
   const auto go = [&](auto rb, auto ct) {
     constexpr int RB = decltype(rb)::value, CT = decltype(ct)::value;
     const size_t lds = (size_t)p.unit * (P * (kStep * RB + 8) * 2 + 8);
-    const int64_t columns = divide_up(p.n, 4 * 16 * CT);  // 0: h is joined all the same
-    hipLaunchKernelGGL((up_kernel<DT, OUT, RB, CT, P>),
-                       dim3((uint32_t)pieces, (uint32_t)(columns > 0 ? columns : 1)), dim3(256), lds,
-                       stream, p);
+    // the columns of a token's row run together: whole rows of y and out, and with as many chunks as
+    // XCDs (or a multiple) each of them meets only its own columns of the weights
+    p.chunks = p.n > 0 ? (int)divide_up(p.n, 4 * 16 * CT) : 1;  // without columns h is joined
+    const dim3 grid((uint32_t)(pieces * p.chunks));
+    if (p.n % (16 * CT) == 0)
+      hipLaunchKernelGGL((up_kernel<DT, OUT, RB, CT, P, kAhead, true>), grid, dim3(256), lds, stream, p);
+    else
+      hipLaunchKernelGGL((up_kernel<DT, OUT, RB, CT, P, kAhead, false>), grid, dim3(256), lds, stream, p);
   };
   using std::integral_constant;
   const integral_constant<int, 8> eight{};
@@ -687,9 +959,14 @@ void launch_gradient(const GradientArgs &p, hipStream_t stream) {
   const int ranks = p.rank <= 16 ? 1 : p.rank <= 32 ? 2 : 4;
   const dim3 grid((uint32_t)divide_up(p.width, kGradColumns), (uint32_t)(p.groups * p.splits),
                   (uint32_t)divide_up(p.rank, 16 * ranks));
+  const bool streams = aligned_to(p.x, 16) && p.x_stride % 8 == 0 && p.width % 8 == 0;
   const auto go = [&](auto rt) {
-    hipLaunchKernelGGL((gradient_kernel<DT, OUT, decltype(rt)::value, P>), grid,
-                       dim3(kGradWaves * kWave), 0, stream, p);
+    if (streams)
+      hipLaunchKernelGGL((gradient_kernel<DT, OUT, decltype(rt)::value, P>), grid,
+                         dim3(kGradWaves * kWave), 0, stream, p);
+    else
+      hipLaunchKernelGGL((gradient_any_kernel<DT, OUT, decltype(rt)::value, P>), grid,
+                         dim3(kAnyWaves * kWave), 0, stream, p);
   };
   using std::integral_constant;
   if (ranks == 1)
@@ -711,10 +988,6 @@ constexpr int64_t kMaxPitch = int64_t(1) << 26;
 constexpr int64_t kMaxBytes = int64_t(1) << 42;
 constexpr int64_t kMaxTokens = int64_t(1) << 27;  // a launch stays below 2^32 work-items
 constexpr int64_t kMaxWidth = int64_t(1) << 22;
-
-bool aligned_to(const void *p, uintptr_t bytes) {
-  return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0;
-}
 
 // `batch` matrices of `rows` rows: strides, size, address.
 hadacore_status check_matrices(const void *p, int64_t batch, int64_t step, int64_t rows, int64_t pitch,
