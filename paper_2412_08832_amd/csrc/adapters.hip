@@ -281,19 +281,24 @@ __global__ __launch_bounds__(W *kWave) void down_kernel(AdapterArgs p) {
   }
 }
 
-// Values that are read or written once: with the streaming policy they do not push the weights
-// and h out of the L2.
-template <class V>
+// Values that are read or written once: where rows are whole lines, the streaming policy (NT)
+// keeps them from pushing the weights and h out of the L2 (16384 x 8192: up_kernel 118 us instead of
+// 150).  Rows that share lines are slower with it (1733 x 5003 in 32 bits: 28 instead of 23).
+template <bool NT, class V>
 __device__ __forceinline__ V stream_in(const void *p) {
-  return __builtin_nontemporal_load(reinterpret_cast<const V *>(p));
+  if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const V *>(p));
+  return *reinterpret_cast<const V *>(p);
 }
-template <class V>
+template <bool NT, class V>
 __device__ __forceinline__ void stream_out(void *p, V v) {
-  __builtin_nontemporal_store(v, reinterpret_cast<V *>(p));
+  if constexpr (NT)
+    __builtin_nontemporal_store(v, reinterpret_cast<V *>(p));
+  else
+    *reinterpret_cast<V *>(p) = v;
 }
 
 // CT consecutive outputs of a row as words.
-template <int OUT, int CT>
+template <int OUT, int CT, bool NT>
 struct OutRow {
   static constexpr int kWords = CT * (OUT == HADACORE_FP32 ? 4 : 2) / 4;
   uint32_t w[kWords];
@@ -320,13 +325,13 @@ struct OutRow {
   // Rows may start at any value's address.
   __device__ __forceinline__ void load(const uint8_t *p) {
     if constexpr (kWords == 2) {
-      const u2 v = stream_in<u2_any>(p);
+      const u2 v = stream_in<NT, u2_any>(p);
       w[0] = v[0];
       w[1] = v[1];
     } else {
 #pragma unroll
       for (int i = 0; i < kWords / 4; ++i) {
-        const u4 v = stream_in<u4_any>(p + 16 * i);
+        const u4 v = stream_in<NT, u4_any>(p + 16 * i);
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
       }
@@ -347,11 +352,11 @@ struct OutRow {
   }
   __device__ __forceinline__ void store(uint8_t *p) const {
     if constexpr (kWords == 2) {
-      stream_out<u2_any>(p, u2{w[0], w[1]});
+      stream_out<NT, u2_any>(p, u2{w[0], w[1]});
     } else {
 #pragma unroll
       for (int i = 0; i < kWords / 4; ++i)
-        stream_out<u4_any>(p + 16 * i, u4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]});
+        stream_out<NT, u4_any>(p + 16 * i, u4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]});
     }
   }
   __device__ __forceinline__ void store(uint8_t *p, int64_t valid) const {
@@ -404,7 +409,7 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
   }
   const uint8_t *y = static_cast<const uint8_t *>(p.y);
   uint8_t *out = static_cast<uint8_t *>(p.out);
-  using Row = OutRow<OUT, CT>;
+  using Row = OutRow<OUT, CT, EVEN>;
   // Whole tiles of 16 tokens whose columns are all there go without a branch in a lane, so that
   // loads stay in flight over stores and products.
   const bool whole = EVEN || (chunk * 4 + wave + 1) * (kTile * CT) <= p.n;
@@ -861,7 +866,7 @@ Cut cut_of(int64_t m, int64_t k, int64_t n, int64_t rank, int64_t groups, int pa
   const int64_t depth = round_up(rank, kStep), columns = divide_up(n, rank > 128 ? 256 : 512);
   cut.unit = 16;
   while (cut.unit < 128 && !few && 2 * cut.unit * (depth + 8) * 2 * parts <= 48 * 1024 &&
-         m / (2 * cut.unit) * columns >= 2 * kBlocksWanted)
+         m / (2 * cut.unit) * columns >= (rank > 64 ? 1 : 2) * kBlocksWanted)
     cut.unit *= 2;
   return cut;
 }
@@ -928,6 +933,10 @@ template <int DT, int OUT>
 void launch_up(AdapterArgs p, hipStream_t stream) {
   constexpr int P = parts_of(DT, OUT);
   const int64_t pieces = most_pieces(p.m, p.groups, p.unit);
+  // EVEN: columns in whole tiles, and rows of y and out from the start of a line
+  constexpr int64_t kLine = 128 / (OUT == HADACORE_FP32 ? 4 : 2);
+  const bool lines = aligned_to(p.out, 128) && p.out_stride % kLine == 0 &&
+                     (p.y == nullptr || (aligned_to(p.y, 128) && p.y_stride % kLine == 0));
   constexpr int kAhead = 2;
   const auto go = [&](auto rb, auto ct) {
     constexpr int RB = decltype(rb)::value, CT = decltype(ct)::value;
@@ -936,7 +945,7 @@ void launch_up(AdapterArgs p, hipStream_t stream) {
     // XCDs (or a multiple) each of them meets only its own columns of the weights
     p.chunks = p.n > 0 ? (int)divide_up(p.n, 4 * 16 * CT) : 1;  // without columns h is joined
     const dim3 grid((uint32_t)(pieces * p.chunks));
-    if (p.n % (16 * CT) == 0)
+    if (p.n % (16 * CT) == 0 && lines)
       hipLaunchKernelGGL((up_kernel<DT, OUT, RB, CT, P, kAhead, true>), grid, dim3(256), lds, stream, p);
     else
       hipLaunchKernelGGL((up_kernel<DT, OUT, RB, CT, P, kAhead, false>), grid, dim3(256), lds, stream, p);

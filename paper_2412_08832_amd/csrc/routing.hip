@@ -62,41 +62,66 @@ __device__ __forceinline__ typename Stored<DT>::type narrow(float v) {
     return __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
-// N consecutive values, of which the first `valid` exist (the others are `rest`).  Rows may start
-// at any value's address; the hardware takes wide loads and stores from there.
+// N consecutive values of a row.  Rows may start at any value's address; the hardware takes wide loads
+// and stores from there.  NT: with the streaming policy, for data that is touched once and more
+// than the caches keep.
+template <int DT, int N>
+struct Values {
+  using T = typename Stored<DT>::type;
+  struct Raw {
+    T v[N];
+  };
+  typedef uint32_t Words __attribute__((ext_vector_type(sizeof(Raw) / 4)));
+  typedef Words Words_any __attribute__((aligned(sizeof(T))));
+  Raw raw;
+
+  // the first `valid` of them; zeros behind
+  template <bool NT = false>
+  __device__ __forceinline__ void load(const T *p, int valid) {
+    if (valid >= N) {
+      if constexpr (NT)
+        raw = __builtin_bit_cast(Raw, __builtin_nontemporal_load(reinterpret_cast<const Words_any *>(p)));
+      else
+        raw = __builtin_bit_cast(Raw, *reinterpret_cast<const Words_any *>(p));
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) raw.v[i] = i < valid ? p[i] : T(0);
+    }
+  }
+  template <bool NT = false>
+  __device__ __forceinline__ void store(T *p, int valid) const {
+    if (valid >= N) {
+      if constexpr (NT)
+        __builtin_nontemporal_store(__builtin_bit_cast(Words, raw), reinterpret_cast<Words_any *>(p));
+      else
+        *reinterpret_cast<Words_any *>(p) = __builtin_bit_cast(Words, raw);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (i < valid) p[i] = raw.v[i];
+    }
+  }
+  __device__ __forceinline__ float get(int i) const { return widen<DT>(raw.v[i]); }
+  __device__ __forceinline__ void set(const float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) raw.v[i] = narrow<DT>(v[i]);
+  }
+};
+
 template <int DT, int N>
 __device__ __forceinline__ void load_row(const typename Stored<DT>::type *p, int valid, float rest,
                                          float (&v)[N]) {
-  using T = typename Stored<DT>::type;
-  struct __attribute__((packed, aligned(sizeof(T)))) Raw {
-    T v[N];
-  };
-  if (valid >= N) {
-    const Raw raw = *reinterpret_cast<const Raw *>(p);
+  Values<DT, N> row;
+  row.load(p, valid);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = widen<DT>(raw.v[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = i < valid ? widen<DT>(p[i]) : rest;
-  }
+  for (int i = 0; i < N; ++i) v[i] = i < valid ? row.get(i) : rest;
 }
 
 template <int DT, int N>
 __device__ __forceinline__ void store_row(typename Stored<DT>::type *p, int valid, const float (&v)[N]) {
-  using T = typename Stored<DT>::type;
-  struct __attribute__((packed, aligned(sizeof(T)))) Raw {
-    T v[N];
-  };
-  if (valid >= N) {
-    Raw raw;
-#pragma unroll
-    for (int i = 0; i < N; ++i) raw.v[i] = narrow<DT>(v[i]);
-    *reinterpret_cast<Raw *>(p) = raw;
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < valid) p[i] = narrow<DT>(v[i]);
-  }
+  Values<DT, N> row;
+  row.set(v);
+  row.store(p, valid);
 }
 
 // ---- reductions over the L lanes (a power of two, at least 8) that share a row ----------
@@ -622,9 +647,10 @@ typedef u4 u4_any __attribute__((aligned(1)));
 constexpr int kDispatchLoads = 4;
 constexpr int kDispatchChunk = kWave * 16 * kDispatchLoads;
 
+template <bool NT>
 __global__ __launch_bounds__(256) void dispatch_kernel(DispatchArgs p) {
   const int lane = threadIdx.x % kWave;
-  const int64_t id = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+  const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int t = (int)(id / p.chunks), chunk = (int)(id % p.chunks);
   if (t >= p.m) return;
   const int slots = p.m * p.k;
@@ -638,13 +664,17 @@ __global__ __launch_bounds__(256) void dispatch_kernel(DispatchArgs p) {
     v[i] = u4{0, 0, 0, 0};
     if (at + 16 <= p.bytes) v[i] = *reinterpret_cast<const u4_any *>(from + at);
   }
-  const auto put = [&](int row, bool zero) {
+  const auto copy = [&](int row, bool zero) {
     uint8_t *to = p.out + row * p.out_stride;
 #pragma unroll
     for (int i = 0; i < kDispatchLoads; ++i) {
       const int at = start + i * kWave * 16;
       if (at + 16 <= p.bytes) {
-        *reinterpret_cast<u4_any *>(to + at) = zero ? u4{0, 0, 0, 0} : v[i];
+        const u4 put = zero ? u4{0, 0, 0, 0} : v[i];
+        if constexpr (NT)
+          __builtin_nontemporal_store(put, reinterpret_cast<u4_any *>(to + at));
+        else
+          *reinterpret_cast<u4_any *>(to + at) = put;
       } else {
         // the row's last bytes, value by value
         for (int b = at; b < p.bytes; b += p.size) {
@@ -662,9 +692,9 @@ __global__ __launch_bounds__(256) void dispatch_kernel(DispatchArgs p) {
   };
   for (int j = 0; j < p.k; ++j) {
     const int slot = t * p.k + j;
-    const int row = __builtin_amdgcn_readfirstlane(p.rows[slot]);
-    if ((uint32_t)row < (uint32_t)used) put(row, false);
-    if (slot >= used) put(slot, true);
+    const int row = p.rows[slot];
+    if ((uint32_t)row < (uint32_t)used) copy(row, false);
+    if (slot >= used) copy(slot, true);
   }
 }
 
@@ -677,47 +707,38 @@ struct CombineArgs {
   int places, m, k, width, chunks;
 };
 
-// One wave joins 64 * N * U columns of a token's rows: the loads of four slots before their sums.
-template <int DT, int N, int U>
+// One wave joins 64 N columns of a token's rows: the loads of K slots before their sums.
+template <int DT, int N, int K, bool NT>
 __global__ __launch_bounds__(256) void combine_kernel(CombineArgs p) {
   using T = typename Stored<DT>::type;
   const int lane = threadIdx.x % kWave;
-  const int64_t id = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+  const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int t = (int)(id / p.chunks), chunk = (int)(id % p.chunks);
   if (t >= p.m) return;
-  const int col = chunk * (kWave * N * U) + lane * N;
-  const T *in = static_cast<const T *>(p.in);
-  float acc[U][N] = {};
+  const int col = chunk * (kWave * N) + lane * N, valid = p.width - col;
+  const T *in = static_cast<const T *>(p.in) + col;
+  float acc[N] = {};
   const int32_t *rows = p.rows + (int64_t)t * p.k;
   const float *weights = p.weights != nullptr ? p.weights + (int64_t)t * p.k : nullptr;
-  constexpr int kAhead = 4;
-  for (int j0 = 0; j0 < p.k; j0 += kAhead) {
-    float v[kAhead][U][N], w[kAhead];
+  for (int j0 = 0; j0 < p.k; j0 += K) {
+    Values<DT, N> v[K];
+    float w[K];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      const int row = j0 + j < p.k ? __builtin_amdgcn_readfirstlane(rows[j0 + j]) : -1;
+    for (int j = 0; j < K; ++j) {
+      const int row = j0 + j < p.k ? rows[j0 + j] : -1;
       const bool there = (uint32_t)row < (uint32_t)p.places;
       w[j] = !there ? 0.0f : weights != nullptr ? weights[j0 + j] : 1.0f;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int at = col + u * kWave * N;
-        // a row that is not there adds nothing, whatever its weight: zeros times 0
-        load_row<DT, N>(in + (there ? row : 0) * p.in_stride + at, there ? p.width - at : 0, 0.0f, v[j][u]);
-      }
+      // a row that is not there adds nothing, whatever its weight: zeros times 0
+      v[j].template load<NT>(in + (there ? row : 0) * p.in_stride, there ? valid : 0);
     }
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j)
+    for (int j = 0; j < K; ++j)
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int i = 0; i < N; ++i) acc[u][i] = fmaf(w[j], v[j][u][i], acc[u][i]);
+      for (int i = 0; i < N; ++i) acc[i] = fmaf(w[j], v[j].get(i), acc[i]);
   }
-  T *out = static_cast<T *>(p.out) + t * p.out_stride;
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int at = col + u * kWave * N;
-    store_row<DT, N>(out + at, p.width - at, acc[u]);
-  }
+  Values<DT, N> out;
+  out.set(acc);
+  out.template store<NT>(static_cast<T *>(p.out) + t * p.out_stride + col, valid);
 }
 
 struct CombineGradArgs {
@@ -732,11 +753,12 @@ struct CombineGradArgs {
 
 // dy[rows[t,j]] = w_tj dout[t], dw_tj = <dout[t], y[rows[t,j]]>; places behind the last end get zeros.
 // W waves go through a token's row together, K slots at a time: dout is read once for them.
-template <int DT, int N, int W, int K>
+template <int DT, int N, int W, int K, bool NT>
 __global__ __launch_bounds__(256) void combine_gradient_kernel(CombineGradArgs p) {
   using T = typename Stored<DT>::type;
   __shared__ float parts[4][K];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int64_t id = (int64_t)blockIdx.x * (4 / W) + (W == 1 ? wave : 0);
   if (W == 1 && id >= p.m) return;
   const int t = (int)id, slots = p.m * p.k;
@@ -751,25 +773,24 @@ __global__ __launch_bounds__(256) void combine_gradient_kernel(CombineGradArgs p
 #pragma unroll
     for (int j = 0; j < K; ++j) {
       const int64_t at = (int64_t)t * p.k + (j0 + j < p.k ? j0 + j : 0);
-      row[j] = __builtin_amdgcn_readfirstlane(p.rows[at]);
+      row[j] = p.rows[at];
       if (j0 + j >= p.k || (uint32_t)row[j] >= (uint32_t)used) row[j] = -1;
       w[j] = p.weights != nullptr ? p.weights[at] : 1.0f;
       dot[j] = 0.0f;
     }
     for (int at = first; at < p.width; at += W * kWave * N) {
       const int valid = p.width - at;
-      float d[N], v[K][N];
-      load_row<DT, N>(dout + at, valid, 0.0f, d);
+      Values<DT, N> d, v[K];
+      d.template load<NT>(dout + at, valid);
       if (p.dweights != nullptr) {
 #pragma unroll
         for (int j = 0; j < K; ++j)
-          if (row[j] >= 0) load_row<DT, N>(y + row[j] * p.y_stride + at, valid, 0.0f, v[j]);
+          v[j].template load<NT>(y + (row[j] >= 0 ? row[j] : 0) * p.y_stride + at, row[j] >= 0 ? valid : 0);
 #pragma unroll
-        for (int j = 0; j < K; ++j)
-          if (row[j] >= 0) {
+        for (int j = 0; j < K; ++j) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) dot[j] = fmaf(d[i], v[j][i], dot[j]);
-          }
+          for (int i = 0; i < N; ++i) dot[j] = fmaf(d.get(i), v[j].get(i), dot[j]);
+        }
       }
       if (dy != nullptr) {
 #pragma unroll
@@ -777,13 +798,15 @@ __global__ __launch_bounds__(256) void combine_gradient_kernel(CombineGradArgs p
           if (row[j] >= 0) {
             float s[N];
 #pragma unroll
-            for (int i = 0; i < N; ++i) s[i] = w[j] * d[i];
-            store_row<DT, N>(dy + row[j] * p.dy_stride + at, valid, s);
+            for (int i = 0; i < N; ++i) s[i] = w[j] * d.get(i);
+            v[j].set(s);
+            v[j].template store<NT>(dy + row[j] * p.dy_stride + at, valid);
           }
           const int slot = t * p.k + j0 + j;
           if (j0 + j < p.k && slot >= used) {
             const float zero[N] = {};
-            store_row<DT, N>(dy + slot * p.dy_stride + at, valid, zero);
+            v[j].set(zero);
+            v[j].template store<NT>(dy + slot * p.dy_stride + at, valid);
           }
         }
       }
@@ -862,6 +885,16 @@ bool any_overlap(const Span (&out)[O], const Span (&in)[I]) {
 }
 
 Span words(const void *p, int64_t n) { return span(p, p != nullptr, n, n, 4); }
+
+// Whether rows go with the streaming policy: `bytes` of them, and each of whole lines.
+struct Lines {
+  const void *p;
+  int64_t stride, width;  // bytes
+};
+bool streams(int64_t bytes, Lines a, Lines b = {nullptr, 0, 0}) {
+  return bytes >= (int64_t(1) << 24) && aligned_to(a.p, 128) && (a.stride | a.width) % 128 == 0 &&
+         aligned_to(b.p, 128) && (b.stride | b.width) % 128 == 0;
+}
 
 hadacore_status check_choices(int64_t m, int64_t experts, int64_t k, hadacore_dtype dtype) {
   if (m < 0) return HADACORE_ERROR_INVALID_VALUE;
@@ -1084,8 +1117,12 @@ extern "C" hadacore_status hadacore_dispatch_rows(const void *in, int64_t in_row
   if (blocks * 256 >= (int64_t(1) << 32)) return HADACORE_ERROR_TOO_LARGE;
   st = check_device();
   if (st != HADACORE_SUCCESS) return st;
-  hipLaunchKernelGGL(dispatch_kernel, dim3((uint32_t)blocks), dim3(256), 0,
-                     static_cast<hipStream_t>(stream), p);
+  if (streams(m * k * p.bytes, {out, p.out_stride, p.bytes}))
+    hipLaunchKernelGGL(dispatch_kernel<true>, dim3((uint32_t)blocks), dim3(256), 0,
+                       static_cast<hipStream_t>(stream), p);
+  else
+    hipLaunchKernelGGL(dispatch_kernel<false>, dim3((uint32_t)blocks), dim3(256), 0,
+                       static_cast<hipStream_t>(stream), p);
   return status_of(hipGetLastError());
 }
 
@@ -1121,8 +1158,8 @@ extern "C" hadacore_status hadacore_combine_rows(const void *in, int64_t in_row_
   p.width = (int)width;
   hadacore_status result = HADACORE_SUCCESS;
   for_type(dtype, [&](auto dt) {
-    constexpr int DT = decltype(dt)::value, N = DT == HADACORE_FP32 ? 4 : 8, U = 1;
-    p.chunks = (p.width + kWave * N * U - 1) / (kWave * N * U);
+    constexpr int DT = decltype(dt)::value, N = DT == HADACORE_FP32 ? 4 : 8;
+    p.chunks = (p.width + kWave * N - 1) / (kWave * N);
     const int64_t blocks = (m * p.chunks + 3) / 4;
     if (blocks * 256 >= (int64_t(1) << 32)) {
       result = HADACORE_ERROR_TOO_LARGE;
@@ -1130,8 +1167,21 @@ extern "C" hadacore_status hadacore_combine_rows(const void *in, int64_t in_row_
     }
     result = check_device();
     if (result != HADACORE_SUCCESS) return;
-    hipLaunchKernelGGL((combine_kernel<DT, N, U>), dim3((uint32_t)blocks), dim3(256), 0,
-                       static_cast<hipStream_t>(stream), p);
+    const auto go = [&](auto slots, auto nt) {
+      hipLaunchKernelGGL((combine_kernel<DT, N, decltype(slots)::value, decltype(nt)::value>),
+                         dim3((uint32_t)blocks), dim3(256), 0, static_cast<hipStream_t>(stream), p);
+    };
+    const auto by_slots = [&](auto nt) {
+      if (k <= 2)
+        go(std::integral_constant<int, 2>{}, nt);
+      else
+        go(std::integral_constant<int, 4>{}, nt);
+    };
+    if (streams(m * k * width * size, {in, in_row_stride * size, width * size},
+                {out, out_row_stride * size, width * size}))
+      by_slots(std::true_type{});
+    else
+      by_slots(std::false_type{});
     result = status_of(hipGetLastError());
   });
   return result;
@@ -1178,10 +1228,14 @@ extern "C" hadacore_status hadacore_combine_gradient(
   for_type(dtype, [&](auto dt) {
     constexpr int DT = decltype(dt)::value, N = DT == HADACORE_FP32 ? 4 : 8;
     const auto go = [&](auto waves, auto slots) {
-      constexpr int W = decltype(waves)::value;
-      hipLaunchKernelGGL((combine_gradient_kernel<DT, N, W, decltype(slots)::value>),
-                         dim3((uint32_t)((m * W + 3) / 4)), dim3(256), 0,
-                         static_cast<hipStream_t>(stream), p);
+      constexpr int W = decltype(waves)::value, K = decltype(slots)::value;
+      const dim3 grid((uint32_t)((m * W + 3) / 4));
+      hipStream_t s = static_cast<hipStream_t>(stream);
+      if (streams(m * k * width * size, {want_y ? dy : y, (want_y ? dy_row_stride : y_row_stride) * size,
+                                         width * size}))
+        hipLaunchKernelGGL((combine_gradient_kernel<DT, N, W, K, true>), grid, dim3(256), 0, s, p);
+      else
+        hipLaunchKernelGGL((combine_gradient_kernel<DT, N, W, K, false>), grid, dim3(256), 0, s, p);
     };
     const auto by_slots = [&](auto waves) {
       if (k == 1)
