@@ -452,7 +452,7 @@ int64_t hadacore_route_workspace_size(int64_t m, int64_t experts);
  *   valid       m bytes, or NULL: all are valid
  *   k           1 to HADACORE_MAX_CHOICES and at most `experts` (INVALID_SIZE otherwise)
  *   out_experts, out_weights  m * k values, in falling order of the logits
- *   workspace   hadacore_route_workspace_size(m, experts) bytes, 4-byte aligned
+ *   workspace   hadacore_route_workspace_size(m, experts) bytes, 16-byte aligned
  */
 hadacore_status hadacore_route(const void *logits, int64_t logits_row_stride, hadacore_dtype dtype,
                                const uint8_t *valid, int64_t m, int64_t experts, int64_t k,

@@ -151,6 +151,11 @@ __device__ __forceinline__ uint32_t max_across(uint32_t x) {
   return across(x, L, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
 
+template <int L>
+__device__ __forceinline__ uint32_t min_across(uint32_t x) {
+  return across(x, L, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+}
+
 // In an order of its own for every L, the same in every lane.
 template <int L>
 __device__ __forceinline__ float sum_across(float x) {
@@ -175,6 +180,17 @@ __device__ __forceinline__ T sum_workgroup(T x, T *room) {
   return x;
 }
 
+// exp(x) for x <= 0 (NaN: some value), 0 below 2^-126: 2^t for the rounded t = x log2(e), and what t
+// lacks as a factor.  Within 2 units of the last place, in six operations.
+__device__ __forceinline__ float exp_down(float x) {
+  x = fmaxf(x, -200.0f);
+  const float t = x * 1.44269504f;
+  float rest = fmaf(x, 1.44269504f, -t);
+  rest = fmaf(x, 1.92596303e-8f, rest);
+  const float e = __builtin_amdgcn_exp2f(t);
+  return fmaf(e, rest * 0.69314718f, e);
+}
+
 // What one lane of a wave wrote to LDS is there for its others: LDS works through a wave's
 // accesses in order, and the compiler may not move them over this.
 __device__ __forceinline__ void wave_sync() {
@@ -186,10 +202,10 @@ __device__ __forceinline__ void wave_sync() {
 //
 // p = softmax(l), S the k largest logits, f_e the share of expert e in all choices, T the tokens:
 //   loss = E sum_e f_e (1/T) sum_t p_te,   slopes_e = d loss / d p_te = E f_e / T.
-// L lanes share a row, V consecutive experts in each, so that an equal logit's lower index is in the
-// lower lane: a choice is one maximum over the lanes and one ballot.  Sums of p stay in the lanes'
-// registers over a workgroup's rows; workgroups leave theirs and their counts in the workspace,
-// and a workgroup joins them in order.
+// L lanes share a row; each has V experts, four consecutive ones of each 4 L (expert_of).  A choice is a
+// maximum over the lanes, and the least index that has it.  Sums of p stay in the lanes' registers
+// over a workgroup's rows; workgroups leave theirs and their counts in the workspace, and other
+// workgroups, one for 64 experts, join them in order.
 
 struct RouteArgs {
   const void *logits;
@@ -200,9 +216,14 @@ struct RouteArgs {
   float *weights;
   int32_t *counts;
   float *loss, *slopes;
-  // of each workgroup: sums of p, counts, and how many tokens have an expert
+  // of each workgroup: sums of p, counts (`pitch` of each, in fours), how many tokens have an expert
+  // and how many they have
+  int pitch;
   float *part_p;
-  int32_t *part_counts, *part_tokens;
+  int32_t *part_counts, *part_tokens, *part_choices;
+  // of each joining workgroup its share of the loss, and how many are done
+  uint64_t *part_loss;
+  uint32_t *done;
 };
 
 constexpr int kRouteThreads = 1024;
@@ -219,83 +240,149 @@ __device__ __forceinline__ float from_key(uint32_t k) {
   return __builtin_bit_cast(float, (k & 0x80000000u) ? k ^ 0x80000000u : ~k);
 }
 
-__device__ void join_routes(const RouteArgs &p, int parts) {
-  constexpr int kWaves = kRouteThreads / kWave;
-  __shared__ float sum_p[kRouteThreads];
-  __shared__ int sum_c[kRouteThreads];
+typedef int i4 __attribute__((ext_vector_type(4)));
+
+constexpr int kJoinExperts = 64;
+
+// 64 experts: four a thread, as many threads to four experts as there are.  Returns their part
+// of the loss.
+__device__ double join_routes(const RouteArgs &p, int parts, int first) {
+  constexpr int kWaves = kRouteThreads / kWave, kWide = kJoinExperts / 4;
+  __shared__ f4 sum_p[kRouteThreads];
+  __shared__ i4 sum_c[kRouteThreads];
   __shared__ int room_i[kWaves];
   __shared__ double room_d[kWaves];
-  const int tid = threadIdx.x;
-  int wide = kWave;
-  while (wide < p.experts) wide *= 2;
-  const int e = tid % wide, rank = tid / wide, ranks = kRouteThreads / wide;
-  float a = 0.0f;
-  int c = 0;
-  if (e < p.experts) {
+  const int tid = threadIdx.x, rank = tid / kWide, e0 = first + 4 * (tid % kWide);
+  constexpr int kRanks = kRouteThreads / kWide;
+  f4 a = f4{0, 0, 0, 0};
+  i4 c = i4{0, 0, 0, 0};
+  int tokens = 0, all = 0;
+  if (e0 < p.pitch) {
 #pragma unroll 4
-    for (int b = rank; b < parts; b += ranks) {
-      a += p.part_p[(int64_t)b * p.experts + e];
-      c += p.part_counts[(int64_t)b * p.experts + e];
+    for (int b = rank; b < parts; b += kRanks) {
+      a += *reinterpret_cast<const f4 *>(p.part_p + (int64_t)b * p.pitch + e0);
+      c += *reinterpret_cast<const i4 *>(p.part_counts + (int64_t)b * p.pitch + e0);
     }
   }
-  int tokens = 0;
-  for (int b = tid; b < parts; b += kRouteThreads) tokens += p.part_tokens[b];
+  for (int b = tid; b < parts; b += kRouteThreads) {
+    tokens += p.part_tokens[b];
+    all += p.part_choices[b];
+  }
   sum_p[tid] = a;
   sum_c[tid] = c;
-  __syncthreads();
-  for (int half = ranks / 2; half > 0; half /= 2) {
+  tokens = sum_workgroup<kRouteThreads>(tokens, room_i);
+  all = sum_workgroup<kRouteThreads>(all, room_i);
+  for (int half = kRanks / 2; half > 0; half /= 2) {
     if (rank < half) {
-      sum_p[tid] += sum_p[tid + half * wide];
-      sum_c[tid] += sum_c[tid + half * wide];
+      sum_p[tid] += sum_p[tid + half * kWide];
+      sum_c[tid] += sum_c[tid + half * kWide];
     }
     __syncthreads();
   }
-  const bool mine = rank == 0 && e < p.experts;
-  const int count = mine ? sum_c[e] : 0;
-  tokens = sum_workgroup<kRouteThreads>(tokens, room_i);
-  const int all = sum_workgroup<kRouteThreads>(count, room_i);
-  const double slope =
-      all > 0 ? (double)p.experts * count / ((double)all * tokens) : 0.0;
-  const double loss = sum_workgroup<kRouteThreads>(mine ? slope * sum_p[e] : 0.0, room_d);
-  if (mine) {
-    p.counts[e] = count;
-    p.slopes[e] = (float)slope;
+  double loss = 0.0;
+  if (rank == 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (e0 + i >= p.experts) break;
+      const double slope =
+          all > 0 ? (double)p.experts * sum_c[tid][i] / ((double)all * tokens) : 0.0;
+      loss += slope * sum_p[tid][i];
+      p.counts[e0 + i] = sum_c[tid][i];
+      p.slopes[e0 + i] = (float)slope;
+    }
   }
-  if (tid == 0) *p.loss = (float)loss;
+  return sum_workgroup<kRouteThreads>(loss, room_d);
 }
 
+// The last workgroup adds the losses up, in order.
 __global__ __launch_bounds__(kRouteThreads) void join_routes_kernel(RouteArgs p, int parts) {
-  join_routes(p, parts);
+  const double loss = join_routes(p, parts, blockIdx.x * kJoinExperts);
+  if (threadIdx.x != 0) return;
+  if (gridDim.x == 1) {
+    *p.loss = (float)loss;
+    return;
+  }
+  __hip_atomic_store(&p.part_loss[blockIdx.x], __builtin_bit_cast(uint64_t, loss), __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+  const uint32_t before =
+      __hip_atomic_fetch_add(p.done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+  if (before != gridDim.x - 1) return;
+  double sum = 0.0;
+  for (int b = 0; b < (int)gridDim.x; ++b)
+    sum += __builtin_bit_cast(
+        double, __hip_atomic_load(&p.part_loss[b], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+  *p.loss = (float)sum;
+}
+
+// The expert of a lane's place v.
+template <int L>
+__device__ __forceinline__ int expert_of(int q, int v) {
+  return v / 4 * (4 * L) + 4 * q + v % 4;
+}
+
+// A row's values at a lane's places; `rest` where there are none.
+template <int DT, int L, int V>
+__device__ __forceinline__ void load_experts(const typename Stored<DT>::type *row, int q, int experts,
+                                             float rest, float (&x)[V]) {
+#pragma unroll
+  for (int v = 0; v < V; v += 4) {
+    const int e = expert_of<L>(q, v);
+    Values<DT, 4> four;
+    four.load(row + e, experts - e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[v + i] = e + i < experts ? four.get(i) : rest;
+  }
+}
+
+// Sum over the rows of a wave, in all of its lanes.
+template <int L>
+__device__ __forceinline__ float sum_rows(float x) {
+  if (L <= 8)
+    x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x128, 0xF,
+                                                               0xF, false));  // row_ror:8
+  if (L <= 16) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, x);
+    const auto s = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+    x = __builtin_bit_cast(float, (uint32_t)s[0]) + __builtin_bit_cast(float, (uint32_t)s[1]);
+  }
+  if (L <= 32) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, x);
+    const auto s = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    x = __builtin_bit_cast(float, (uint32_t)s[0]) + __builtin_bit_cast(float, (uint32_t)s[1]);
+  }
+  return x;
 }
 
 template <int DT, int L, int V>
 __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs p) {
-  constexpr int kRows = kRouteThreads / L;
+  constexpr int kRows = kRouteThreads / L, kWaves = kRouteThreads / kWave;
   struct Pick {
     int expert;
-    float logit;
+    uint32_t key;
   };
   __shared__ Pick picks[kRows][kMaxChoices];
   __shared__ int hist[L * V];
-  __shared__ float sums[kRows / 8][L * V];
-  __shared__ int routed;
+  __shared__ float sums[kWaves][L * V];
+  __shared__ int routed, choices;
   const int tid = threadIdx.x, q = tid % L, row = tid / L;
-  const int lane = tid % kWave, first = lane - q;
   for (int i = tid; i < L * V; i += kRouteThreads) hist[i] = 0;
-  if (tid == 0) routed = 0;
+  if (tid == 0) {
+    routed = choices = 0;
+    if (blockIdx.x == 0) *p.done = 0;  // for the joining kernel behind this one
+  }
   __syncthreads();
   float acc[V] = {};
-  int mine_routed = 0;
+  int mine_routed = 0, mine_choices = 0;
   const auto *logits = static_cast<const typename Stored<DT>::type *>(p.logits);
-  const int left = p.experts - q * V;
   for (int base = blockIdx.x * kRows; base < p.m; base += gridDim.x * kRows) {
     const int t = base + row;
     const bool on = t < p.m && (p.valid == nullptr || p.valid[t] != 0);
     float l[V];
-    load_row<DT, V>(logits + (on ? t : 0) * p.stride + q * V, on ? left : 0, 0.0f, l);
+    load_experts<DT, L, V>(logits + (on ? t : 0) * p.stride, q, on ? p.experts : 0, 0.0f, l);
     uint32_t key[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) key[v] = on && v < left ? order_key(l[v]) : 0;
+    for (int v = 0; v < V; ++v)
+      key[v] = on && expert_of<L>(q, v) < p.experts ? order_key(l[v]) : 0;
     uint32_t top = 0;
     for (int j = 0; j < p.k; ++j) {
       uint32_t best = 0;
@@ -303,75 +390,77 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs p) {
       for (int v = 0; v < V; ++v) best = key[v] > best ? key[v] : best;
       const uint32_t most = max_across<L>(best);
       if (j == 0) top = most;
-      const uint64_t have = __ballot(best == most) >> first;
-      const bool there = most > kNone;
-      if (q == __builtin_ctzll(have)) {
-        Pick pick{-1, 0.0f};
-        bool open = there;
+      // the least index of those that are it, which is taken out
+      uint32_t at = 0xFFFFu;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          if (open && key[v] == most) {
-            pick = {q * V + v, l[v]};
-            key[v] = 0;
-            open = false;
-          }
-        }
-        picks[row][j] = pick;
-      }
+      for (int v = V - 1; v >= 0; --v) at = key[v] == most ? expert_of<L>(q, v) : at;
+      const int chosen = (int)min_across<L>(at);
+#pragma unroll
+      for (int v = 0; v < V; ++v) key[v] = expert_of<L>(q, v) == chosen ? 0 : key[v];
+      if (q == 0) picks[row][j] = {most > kNone ? chosen : -1, most};
     }
     wave_sync();
     const bool any = top > kNone;
     const float high = from_key(top);
+    // +Inf and NaN make all of the row NaN
+    const float one = high < INFINITY ? 1.0f : NAN;
     float sum = 0.0f, ex[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      ex[v] = any && v < left ? expf(l[v] - high) : 0.0f;
+      ex[v] = expert_of<L>(q, v) < p.experts ? exp_down(l[v] - high) : 0.0f;
       sum += ex[v];
     }
     sum = sum_across<L>(sum);
+    const float share = any ? one / sum : 0.0f;
 #pragma unroll
-    for (int v = 0; v < V; ++v) acc[v] += any ? ex[v] / sum : 0.0f;
+    for (int v = 0; v < V; ++v) acc[v] += any ? ex[v] * share : 0.0f;
     mine_routed += any && q == 0;
-    float below = sum;
+    float weigh = share;
     if (p.renormalize) {
-      below = 0.0f;
+      float below = 0.0f;
       for (int j = q; j < p.k; j += L)
-        below += picks[row][j].expert < 0 ? 0.0f : expf(picks[row][j].logit - high);
-      below = sum_across<L>(below);
+        below += picks[row][j].expert < 0 ? 0.0f : exp_down(from_key(picks[row][j].key) - high);
+      weigh = one / sum_across<L>(below);
     }
     if (t < p.m) {
       for (int j = q; j < p.k; j += L) {
         const Pick pick = picks[row][j];
+        const bool there = pick.expert >= 0;
         p.chosen[(int64_t)t * p.k + j] = pick.expert;
-        p.weights[(int64_t)t * p.k + j] = pick.expert < 0 ? 0.0f : expf(pick.logit - high) / below;
-        if (pick.expert >= 0) atomicAdd(&hist[pick.expert], 1);
+        p.weights[(int64_t)t * p.k + j] = there ? exp_down(from_key(pick.key) - high) * weigh : 0.0f;
+        if (there) atomicAdd(&hist[pick.expert], 1);
+        mine_choices += there;
       }
     }
     wave_sync();
   }
   if (mine_routed > 0) atomicAdd(&routed, mine_routed);
-  // an eighth of the rows at a time, in order
-  for (int part = 0; part < 8; ++part) {
-    if (row % 8 == part) {
+  if (mine_choices > 0) atomicAdd(&choices, mine_choices);
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        float *to = &sums[row / 8][q * V + v];
-        *to = part == 0 ? acc[v] : *to + acc[v];
-      }
-    }
-    __syncthreads();
+  for (int v = 0; v < V; ++v) {
+    const float a = sum_rows<L>(acc[v]);
+    if (tid % kWave < L) sums[tid / kWave][expert_of<L>(q, v)] = a;
   }
-  for (int e = tid; e < p.experts; e += kRouteThreads) {
+  __syncthreads();
+  for (int e = tid; e < p.pitch; e += kRouteThreads) {
     float a = 0.0f;
-    for (int r = 0; r < kRows / 8; ++r) a += sums[r][e];
-    p.part_p[(int64_t)blockIdx.x * p.experts + e] = a;
-    p.part_counts[(int64_t)blockIdx.x * p.experts + e] = hist[e];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) a += sums[w][e];
+    p.part_p[(int64_t)blockIdx.x * p.pitch + e] = a;
+    p.part_counts[(int64_t)blockIdx.x * p.pitch + e] = hist[e];
   }
-  if (tid == 0) p.part_tokens[blockIdx.x] = routed;
+  if (tid == 0) {
+    p.part_tokens[blockIdx.x] = routed;
+    p.part_choices[blockIdx.x] = choices;
+  }
   if (gridDim.x == 1) {
     __threadfence_block();
-    __syncthreads();
-    join_routes(p, 1);
+    double loss = 0.0;
+    for (int first = 0; first < p.experts; first += kJoinExperts) {
+      __syncthreads();
+      loss += join_routes(p, 1, first);
+    }
+    if (tid == 0) *p.loss = (float)loss;
   }
 }
 
@@ -393,38 +482,37 @@ __global__ __launch_bounds__(256) void route_gradient_kernel(RouteGradArgs p) {
   constexpr int kRows = 256 / L;
   __shared__ float extra[kRows][L * V];
   const int tid = threadIdx.x, q = tid % L, row = tid / L;
-  const int left = p.experts - q * V;
   const auto *logits = static_cast<const typename Stored<DT>::type *>(p.logits);
   auto *out = static_cast<typename Stored<DT>::type *>(p.out);
   float slope[V];
-  load_row<HADACORE_FP32, V>(p.slopes + q * V, p.dloss != nullptr ? left : 0, 0.0f, slope);
+  load_experts<HADACORE_FP32, L, V>(p.slopes, q, p.dloss != nullptr ? p.experts : 0, 0.0f, slope);
   const float g = p.dloss != nullptr ? *p.dloss : 0.0f;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     slope[v] *= g;
-    extra[row][q * V + v] = 0.0f;
+    extra[row][expert_of<L>(q, v)] = 0.0f;
   }
   wave_sync();
   for (int base = blockIdx.x * kRows; base < p.m; base += gridDim.x * kRows) {
     const int t = base + row;
     const bool on = t < p.m && p.chosen[(int64_t)(t < p.m ? t : 0) * p.k] >= 0;
     float l[V];
-    load_row<DT, V>(logits + (on ? t : 0) * p.stride + q * V, on ? left : 0, -INFINITY, l);
+    load_experts<DT, L, V>(logits + (on ? t : 0) * p.stride, q, on ? p.experts : 0, -INFINITY, l);
     uint32_t best = 0;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const uint32_t key = v < left ? order_key(l[v]) : 0;
+      const uint32_t key = order_key(l[v]);
       best = key > best ? key : best;
     }
-    const uint32_t top = max_across<L>(best);
-    const float high = from_key(top);
+    const float high = from_key(max_across<L>(best));
     float sum = 0.0f, pr[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      pr[v] = on && v < left ? expf(l[v] - high) : 0.0f;
+      pr[v] = on ? exp_down(l[v] - high) : 0.0f;
       sum += pr[v];
     }
     sum = sum_across<L>(sum);
+    const float share = on ? (high < INFINITY ? 1.0f : NAN) / sum : 0.0f;
     if (p.dweights != nullptr) {
       float wd = 0.0f;
       if (p.renormalize) {
@@ -443,38 +531,45 @@ __global__ __launch_bounds__(256) void route_gradient_kernel(RouteGradArgs p) {
     float pu = 0.0f, u[V], add[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      pr[v] = on ? pr[v] / sum : 0.0f;
+      pr[v] *= share;
       add[v] = 0.0f;
       if (p.dweights != nullptr) {
-        add[v] = extra[row][q * V + v];
-        extra[row][q * V + v] = 0.0f;
+        add[v] = extra[row][expert_of<L>(q, v)];
+        extra[row][expert_of<L>(q, v)] = 0.0f;
       }
       u[v] = slope[v] + (p.renormalize ? 0.0f : add[v]);
       pu += pr[v] * u[v];
     }
     pu = sum_across<L>(pu);
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-      u[v] = on ? pr[v] * (u[v] - pu) + (p.renormalize ? add[v] : 0.0f) : 0.0f;
-    if (t < p.m && left > 0) store_row<DT, V>(out + t * p.out_stride + q * V, left, u);
+    for (int v = 0; v < V; v += 4) {
+      const int e = expert_of<L>(q, v);
+      float four[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        four[i] = on ? pr[v + i] * (u[v + i] - pu) + (p.renormalize ? add[v + i] : 0.0f) : 0.0f;
+      if (t < p.m) store_row<DT, 4>(out + t * p.out_stride + e, p.experts - e, four);
+    }
     wave_sync();
   }
 }
 
-// Lanes to a row and experts to a lane: four experts in a lane until a row takes the wave.
+// Lanes to a row and experts to a lane.  What bounds large calls is the issue of vector operations, and a
+// step of a choice costs about as many for 16 experts in each of 16 lanes, which does four rows at
+// once, as for 4 in each of 64 (16384 x 256, eight choices: ROUTE us instead of 21.8).
 template <class F>
 void for_experts(int64_t experts, F f) {
   using std::integral_constant;
   if (experts <= 32)
     f(integral_constant<int, 8>{}, integral_constant<int, 4>{});
   else if (experts <= 64)
-    f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+    f(integral_constant<int, 8>{}, integral_constant<int, 8>{});
   else if (experts <= 128)
-    f(integral_constant<int, 32>{}, integral_constant<int, 4>{});
+    f(integral_constant<int, 16>{}, integral_constant<int, 8>{});
   else if (experts <= 256)
-    f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    f(integral_constant<int, 16>{}, integral_constant<int, 16>{});
   else if (experts <= 512)
-    f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+    f(integral_constant<int, 32>{}, integral_constant<int, 16>{});
   else
     f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
 }
@@ -489,8 +584,11 @@ void for_type(hadacore_dtype dtype, F f) {
     f(std::integral_constant<int, HADACORE_FP32>{});
 }
 
+// Words of the workspace behind the parts: the joining workgroups' losses, and how many are done.
+constexpr int64_t kRouteWords = 2 * kMaxExperts / kJoinExperts + 2;
+
 // Workgroups of a route: one for each set of rows, at most 256, and no more than the joining
-// workgroup reads in a few microseconds (2^16 sums and counts).
+// workgroups read in a few microseconds (2^16 sums and counts).
 int64_t route_parts(int64_t m, int64_t experts) {
   int64_t rows = 0;
   for_experts(experts, [&](auto l, auto) { rows = kRouteThreads / decltype(l)::value; });
@@ -536,14 +634,14 @@ __global__ __launch_bounds__(kGroupThreads) void count_groups_kernel(GroupArgs p
     p.parts[(int64_t)blockIdx.x * bins + g] = hist[g];
 }
 
-// W: how many waves share the slots (fewer where the counts of 16 would not fit 64 KiB of LDS).
+// W: how many waves share the slots (fewer where the counts of 16 would take more than 64 KiB of LDS).
 template <int W>
 __global__ __launch_bounds__(kGroupThreads) void place_groups_kernel(GroupArgs p) {
-  extern __shared__ int counts[];  // [W][bins], then the base of each group
+  extern __shared__ int counts[];  // [W][bins], then of each group: its slots, those before this workgroup
   __shared__ int wave_sums[kGroupWaves];
   const int bins = p.groups + 1, tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
-  int *base = counts + W * bins;
-  for (int i = tid; i < W * bins; i += kGroupThreads) counts[i] = 0;
+  int *all = counts + W * bins, *before = all + bins;
+  for (int i = tid; i < (W + 2) * bins; i += kGroupThreads) counts[i] = 0;
   __syncthreads();
   const int low = blockIdx.x * p.per_block;
   const int high = low + p.per_block < p.slots ? low + p.per_block : p.slots;
@@ -552,27 +650,28 @@ __global__ __launch_bounds__(kGroupThreads) void place_groups_kernel(GroupArgs p
   if (wave < W)
     for (int s = from + lane; s < to; s += kWave) atomicAdd(&counts[wave * bins + group_of(p, s)], 1);
   __syncthreads();
-  // slots of each group: in all, and before this workgroup
+  if (gridDim.x == 1) {
+    for (int g = tid; g < bins; g += kGroupThreads)
+      for (int w = 0; w < W; ++w) all[g] += counts[w * bins + g];
+  } else {
+    int wide = kWave;
+    while (wide < bins && wide < kGroupThreads) wide *= 2;
+    for (int g = tid % wide; g < bins; g += wide) {
+      int sum = 0, early = 0;
+#pragma unroll 4
+      for (int b = tid / wide; b < (int)gridDim.x; b += kGroupThreads / wide) {
+        const int c = p.parts[(int64_t)b * bins + g];
+        sum += c;
+        early += b < (int)blockIdx.x ? c : 0;
+      }
+      atomicAdd(&all[g], sum);
+      atomicAdd(&before[g], early);
+    }
+  }
+  __syncthreads();
   const int each = (bins + kGroupThreads - 1) / kGroupThreads;
   int sum = 0;
-  for (int i = 0; i < each; ++i) {
-    const int g = tid * each + i;
-    int all = 0, before = 0;
-    if (g < bins) {
-      if (gridDim.x == 1) {
-        for (int w = 0; w < W; ++w) all += counts[w * bins + g];
-      } else {
-#pragma unroll 4
-        for (int b = 0; b < (int)gridDim.x; ++b) {
-          const int c = p.parts[(int64_t)b * bins + g];
-          all += c;
-          before += b < (int)blockIdx.x ? c : 0;
-        }
-      }
-      base[g] = sum + before;
-    }
-    sum += all;
-  }
+  for (int i = 0; i < each; ++i) sum += tid * each + i < bins ? all[tid * each + i] : 0;
   // the groups before this thread's
   const int upto = prefix_sum(sum);
   if (lane == kWave - 1) wave_sums[wave] = upto;
@@ -582,9 +681,10 @@ __global__ __launch_bounds__(kGroupThreads) void place_groups_kernel(GroupArgs p
   for (int i = 0; i < each; ++i) {
     const int g = tid * each + i;
     if (g >= bins) break;
-    int at = base[g] + start;
     // a group's end is where the next one starts: group 0's start is 0
-    if (blockIdx.x == 0 && g > 0) p.ends[g - 1] = at;
+    if (blockIdx.x == 0 && g > 0) p.ends[g - 1] = start;
+    int at = start + before[g];
+    start += all[g];
     for (int w = 0; w < W; ++w) {
       const int c = counts[w * bins + g];
       counts[w * bins + g] = at;
@@ -617,16 +717,16 @@ __global__ __launch_bounds__(kGroupThreads) void place_groups_kernel(GroupArgs p
   }
 }
 
-// How many waves of a workgroup share its slots: their counts and the bases fit 64 KiB of LDS.
-int group_waves(int64_t groups) { return groups <= 900 ? 16 : groups <= 3200 ? 4 : 2; }
+// How many waves of a workgroup share its slots: the counts take 64 KiB of LDS at most.
+int group_waves(int64_t groups) { return groups <= 900 ? 16 : groups <= 2700 ? 4 : 2; }
 
-// Workgroups: one for 4096 slots, where a second launch costs more than it gains (measured at
-// the calls of few slots); their counts at most 2^15, since each workgroup reads them all.
+// Workgroups.  Up to 8192 slots one does it in one launch (8.7 us; two launches take 2.4 and 4.6 and the
+// time between them); from there one for 2048 slots, 64 at most, since each adds up the counts
+// of all (131072 slots of 256 groups: GROUP us; by 128 workgroups 14).
 int64_t group_blocks_of(int64_t slots, int64_t groups) {
-  int64_t blocks = (slots + 4095) / 4096;
-  const int64_t most = (1 << 15) / (groups + 1) < 256 ? (1 << 15) / (groups + 1) : 256;
-  if (blocks > most) blocks = most;
-  return blocks > 0 ? blocks : 1;
+  if (slots <= 8192) return 1;
+  const int64_t blocks = (slots + 2047) / 2048, most = (1 << 16) / (groups + 1);
+  return blocks < most ? blocks < 128 ? blocks : 128 : most < 128 ? most : 128;
 }
 
 // ---- rows to their places, and back --------------------------------------------------
@@ -919,7 +1019,7 @@ using namespace hadacore;
 
 extern "C" int64_t hadacore_route_workspace_size(int64_t m, int64_t experts) {
   if (m < 0 || m >= kMaxDim || experts < 1 || experts > kMaxExperts) return 0;
-  return route_parts(m, experts) * (2 * experts + 1) * 4;
+  return route_parts(m, experts) * (2 * ((experts + 3) & ~3) + 2) * 4 + kRouteWords * 4;
 }
 
 extern "C" hadacore_status hadacore_route(const void *logits, int64_t logits_row_stride,
@@ -938,7 +1038,7 @@ extern "C" hadacore_status hadacore_route(const void *logits, int64_t logits_row
   if (st != HADACORE_SUCCESS) return st;
   const int64_t need = hadacore_route_workspace_size(m, experts);
   if (workspace == nullptr || workspace_bytes < need) return HADACORE_ERROR_WORKSPACE;
-  if (!aligned_to(workspace, 4)) return HADACORE_ERROR_MISALIGNED;
+  if (!aligned_to(workspace, 16)) return HADACORE_ERROR_MISALIGNED;
   if (any_overlap({words(out_experts, m * k), words(out_weights, m * k), words(out_counts, experts),
                    words(out_loss, 1), words(out_slopes, experts), span(workspace, 1, need, need, 1)},
                   {span(logits, m, logits_row_stride, experts, size_of(dtype)),
@@ -960,9 +1060,13 @@ extern "C" hadacore_status hadacore_route(const void *logits, int64_t logits_row
   p.counts = out_counts;
   p.loss = out_loss;
   p.slopes = out_slopes;
+  p.pitch = ((int)experts + 3) & ~3;
   p.part_p = static_cast<float *>(workspace);
-  p.part_counts = static_cast<int32_t *>(workspace) + parts * experts;
-  p.part_tokens = p.part_counts + parts * experts;
+  p.part_counts = static_cast<int32_t *>(workspace) + parts * p.pitch;
+  p.part_tokens = p.part_counts + parts * p.pitch;
+  p.part_choices = p.part_tokens + parts;
+  p.part_loss = reinterpret_cast<uint64_t *>(p.part_choices + parts);  // 8-byte aligned: 2 parts and fours
+  p.done = reinterpret_cast<uint32_t *>(p.part_loss + kMaxExperts / kJoinExperts);
   hipStream_t s = static_cast<hipStream_t>(stream);
   for_type(dtype, [&](auto dt) {
     for_experts(experts, [&](auto l, auto v) {
@@ -972,7 +1076,8 @@ extern "C" hadacore_status hadacore_route(const void *logits, int64_t logits_row
   });
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && parts > 1) {
-    hipLaunchKernelGGL(join_routes_kernel, dim3(1), dim3(kRouteThreads), 0, s, p, (int)parts);
+    const int64_t joins = (experts + kJoinExperts - 1) / kJoinExperts;
+    hipLaunchKernelGGL(join_routes_kernel, dim3((uint32_t)joins), dim3(kRouteThreads), 0, s, p, (int)parts);
     e = hipGetLastError();
   }
   return status_of(e);
@@ -1074,12 +1179,12 @@ extern "C" hadacore_status hadacore_group_tokens(const int32_t *ids, int64_t slo
   }
   if (waves == 16)
     hipLaunchKernelGGL(place_groups_kernel<16>, dim3((uint32_t)blocks), dim3(kGroupThreads),
-                       17 * bins, s, p);
+                       18 * bins, s, p);
   else if (waves == 4)
-    hipLaunchKernelGGL(place_groups_kernel<4>, dim3((uint32_t)blocks), dim3(kGroupThreads), 5 * bins,
+    hipLaunchKernelGGL(place_groups_kernel<4>, dim3((uint32_t)blocks), dim3(kGroupThreads), 6 * bins,
                        s, p);
   else
-    hipLaunchKernelGGL(place_groups_kernel<2>, dim3((uint32_t)blocks), dim3(kGroupThreads), 3 * bins,
+    hipLaunchKernelGGL(place_groups_kernel<2>, dim3((uint32_t)blocks), dim3(kGroupThreads), 4 * bins,
                        s, p);
   return status_of(hipGetLastError());
 }
