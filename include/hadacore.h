@@ -519,7 +519,7 @@ hadacore_status hadacore_combine_gradient(const void *dout, int64_t dout_row_str
                                           float *dweights, int64_t m, int64_t k, int64_t width,
                                           void *stream);
 
-/* Bytes of workspace of hadacore_adapters (0 for arguments that it rejects). */
+/* Bytes of workspace of hadacore_adapters (0 for few tokens, and for arguments that it rejects). */
 int64_t hadacore_adapters_workspace_size(int64_t m, int64_t k, int64_t n, int64_t rank,
                                          int64_t groups);
 

@@ -395,6 +395,8 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
   const int count = piece.high - piece.low < p.unit ? piece.high - piece.low : p.unit;
   const int col = (chunk * 4 + wave) * (kTile * CT) + c * CT;
   const int64_t valid = EVEN ? CT : (int64_t)p.n - col;
+  // a wave behind the last column loads the first ones in their place
+  const bool behind = (chunk * 4 + wave) * (kTile * CT) >= p.n;
   uint32_t raw[RB][8][CT / 2];
   if (!bare) {
 #pragma unroll
@@ -403,7 +405,8 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
       for (int j = 0; j < 8; ++j) {
         const int row = b * kStep + quarter * 8 + j;
         // ranks that are not there: any values, cleared below
-        load_columns<CT>(p.up + piece.group * p.up_batch + (row < p.rank ? row : 0) * p.up_stride + col,
+        load_columns<CT>(p.up + piece.group * p.up_batch + (row < p.rank ? row : 0) * p.up_stride +
+                             (EVEN && behind ? c * CT : col),
                          valid, raw[b][j]);
       }
   }
@@ -412,7 +415,7 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
   using Row = OutRow<OUT, CT, EVEN>;
   // Whole tiles of 16 tokens whose columns are all there go without a branch in a lane, so that
   // loads stay in flight over stores and products.
-  const bool whole = EVEN || (chunk * 4 + wave + 1) * (kTile * CT) <= p.n;
+  const bool whole = (chunk * 4 + wave + 1) * (kTile * CT) <= p.n;
   const int fast = whole && y != nullptr ? count / kTile * kTile : 0;
   Row old[D][4];
 #pragma unroll
@@ -495,7 +498,7 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
   }
   __syncthreads();
   // whole waves only: a matrix instruction reads the registers of all 64 lanes
-  if ((chunk * 4 + wave) * (kTile * CT) >= p.n) return;
+  if (behind) return;
   const auto multiply = [&](int t0, f4 (&acc)[CT]) {
     if (bare) return;
 #pragma unroll
@@ -551,6 +554,163 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
       add(t, v, acc, rest[v]);
       rest[v].store(out + (tokens[t] * p.out_stride + col) * kSize, valid);
     }
+  }
+}
+
+// Both products in one launch, for up to 16 tokens of a group and 1024 columns: every workgroup makes
+// h itself, which costs it the group's `down` again (from the L2) but saves a launch and the
+// way of h through memory.  Eight waves share k and add up; then each has its 128 columns, whose weights
+// and y were loaded at the start.  Called one by one 1 token of rank 16, 4096 x 4096 takes 9.5 us
+// instead of 13, and 64 tokens of 32 adapters 10.8 instead of 13; inside a graph, where a launch
+// costs little, 8.5 instead of 7.3 and 11.0 instead of 9.3.  For ranks up to 16 and few workgroups:
+// 256 tokens of 64 adapters gain nothing, rank 64 takes 20 instead of 9.
+constexpr int kFewWaves = 8;
+
+template <int DT, int OUT, int P, bool EVEN>
+__global__ __launch_bounds__(kFewWaves *kWave) void few_tokens_kernel(AdapterArgs p) {
+  constexpr int CT = 8, U = 4, kPitch = kStep + 8;
+  constexpr int kSize = OUT == HADACORE_FP32 ? 4 : 2;
+  __shared__ f4 sums[kFewWaves][kWave];
+  __shared__ __attribute__((aligned(16))) float hs[kTile][kTile + 4];
+  __shared__ __attribute__((aligned(16))) uint16_t parts[P][kTile][kPitch];
+  __shared__ float back[kTile];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int c = lane % kTile, quarter = lane / kTile;
+  const int chunk = blockIdx.x % p.chunks;
+  const Piece piece = piece_of(p.ends, p.groups, p.m, kTile, blockIdx.x / p.chunks, true);
+  if (piece.group < 0) return;
+  const bool bare = piece.group == p.groups;  // no adapter
+  if (bare && p.y == p.out) return;
+  const int count = piece.high - piece.low < kTile ? piece.high - piece.low : kTile;
+  const int col = (chunk * kFewWaves + wave) * (kTile * CT) + c * CT;
+  const int64_t valid = EVEN ? (col < p.n ? CT : 0) : (int64_t)p.n - col;
+  using Row = OutRow<OUT, CT, false>;
+  const uint8_t *y = static_cast<const uint8_t *>(p.y);
+  uint8_t *out = static_cast<uint8_t *>(p.out);
+  int token[4];
+  Row old[4];
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    const int t = 4 * quarter + v;
+    token[v] = token_of(p.slots, piece.low + (t < count ? t : 0), p.m);
+    old[v].clear();
+    if (y != nullptr && t < count && valid > 0)
+      old[v].load(y + (token[v] * p.y_stride + col) * kSize, EVEN ? CT : valid);
+  }
+  f4 acc[CT] = {};
+  if (!bare) {
+    uint32_t raw[8][CT / 2];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int row = quarter * 8 + j;
+      // ranks and columns that are not there: any values, cleared below or not stored
+      load_columns<CT>(p.up + piece.group * p.up_batch + (row < p.rank ? row : 0) * p.up_stride +
+                           (EVEN && valid == 0 ? 0 : col),
+                       EVEN ? CT : valid, raw[j]);
+    }
+    const int64_t steps = p.k / kStep;
+    const int from = (int)(steps * wave / kFewWaves), to = (int)(steps * (wave + 1) / kFewWaves);
+    const int mine = piece.low + (c < count ? c : count - 1);
+    const uint16_t *xp = p.x + token_of(p.slots, mine, p.m) * p.x_stride + quarter * 8;
+    const uint16_t *wp = p.down + piece.group * p.down_batch +
+                         (c < p.rank ? c : p.rank - 1) * p.down_stride + quarter * 8;
+    f4 h = f4{0, 0, 0, 0};
+    u4 xv[2][U], wv[2][U];
+    const auto load = [&](int s, int now) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t at = (int64_t)(s + u) * kStep;
+        xv[now][u] = *reinterpret_cast<const u4_any *>(xp + at);
+        wv[now][u] = *reinterpret_cast<const u4_any *>(wp + at);
+      }
+    };
+    const auto multiply = [&](int now) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) h = mfma<DT>(wv[now][u], xv[now][u], h);
+    };
+    const int turns = (to - from) / U;
+    if (turns > 0) load(from, 0);
+    for (int i = 0; i < turns; i += 2) {
+      if (i + 1 < turns) load(from + (i + 1) * U, 1);
+      multiply(0);
+      if (i + 1 >= turns) break;
+      if (i + 2 < turns) load(from + (i + 2) * U, 0);
+      multiply(1);
+    }
+    int s = from + turns * U;
+    // the rest of k by the last wave
+    const int last = to + (wave == kFewWaves - 1 && p.k % kStep != 0);
+#pragma unroll 1
+    for (; s < last; ++s) {
+      const int there = (s < to ? kStep : p.k % kStep) - quarter * 8;
+      h = mfma<DT>(load8(wp + (int64_t)s * kStep, there), load8(xp + (int64_t)s * kStep, there), h);
+    }
+    sums[wave][lane] = h;
+    __syncthreads();
+    if (wave == 0) {
+      f4 v = sums[0][lane];
+#pragma unroll
+      for (int w = 1; w < kFewWaves; ++w) v += sums[w][lane];
+      const int rank = 4 * quarter;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (rank + j >= p.rank) v[j] = 0.0f;
+      *reinterpret_cast<f4 *>(&hs[c][rank]) = v;
+      if (p.hidden != nullptr && chunk == 0 && c < count)
+        *reinterpret_cast<f4 *>(p.hidden + (int64_t)(piece.low + c) * p.hidden_stride + rank) = v;
+    }
+    u4 w[CT];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int i = 0; i < CT / 2; ++i) raw[j][i] = quarter * 8 + j < p.rank ? raw[j][i] : 0;
+    turn<CT>(raw, w);
+    __syncthreads();
+    if (tid < 256) {
+      const int t = tid / kTile, q = tid % kTile, r = 4 * q;
+      const float scale = p.scales != nullptr ? p.scales[piece.group] : 1.0f;
+      f4 v = f4{0, 0, 0, 0};
+      if (r < kTile) v = *reinterpret_cast<const f4 *>(&hs[t][r]);
+      float most = 0.0f, shift = 1.0f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[j] *= scale;
+        most = fmaxf(most, fabsf(v[j]));
+      }
+      if constexpr (DT == HADACORE_FP16) {
+        const int e = scale_exponent(max_lanes(most, kTile));
+        shift = power_of_two(-e);
+        if (q == 0) back[t] = power_of_two(e);
+      }
+      if (r < kStep) {
+        uint16_t part[4][P];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) split<DT, P>(v[j] * shift, part[j]);
+#pragma unroll
+        for (int k = 0; k < P; ++k)
+          *reinterpret_cast<u2 *>(&parts[k][t][r]) =
+              u2{part[0][k] | (uint32_t)part[1][k] << 16, part[2][k] | (uint32_t)part[3][k] << 16};
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = P - 1; k >= 0; --k) {
+      const u4 a = *reinterpret_cast<const u4 *>(&parts[k][c][quarter * 8]);
+#pragma unroll
+      for (int i = 0; i < CT; ++i) acc[i] = mfma<DT>(a, w[i], acc[i]);
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    const int t = 4 * quarter + v;
+    if (t >= count || valid <= 0) continue;
+    const float unshift = DT == HADACORE_FP16 && !bare ? back[t] : 1.0f;
+    float sum[CT];
+#pragma unroll
+    for (int i = 0; i < CT; ++i) sum[i] = fmaf(acc[i][v], unshift, old[v].get(i));
+    Row row;
+    row.set(sum);
+    row.store(out + (token[v] * p.out_stride + col) * kSize, EVEN ? CT : valid);
   }
 }
 
@@ -843,7 +1003,11 @@ int64_t most_pieces(int64_t m, int64_t groups, int64_t unit) {
   return m / unit + (groups < m ? groups : m) + 1;
 }
 
+// Workgroups of few_tokens_kernel at most, and the longest k of which each makes its own h.
+constexpr int64_t kFewBlocks = 192, kFewDepth = 8192;
+
 struct Cut {
+  bool fused;  // few_tokens_kernel
   int ranks;   // tiles of ranks in a workgroup of down_kernel
   int tiles;   // tiles of tokens there
   int splits;  // shares of k
@@ -856,6 +1020,11 @@ Cut cut_of(int64_t m, int64_t k, int64_t n, int64_t rank, int64_t groups, int pa
   const int64_t live = groups < 1 || m < 1 ? 1 : groups < m ? groups : m;
   const bool few = m <= 32 * live;
   cut.tiles = few ? 1 : cut.ranks == 8 ? 2 : 4;
+  cut.splits = 1;
+  cut.unit = kTile;
+  cut.fused = few && rank <= kTile && k <= kFewDepth &&
+              most_pieces(m, groups, kTile) * divide_up(n, kFewWaves * 128) <= kFewBlocks;
+  if (cut.fused) return cut;
   const int64_t blocks =
       (divide_up(m, 16 * cut.tiles) + live - 1) * divide_up(rank, 16 * cut.ranks);
   // with four tiles of ranks a wave takes a whole SIMD: a workgroup to a CU
@@ -945,7 +1114,7 @@ void launch_up(AdapterArgs p, hipStream_t stream) {
     // XCDs (or a multiple) each of them meets only its own columns of the weights
     p.chunks = p.n > 0 ? (int)divide_up(p.n, 4 * 16 * CT) : 1;  // without columns h is joined
     const dim3 grid((uint32_t)(pieces * p.chunks));
-    if (p.n % (16 * CT) == 0 && lines)
+    if (p.n > 0 && p.n % (16 * CT) == 0 && lines)
       hipLaunchKernelGGL((up_kernel<DT, OUT, RB, CT, P, kAhead, true>), grid, dim3(256), lds, stream, p);
     else
       hipLaunchKernelGGL((up_kernel<DT, OUT, RB, CT, P, kAhead, false>), grid, dim3(256), lds, stream, p);
@@ -960,6 +1129,17 @@ void launch_up(AdapterArgs p, hipStream_t stream) {
     go(integral_constant<int, 4>{}, eight);
   else
     go(eight, integral_constant<int, 4>{});
+}
+
+template <int DT, int OUT>
+void launch_few(AdapterArgs p, hipStream_t stream) {
+  constexpr int P = parts_of(DT, OUT);
+  p.chunks = p.n > 0 ? (int)divide_up(p.n, kFewWaves * 128) : 1;
+  const dim3 grid((uint32_t)(most_pieces(p.m, p.groups, kTile) * p.chunks));
+  if (p.n > 0 && p.n % 128 == 0)
+    hipLaunchKernelGGL((few_tokens_kernel<DT, OUT, P, true>), grid, dim3(kFewWaves * kWave), 0, stream, p);
+  else
+    hipLaunchKernelGGL((few_tokens_kernel<DT, OUT, P, false>), grid, dim3(kFewWaves * kWave), 0, stream, p);
 }
 
 template <int DT, int OUT>
@@ -1050,8 +1230,8 @@ using namespace hadacore;
 extern "C" int64_t hadacore_adapters_workspace_size(int64_t m, int64_t k, int64_t n, int64_t rank,
                                                     int64_t groups) {
   if (check_sizes(m, k, n, rank, groups) != HADACORE_SUCCESS) return 0;
-  const int64_t splits = cut_of(m, k, n, rank, groups, 2).splits;
-  return splits * m * round_up(rank, 16) * 4;
+  const Cut cut = cut_of(m, k, n, rank, groups, 2);
+  return cut.fused ? 0 : cut.splits * m * round_up(rank, 16) * 4;
 }
 
 extern "C" hadacore_status hadacore_adapters(
@@ -1084,11 +1264,12 @@ extern "C" hadacore_status hadacore_adapters(
   }
   if (m == 0) return HADACORE_SUCCESS;
   const int64_t need = hadacore_adapters_workspace_size(m, k, n, rank, groups);
-  if (workspace == nullptr || workspace_bytes < need) return HADACORE_ERROR_WORKSPACE;
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return HADACORE_ERROR_WORKSPACE;
   if (!aligned_to(workspace, 16)) return HADACORE_ERROR_MISALIGNED;
   const Span so = matrices(out, 1, 0, m, out_row_stride, n, size),
              sh = matrices(hidden, 1, 0, m, hidden_row_stride, padded, 4),
-             sw = span(workspace, 1, need, need, 1), sy = matrices(y, 1, 0, m, y_row_stride, n, size);
+             sw = span(workspace, need > 0, need, need, 1),
+             sy = matrices(y, 1, 0, m, y_row_stride, n, size);
   const Span in[] = {matrices(x, 1, 0, m, x_row_stride, k, 2),
                      matrices(down, groups, down_batch_stride, rank, down_row_stride, k, 2),
                      matrices(up, groups, up_batch_stride, rank, up_row_stride, n, 2),
@@ -1136,11 +1317,22 @@ extern "C" hadacore_status hadacore_adapters(
   p.padded = (int)padded;
   p.groups = (int)groups;
   hipStream_t s = static_cast<hipStream_t>(stream);
+  if (n == 0 && (hidden == nullptr || groups == 0)) return HADACORE_SUCCESS;
+  if (cut.fused) {
+    for_type(dtype, [&](auto dt) {
+      constexpr int DT = decltype(dt)::value;
+      if (out_dtype == HADACORE_FP32)
+        launch_few<DT, HADACORE_FP32>(p, s);
+      else
+        launch_few<DT, DT>(p, s);
+    });
+    return hipGetLastError() == hipSuccess ? HADACORE_SUCCESS : HADACORE_ERROR_LAUNCH;
+  }
   if (groups > 0) {
     for_type(dtype, [&](auto dt) { launch_down<decltype(dt)::value>(p, cut, s); });
     if (hipGetLastError() != hipSuccess) return HADACORE_ERROR_LAUNCH;
   }
-  if (n == 0 && (hidden == nullptr || direct)) return HADACORE_SUCCESS;
+  if (n == 0 && direct) return HADACORE_SUCCESS;
   for_type(dtype, [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
     if (out_dtype == HADACORE_FP32)

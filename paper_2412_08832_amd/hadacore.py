@@ -1217,12 +1217,13 @@ def adapt_rows(x, down, up, ends=None, slots=None, y=None, scales=None, out=None
     if hidden:
         h = _torch.empty_strided((m, padded), (padded, 1), dtype=_float32, device=where)
         h_ptr = h.data_ptr()
-    need = _adapters_workspace(m, k, n, rank, groups)
-    workspace = _words(need >> 2, where)
+    need, workspace = _adapters_workspace(m, k, n, rank, groups), None
+    if need:
+        workspace = _words(need >> 2, where)
     _call("hadacore_adapters", device, x.data_ptr(), x_stride, down.data_ptr(), down_stride,
           down.stride(0), up.data_ptr(), up_stride, up.stride(0), scales_ptr, ends_ptr, slots_ptr,
           groups, y_ptr, y_stride, out.data_ptr(), _row_stride(out, n), code, _out_codes[dtype], h_ptr,
-          padded, m, k, n, rank, workspace.data_ptr(), need, _stream_of(stream, device))
+          padded, m, k, n, rank, workspace.data_ptr() if need else None, need, _stream_of(stream, device))
     if not hidden:
         return out
     return out, h if padded == rank else h.narrow(1, 0, rank)
