@@ -434,7 +434,7 @@ hadacore_status hadacore_weight_gradient_fp8_grouped(
 #define HADACORE_MAX_GROUPS 4095
 #define HADACORE_MAX_RANK 256
 
-/* Bytes of workspace of hadacore_route (0 for arguments that it rejects). */
+/* Bytes of workspace of hadacore_route (0 for few tokens, and for arguments that it rejects). */
 int64_t hadacore_route_workspace_size(int64_t m, int64_t experts);
 
 /*

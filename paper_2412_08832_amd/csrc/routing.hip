@@ -361,14 +361,14 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs p) {
     uint32_t key;
   };
   __shared__ Pick picks[kRows][kMaxChoices];
-  __shared__ int hist[L * V];
-  __shared__ float sums[kWaves][L * V];
+  __shared__ __attribute__((aligned(16))) int hist[L * V];
+  __shared__ __attribute__((aligned(16))) float sums[kWaves][L * V];
   __shared__ int routed, choices;
   const int tid = threadIdx.x, q = tid % L, row = tid / L;
   for (int i = tid; i < L * V; i += kRouteThreads) hist[i] = 0;
   if (tid == 0) {
     routed = choices = 0;
-    if (blockIdx.x == 0) *p.done = 0;  // for the joining kernel behind this one
+    if (blockIdx.x == 0 && gridDim.x > 1) *p.done = 0;  // for the joining kernel behind this one
   }
   __syncthreads();
   float acc[V] = {};
@@ -442,23 +442,32 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs p) {
     if (tid % kWave < L) sums[tid / kWave][expert_of<L>(q, v)] = a;
   }
   __syncthreads();
+  const bool alone = gridDim.x == 1;  // then nothing goes through the workspace
   for (int e = tid; e < p.pitch; e += kRouteThreads) {
     float a = 0.0f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) a += sums[w][e];
-    p.part_p[(int64_t)blockIdx.x * p.pitch + e] = a;
-    p.part_counts[(int64_t)blockIdx.x * p.pitch + e] = hist[e];
+    if (alone) {
+      sums[0][e] = a;
+    } else {
+      p.part_p[(int64_t)blockIdx.x * p.pitch + e] = a;
+      p.part_counts[(int64_t)blockIdx.x * p.pitch + e] = hist[e];
+    }
   }
-  if (tid == 0) {
+  if (tid == 0 && !alone) {
     p.part_tokens[blockIdx.x] = routed;
     p.part_choices[blockIdx.x] = choices;
   }
-  if (gridDim.x == 1) {
-    __threadfence_block();
+  if (alone) {
+    RouteArgs here = p;
+    here.part_p = sums[0];
+    here.part_counts = hist;
+    here.part_tokens = &routed;
+    here.part_choices = &choices;
     double loss = 0.0;
     for (int first = 0; first < p.experts; first += kJoinExperts) {
       __syncthreads();
-      loss += join_routes(p, 1, first);
+      loss += join_routes(here, 1, first);
     }
     if (tid == 0) *p.loss = (float)loss;
   }
@@ -1019,7 +1028,8 @@ using namespace hadacore;
 
 extern "C" int64_t hadacore_route_workspace_size(int64_t m, int64_t experts) {
   if (m < 0 || m >= kMaxDim || experts < 1 || experts > kMaxExperts) return 0;
-  return route_parts(m, experts) * (2 * ((experts + 3) & ~3) + 2) * 4 + kRouteWords * 4;
+  const int64_t parts = route_parts(m, experts);
+  return parts > 1 ? parts * (2 * ((experts + 3) & ~3) + 2) * 4 + kRouteWords * 4 : 0;
 }
 
 extern "C" hadacore_status hadacore_route(const void *logits, int64_t logits_row_stride,
@@ -1037,10 +1047,11 @@ extern "C" hadacore_status hadacore_route(const void *logits, int64_t logits_row
                     check_words(out_slopes, experts)});
   if (st != HADACORE_SUCCESS) return st;
   const int64_t need = hadacore_route_workspace_size(m, experts);
-  if (workspace == nullptr || workspace_bytes < need) return HADACORE_ERROR_WORKSPACE;
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return HADACORE_ERROR_WORKSPACE;
   if (!aligned_to(workspace, 16)) return HADACORE_ERROR_MISALIGNED;
   if (any_overlap({words(out_experts, m * k), words(out_weights, m * k), words(out_counts, experts),
-                   words(out_loss, 1), words(out_slopes, experts), span(workspace, 1, need, need, 1)},
+                   words(out_loss, 1), words(out_slopes, experts),
+                   span(workspace, need > 0, need, need, 1)},
                   {span(logits, m, logits_row_stride, experts, size_of(dtype)),
                    span(valid, valid != nullptr, m, m, 1)}))
     return HADACORE_ERROR_OVERLAP;

@@ -24,6 +24,20 @@ backward's codes are of w, for which quantize_weights takes one pass more over t
 
 ``python -m paper_2412_08832_amd.experts`` runs a small layer of experts forward and
 backward on the GPU and prints its errors against 32 bits, with and without the rotation.
+
+A mixture of experts around such layers: ``route`` chooses each token's experts from a router's
+logits (with the balance loss), ``hadacore.group_tokens`` sorts the (token, choice) slots by
+expert, ``dispatch`` copies the tokens' rows there and ``combine`` joins the layer's rows by weight,
+each with gradients.  ``mixture`` is one layer of it for training, ``serve_mixture`` for serving: that
+quantizes every token once and dispatches codes.
+
+    routes = route(logits, k, valid=valid)
+    groups = hadacore.group_tokens(routes.experts, experts)
+    out = combine(train_linear(dispatch(x, groups), w, groups.ends), groups, routes.weights)
+    loss = task_loss(out) + 0.01 * routes.loss
+
+To capture a training step into a graph, let no graph of autograd made outside of the capture live
+that has the same leaves (torch would wait for its streams, which a capture cannot).
 """
 from __future__ import annotations
 
@@ -104,7 +118,7 @@ class _NoSecondDerivative(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, *grads):
-        raise RuntimeError("the FP8 linear layers have no second derivative: a gradient taken with "
+        raise RuntimeError("the layers have no second derivative: a gradient taken with "
                            "create_graph=True is not to be differentiated")
 
 
@@ -146,6 +160,129 @@ def train_linear(x: torch.Tensor, w: torch.Tensor, ends: torch.Tensor | None = N
     return _Linear.apply(x, w, ends, rotate)
 
 
+class _First(torch.autograd.Function):
+    """What the exchange's functions share: gradients that are not differentiated again."""
+    @classmethod
+    def backward(cls, ctx, *grads):
+        with torch.no_grad():
+            out = cls.gradients(ctx, *grads)
+        if torch.is_grad_enabled():
+            out = [g if g is None else _NoSecondDerivative.apply(g.requires_grad_()) for g in out]
+        return tuple(out)
+
+
+class _Route(_First):
+    @staticmethod
+    def forward(ctx, logits, k, renormalize, valid):
+        routes = hadacore.route_tokens(logits, k, renormalize, valid)
+        ctx.renormalize = renormalize
+        ctx.mark_non_differentiable(routes.experts, routes.counts, routes.slopes)
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(logits, *routes[:5])
+        return routes[:5]
+
+    @staticmethod
+    def gradients(ctx, _, dweights, __, dloss, ___):
+        if dweights is None and dloss is None:
+            return None, None, None, None
+        logits, *routes = ctx.saved_tensors
+        dweights = None if dweights is None else dweights.contiguous()
+        return hadacore.route_tokens_gradient(logits, hadacore.Routes(*routes, ctx.renormalize),
+                                              dweights, dloss), None, None, None
+
+
+class _Dispatch(_First):
+    @staticmethod
+    def forward(ctx, x, rows, ends):
+        ctx.save_for_backward(rows)
+        return hadacore.dispatch_rows(x, rows, ends)
+
+    @staticmethod
+    def gradients(ctx, dxs):
+        return hadacore.combine_rows(dxs.contiguous(), *ctx.saved_tensors), None, None
+
+
+class _Combine(_First):
+    @staticmethod
+    def forward(ctx, y, weights, rows, ends):
+        # y is needed for the weights' gradient, and the weights for y's
+        ctx.save_for_backward(y if weights is not None and ctx.needs_input_grad[1] else None, weights, rows, ends)
+        return hadacore.combine_rows(y, rows, weights)
+
+    @staticmethod
+    def gradients(ctx, dout):
+        y, weights, rows, ends = ctx.saved_tensors
+        dy, dweights = hadacore.combine_rows_gradient(dout.contiguous(), y, rows, ends, weights,
+                                                      want_dy=ctx.needs_input_grad[0])
+        return dy, dweights, None, None
+
+
+def route(logits: torch.Tensor, k: int, renormalize: bool = True,
+          valid: torch.Tensor | None = None) -> hadacore.Routes:
+    """``hadacore.route_tokens`` with gradients of the logits for ``weights`` and ``loss``."""
+    return hadacore.Routes(*_Route.apply(logits.contiguous(), k, renormalize, valid), renormalize)
+
+
+def dispatch(x: torch.Tensor, groups: hadacore.Groups) -> torch.Tensor:
+    """Rows of ``x`` (tokens x width) at the places of their slots, with a gradient."""
+    return _Dispatch.apply(x.contiguous(), groups.rows, groups.ends)
+
+
+def combine(y: torch.Tensor, groups: hadacore.Groups, weights: torch.Tensor | None = None) -> torch.Tensor:
+    """The rows of each token's slots joined by weight (tokens x choices, float32; None: their
+    sum), with gradients of ``y`` and ``weights``."""
+    return _Combine.apply(y.contiguous(), weights, groups.rows, groups.ends)
+
+
+def mixture(x: torch.Tensor, logits: torch.Tensor, w: torch.Tensor, k: int, renormalize: bool = True,
+            valid: torch.Tensor | None = None, rotate: int | None = None):
+    """(out, routes): each token's ``k`` experts of ``w`` (experts x n x k) by ``logits`` (tokens x
+    experts), joined by their weights; with gradients of x, logits (also for ``routes.loss``) and w."""
+    routes = route(logits, k, renormalize, valid)
+    groups = hadacore.group_tokens(routes.experts, w.shape[0])
+    return combine(train_linear(dispatch(x, groups), w, groups.ends, rotate), groups, routes.weights), routes
+
+
+def serve_mixture(x: torch.Tensor, logits: torch.Tensor, weights: Weights, k: int, renormalize: bool = True,
+                  valid: torch.Tensor | None = None) -> torch.Tensor:
+    """``mixture`` for quantized weights, without gradients: tokens are rotated and quantized once, and
+    their codes dispatched."""
+    routes = hadacore.route_tokens(logits, k, renormalize, valid)
+    groups = hadacore.group_tokens(routes.experts, weights.codes.shape[0])
+    a, a_scales = hadacore.transform_fp8_blocks(x, n=weights.rotate)
+    y = hadacore.grouped_matmul_fp8(hadacore.dispatch_rows(a, groups.rows, groups.ends),
+                                    hadacore.dispatch_rows(a_scales, groups.rows, groups.ends),
+                                    weights.codes, weights.scales, groups.ends, dtype=x.dtype)
+    return hadacore.combine_rows(y, groups.rows, routes.weights)
+
+
+def _mixture_example() -> None:
+    """A mixture of 8 experts, two a token, its balance loss beside its output."""
+    tokens, experts, n, k = 2000, 8, 512, 2048
+    x = torch.randn(tokens, k, device="cuda").bfloat16()
+    w = (torch.randn(experts, n, k, device="cuda") / k ** 0.5).bfloat16()
+    logits, dy = torch.randn(tokens, experts, device="cuda"), torch.randn(tokens, n, device="cuda")
+    grads = []
+    for plain in (False, True):
+        leaves = [t.clone().requires_grad_() for t in ((x.float(), w.float(), logits) if plain else (x, w, logits))]
+        if plain:
+            p = torch.softmax(leaves[2], 1)
+            top = torch.topk(leaves[2], 2, dim=1).indices
+            share = p.gather(1, top) / p.gather(1, top).sum(1, keepdim=True)
+            all_y = torch.einsum("tk,enk->ten", leaves[0], leaves[1])
+            out = (all_y.gather(1, top[..., None].expand(-1, -1, n)) * share[..., None]).sum(1)
+            f = torch.bincount(top.view(-1), minlength=experts) / top.numel()
+            loss = experts * (f * p.mean(0)).sum()
+        else:
+            out, routes = mixture(leaves[0], leaves[2], leaves[1], 2)
+            loss = routes.loss
+        ((out.float() * dy).sum() + loss).backward()
+        grads.append([out.detach().float(), *(t.grad.float() for t in leaves), loss.detach()])
+    off = [float((a - b).norm() / b.norm()) for a, b in zip(*grads)]
+    print(f"mixture: relative error of out {off[0]:.4f}, dx {off[1]:.4f}, dw {off[2]:.4f}, "
+          f"d logits {off[3]:.4f}, balance loss {off[4]:.1e}")
+
+
 def main() -> None:
     torch.manual_seed(0)
     tokens, experts, n, k = 4000, 8, 1024, 4096
@@ -169,6 +306,7 @@ def main() -> None:
                for g, r in zip((y.detach(), leaf_x.grad, leaf_w.grad), want)]
         print(f"rotation of {rotate:4d}: relative error of y {off[0]:.4f}, dx {off[1]:.4f}, "
               f"dw {off[2]:.4f}")
+    _mixture_example()
 
 
 if __name__ == "__main__":

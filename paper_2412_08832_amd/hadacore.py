@@ -946,6 +946,20 @@ def _words(n: int, device, dtype=None):
     return _torch.empty_strided((n,), (1,), dtype=dtype or _torch.int32, device=device)
 
 
+def _scratch(nbytes: int, device, stream):
+    """A workspace of the current stream's memory (None for no bytes) for work on ``stream``: given as
+    an argument, that may be another one, and the memory is not to be reused before it is done."""
+    if not nbytes:
+        return None, None
+    t = _words(nbytes >> 2, device)
+    if stream is not None:
+        if not hasattr(stream, "cuda_stream"):
+            stream = (_torch.cuda.ExternalStream(stream, device=device) if stream
+                      else _torch.cuda.default_stream(device))
+        t.record_stream(stream)
+    return t, t.data_ptr()
+
+
 def _matrix(name: str, t, device: int, dims: int = 2):
     """Checks of a tensor with contiguous rows; the row stride (one that passes for a single row)."""
     if t.dim() != dims:
@@ -1013,10 +1027,10 @@ def route_tokens(logits, k: int, renormalize: bool = True, valid=None, stream=No
     slopes = _words(experts, where, _float32)
     loss = _torch.empty_strided((), (), dtype=_float32, device=where)
     need = _route_workspace(m, experts)
-    workspace = _words(need >> 2, where)
+    workspace, workspace_ptr = _scratch(need, where, stream)
     _call("hadacore_route", device, logits.data_ptr(), stride, code, valid_ptr, m, experts, k,
           renormalize, chosen.data_ptr(), weights.data_ptr(), counts.data_ptr(), loss.data_ptr(),
-          slopes.data_ptr(), workspace.data_ptr(), need, _stream_of(stream, device))
+          slopes.data_ptr(), workspace_ptr, need, _stream_of(stream, device))
     return Routes(chosen, weights, counts, loss, slopes, renormalize)
 
 
@@ -1061,11 +1075,10 @@ def group_tokens(ids, groups: int, stream=None) -> Groups:
     n, where = ids.numel(), ids.device
     ends, slots = _words(groups, where), _words(n, where)
     rows = _torch.empty_strided(ids.shape, ids.stride(), dtype=_torch.int32, device=where)
-    need, workspace = _group_workspace(n, groups), None
-    if need:
-        workspace = _words(need >> 2, where)
+    need = _group_workspace(n, groups)
+    workspace, workspace_ptr = _scratch(need, where, stream)
     _call("hadacore_group_tokens", device, ids.data_ptr(), n, groups, ends.data_ptr(), rows.data_ptr(),
-          slots.data_ptr(), workspace.data_ptr() if need else None, need, _stream_of(stream, device))
+          slots.data_ptr(), workspace_ptr, need, _stream_of(stream, device))
     return Groups(ends, rows, slots)
 
 
@@ -1217,13 +1230,12 @@ def adapt_rows(x, down, up, ends=None, slots=None, y=None, scales=None, out=None
     if hidden:
         h = _torch.empty_strided((m, padded), (padded, 1), dtype=_float32, device=where)
         h_ptr = h.data_ptr()
-    need, workspace = _adapters_workspace(m, k, n, rank, groups), None
-    if need:
-        workspace = _words(need >> 2, where)
+    need = _adapters_workspace(m, k, n, rank, groups)
+    workspace, workspace_ptr = _scratch(need, where, stream)
     _call("hadacore_adapters", device, x.data_ptr(), x_stride, down.data_ptr(), down_stride,
           down.stride(0), up.data_ptr(), up_stride, up.stride(0), scales_ptr, ends_ptr, slots_ptr,
           groups, y_ptr, y_stride, out.data_ptr(), _row_stride(out, n), code, _out_codes[dtype], h_ptr,
-          padded, m, k, n, rank, workspace.data_ptr() if need else None, need, _stream_of(stream, device))
+          padded, m, k, n, rank, workspace_ptr, need, _stream_of(stream, device))
     if not hidden:
         return out
     return out, h if padded == rank else h.narrow(1, 0, rank)
@@ -1258,11 +1270,10 @@ def adapter_gradient(h, x, ends=None, slots=None, scales=None, out=None, dtype=N
     elif out.shape != shape or out.device != x.device or (width > 1 and out.stride(-1) != 1) \
             or out.dtype not in (x.dtype, _float32) or (dtype is not None and out.dtype is not dtype):
         raise ValueError(f"out must be a {shape} tensor of the output's type with contiguous rows")
-    need, workspace = _adapter_gradient_workspace(m, width, rank, groups), None
-    if need:
-        workspace = _words(need >> 2, x.device)
+    need = _adapter_gradient_workspace(m, width, rank, groups)
+    workspace, workspace_ptr = _scratch(need, x.device, stream)
     _call("hadacore_adapter_gradient", device, h.data_ptr(), h_stride, x.data_ptr(), x_stride, code,
           scales_ptr, ends_ptr, slots_ptr, groups, out.data_ptr(), _row_stride(out, width),
           out.stride(0) if ends is not None else 0, _out_codes[out.dtype], m, width, rank,
-          workspace.data_ptr() if need else None, need, _stream_of(stream, device))
+          workspace_ptr, need, _stream_of(stream, device))
     return out
