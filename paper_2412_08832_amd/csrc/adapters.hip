@@ -974,16 +974,28 @@ __global__ __launch_bounds__(kAnyWaves *kWave) void gradient_any_kernel(Gradient
   store_gradient<DT, OUT, RT, kAnyWaves>(p, g, rank0, shift, acc, sums);
 }
 
-template <int OUT>
+// Four values a thread where rows have whole fours.
+template <int OUT, int N>
 __global__ __launch_bounds__(256) void join_gradient_kernel(GradientArgs p) {
   const int64_t all = (int64_t)p.groups * p.rank * p.width;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-    float v = 0.0f;
-    for (int s = 0; s < p.splits; ++s) v += p.part[s * all + i];
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * N; i < all; i += (int64_t)gridDim.x * 256 * N) {
+    float v[N] = {};
+#pragma unroll 4
+    for (int s = 0; s < p.splits; ++s) {
+      if constexpr (N == 4) {
+        const f4 more = *reinterpret_cast<const f4 *>(p.part + s * all + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] += more[j];
+      } else {
+        v[0] += p.part[s * all + i];
+      }
+    }
     const int64_t row = i / p.width;
     const int g = (int)(row / p.rank), rank = (int)(row % p.rank);
     const float factor = p.scales != nullptr ? p.scales[g] : 1.0f;
-    store_value<OUT>(p.out, g * p.out_batch + rank * p.out_stride + i % p.width, factor * v);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      store_value<OUT>(p.out, g * p.out_batch + rank * p.out_stride + i % p.width + j, factor * v[j]);
   }
 }
 
@@ -1165,9 +1177,15 @@ void launch_gradient(const GradientArgs &p, hipStream_t stream) {
   else
     go(integral_constant<int, 4>{});
   if (p.splits > 1) {
-    const int64_t blocks = divide_up((int64_t)p.groups * p.rank * p.width, 256);
-    hipLaunchKernelGGL(join_gradient_kernel<OUT>, dim3((uint32_t)(blocks < 4096 ? blocks : 4096)),
-                       dim3(256), 0, stream, p);
+    const auto join = [&](auto n) {
+      const int64_t blocks = divide_up((int64_t)p.groups * p.rank * p.width, 256 * decltype(n)::value);
+      hipLaunchKernelGGL((join_gradient_kernel<OUT, decltype(n)::value>),
+                         dim3((uint32_t)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, stream, p);
+    };
+    if (p.width % 4 == 0)
+      join(integral_constant<int, 4>{});
+    else
+      join(integral_constant<int, 1>{});
   }
 }
 
@@ -1372,7 +1390,7 @@ extern "C" hadacore_status hadacore_adapter_gradient(
   if (groups == 0 || width == 0) return HADACORE_SUCCESS;
   const int64_t need = hadacore_adapter_gradient_workspace_size(m, width, rank, groups);
   if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return HADACORE_ERROR_WORKSPACE;
-  if (!aligned_to(workspace, 4)) return HADACORE_ERROR_MISALIGNED;
+  if (!aligned_to(workspace, 16)) return HADACORE_ERROR_MISALIGNED;
   const Span so = matrices(out, groups, out_batch_stride, rank, out_row_stride, width, size),
              sw = span(workspace, need > 0, need, need, 1);
   const Span in[] = {matrices(hidden, 1, 0, m, hidden_row_stride, rank, 4),

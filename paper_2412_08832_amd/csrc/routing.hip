@@ -226,7 +226,7 @@ struct RouteArgs {
   uint32_t *done;
 };
 
-constexpr int kRouteThreads = 1024;
+constexpr int kRouteThreads = 512;
 
 // Larger logits have larger keys, NaN the largest, and -0 is 0.  0: no logit.
 __device__ __forceinline__ uint32_t order_key(float x) {
