@@ -819,14 +819,14 @@ __device__ __forceinline__ void store_gradient(const GradientArgs &p, int g, int
 // their tokens three: no barriers, and few instructions, which are loaded anew by every call
 // (with the loads in registers, a step ahead, 31 us instead of NEW for 8191 x 4096, rank 16).
 constexpr int kGradWaves = 2;
-constexpr int kGradRing = 3;
 
 template <int DT, int OUT, int RT, int P>
 __global__ __launch_bounds__(kGradWaves *kWave) void gradient_kernel(GradientArgs p) {
+  constexpr int D = RT == 4 ? 2 : 3;  // stages of the ring: two workgroups to a CU
   constexpr int kX = kStep * kGradColumns * 2, kH = RT * kStep * kTile * 4;
   constexpr int kLoads = 8 + 8 * RT;  // of a step's x and h
   static_assert(kLoads + 1 < 64, "loads in flight that one wait can count");
-  constexpr int kRing = kGradRing * (kX + kH);
+  constexpr int kRing = D * (kX + kH);
   constexpr int kSums = kGradWaves * 8 * (kWave + 1) * 16;
   __shared__ __attribute__((aligned(16))) uint8_t
       room[kGradWaves * kRing > kSums ? kGradWaves * kRing : kSums];
@@ -880,30 +880,28 @@ __global__ __launch_bounds__(kGradWaves *kWave) void gradient_kernel(GradientArg
   };
   f4 acc[RT][8] = {};
   int shift = -100, stage = 1;
-  // Turn i loads the tokens of step i + 3 and the rows of step i + 2, and multiplies step i.
-  // In flight before its wait, in order: the rows of step i, the tokens of i + 2, the rows of i + 1, the
-  // tokens of i + 3; all but the last two have to be there.
+  // Turn i loads the tokens of step i + D and the rows of step i + D - 1, and multiplies step i.
+  // In flight before its wait, in order (D = 3): the rows of step i, the tokens of i + 2, the rows of
+  // i + 1, the tokens of i + 3; all but the last two have to be there.  (D = 2: the tokens of
+  // i + 1, the rows of i, the tokens of i + 2; all but the last.)
 #pragma unroll 1
-  for (int i = -3; i < steps; ++i) {
-    const bool more = i + 3 < steps;
-    if (more) load_tokens(i + 3);
-    if (i == -3) continue;
-    if (i == -2) {
-      if (more)
-        asm volatile("s_waitcnt vmcnt(1)" ::: "memory");
-      else
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  for (int i = -D; i < steps; ++i) {
+    const bool more = i + D < steps;
+    if (more) load_tokens(i + D);
+    if (i == -D) continue;
+    if (more && i == 1 - D) {
+      asm volatile("s_waitcnt vmcnt(1)" ::: "memory");
     } else if (more) {
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads + 1) : "memory");
-    } else if (i + 1 < steps) {
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - 2) * kLoads + 1) : "memory");
+    } else if (D > 2 && i > 1 - D && i + 1 < steps) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - 2) * kLoads) : "memory");
     } else {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
-    // step i is in `stage`, and step i + 2 goes where i - 1 was
+    // step i is in `stage`, and step i + D - 1 goes where i - 1 was
     const uint8_t *from = ring + stage * (kX + kH);
-    if (i + 2 < steps) load_rows(i + 2, stage == 0 ? kGradRing - 1 : stage - 1);
-    stage = stage == kGradRing - 1 ? 0 : stage + 1;
+    if (i + D - 1 < steps) load_rows(i + D - 1, stage == 0 ? D - 1 : stage - 1);
+    stage = stage == D - 1 ? 0 : stage + 1;
     if (i < 0) continue;
     uint32_t raw[8][4];
     float hv[RT][8];
@@ -1055,7 +1053,8 @@ Cut cut_of(int64_t m, int64_t k, int64_t n, int64_t rank, int64_t groups, int pa
 int64_t gradient_splits(int64_t m, int64_t width, int64_t rank, int64_t groups) {
   if (groups < 1 || width < 1) return 1;
   const int64_t blocks = divide_up(width, kGradColumns) * groups * divide_up(rank, 64);
-  int64_t splits = divide_up(2 * kBlocksWanted, blocks);
+  // all at once, two to a CU; of one tile of ranks twice as many do as well or better
+  int64_t splits = divide_up(rank <= kTile ? 2 * kBlocksWanted : kBlocksWanted, blocks);
   // a workgroup goes through 64 tokens in a turn; a share has two turns at least
   const int64_t most = m / groups / (2 * kStep * kGradWaves);
   splits = splits > most ? most : splits;
