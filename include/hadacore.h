@@ -426,8 +426,9 @@ hadacore_status hadacore_weight_gradient_fp8_grouped(
  *
  * HADACORE_ERROR_TOO_LARGE: 2^30 slots and more; rows times their stride past 2^42; for the
  * exchange 2^32 work-items (256 for each token of a gradient, and for each 16 KiB copied or 2048
- * values, 1024 of fp32, joined); for the adapters 2^27 tokens, or rows of more than 2^22
- * values, or more than HADACORE_MAX_GROUPS adapters.
+ * values, 1024 of fp32, joined); for the adapters 2^27 tokens, rows of more than 2^22 values, more
+ * than HADACORE_MAX_GROUPS adapters, or 2^32 work-items (256 for each 16 to 128 tokens of an adapter
+ * by 512 outputs, or 256 from rank 129).
  */
 #define HADACORE_MAX_EXPERTS 1024
 #define HADACORE_MAX_CHOICES 32

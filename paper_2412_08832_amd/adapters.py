@@ -52,7 +52,9 @@ class _Adapt(torch.autograd.Function):
         # of a projection in 32 bits: in x's type, as the products take it
         dout = dout.to(x.dtype).contiguous()
         if need_down:
-            dx, dh = hadacore.adapt_rows(dout, up, down, ends, slots, scales=scales, hidden=True)
+            # without x's gradient only the first of the two products is made
+            back = down if need_x else down[..., :0]
+            dx, dh = hadacore.adapt_rows(dout, up, back, ends, slots, scales=scales, hidden=True)
             d_down = hadacore.adapter_gradient(dh, x, ends, slots, scales).view(down.shape)
         elif need_x:
             dx = hadacore.adapt_rows(dout, up, down, ends, slots, scales=scales)

@@ -512,7 +512,8 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
       }
   };
   const auto add = [&](int t, int v, const f4 (&acc)[CT], Row &row) {
-    const float unshift = DT == HADACORE_FP16 && !bare ? back[t] : 1.0f;
+    if (bare) return;  // y as it is
+    const float unshift = DT == HADACORE_FP16 ? back[t] : 1.0f;
     float sum[CT];
 #pragma unroll
     for (int i = 0; i < CT; ++i) sum[i] = fmaf(acc[i][v], unshift, row.get(i));
@@ -704,13 +705,14 @@ __global__ __launch_bounds__(kFewWaves *kWave) void few_tokens_kernel(AdapterArg
   for (int v = 0; v < 4; ++v) {
     const int t = 4 * quarter + v;
     if (t >= count || valid <= 0) continue;
-    const float unshift = DT == HADACORE_FP16 && !bare ? back[t] : 1.0f;
-    float sum[CT];
+    if (!bare) {
+      const float unshift = DT == HADACORE_FP16 ? back[t] : 1.0f;
+      float sum[CT];
 #pragma unroll
-    for (int i = 0; i < CT; ++i) sum[i] = fmaf(acc[i][v], unshift, old[v].get(i));
-    Row row;
-    row.set(sum);
-    row.store(out + (token[v] * p.out_stride + col) * kSize, EVEN ? CT : valid);
+      for (int i = 0; i < CT; ++i) sum[i] = fmaf(acc[i][v], unshift, old[v].get(i));
+      old[v].set(sum);
+    }
+    old[v].store(out + (token[v] * p.out_stride + col) * kSize, EVEN ? CT : valid);
   }
 }
 
@@ -817,7 +819,7 @@ __device__ __forceinline__ void store_gradient(const GradientArgs &p, int g, int
 // two waves in turn.  Both operands have the tokens along their depth: x is turned in registers, h
 // is split.  Each wave streams its own rows of x and h into a ring in LDS, two steps ahead, and
 // their tokens three: no barriers, and few instructions, which are loaded anew by every call
-// (with the loads in registers, a step ahead, 31 us instead of NEW for 8191 x 4096, rank 16).
+// (8191 x 4096, four adapters of rank 16: 27 us; with the loads in registers, a step ahead, 31).
 constexpr int kGradWaves = 2;
 
 template <int DT, int OUT, int RT, int P>
@@ -1300,9 +1302,13 @@ extern "C" hadacore_status hadacore_adapters(
       spans_overlap(sy, sh) || spans_overlap(sy, sw) ||
       (spans_overlap(so, sy) && !(out == y && (out_row_stride == y_row_stride || m == 1))))
     return HADACORE_ERROR_OVERLAP;
+  const Cut cut = cut_of(m, k, n, rank, groups, parts_of(dtype, out_dtype));
+  // up_kernel's launch, the largest
+  if (!cut.fused && most_pieces(m, groups, cut.unit) * divide_up(n, rank > 128 ? 256 : 512) * 256 >=
+                        (int64_t(1) << 32))
+    return HADACORE_ERROR_TOO_LARGE;
   st = check_device();
   if (st != HADACORE_SUCCESS) return st;
-  const Cut cut = cut_of(m, k, n, rank, groups, parts_of(dtype, out_dtype));
   AdapterArgs p{};
   p.x = static_cast<const uint16_t *>(x);
   p.x_stride = x_row_stride;

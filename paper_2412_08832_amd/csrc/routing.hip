@@ -565,7 +565,7 @@ __global__ __launch_bounds__(256) void route_gradient_kernel(RouteGradArgs p) {
 
 // Lanes to a row and experts to a lane.  What bounds large calls is the issue of vector operations, and a
 // step of a choice costs about as many for 16 experts in each of 16 lanes, which does four rows at
-// once, as for 4 in each of 64 (16384 x 256, eight choices: ROUTE us instead of 21.8).
+// once, as for 4 in each of 64 (16384 x 256, eight choices: 17 us instead of 22).
 template <class F>
 void for_experts(int64_t experts, F f) {
   using std::integral_constant;
@@ -729,9 +729,9 @@ __global__ __launch_bounds__(kGroupThreads) void place_groups_kernel(GroupArgs p
 // How many waves of a workgroup share its slots: the counts take 64 KiB of LDS at most.
 int group_waves(int64_t groups) { return groups <= 900 ? 16 : groups <= 2700 ? 4 : 2; }
 
-// Workgroups.  Up to 8192 slots one does it in one launch (8.7 us; two launches take 2.4 and 4.6 and the
-// time between them); from there one for 2048 slots, 64 at most, since each adds up the counts
-// of all (131072 slots of 256 groups: GROUP us; by 128 workgroups 14).
+// Workgroups.  Up to 8192 slots one does it in one launch (8.7 us; two launches take 2.4 and 4.6 and
+// the time between them); from there one for 2048 slots, 128 at most, since each adds up the counts
+// of all (131072 slots of 256 groups: 2.4 and 9.5 us).
 int64_t group_blocks_of(int64_t slots, int64_t groups) {
   if (slots <= 8192) return 1;
   const int64_t blocks = (slots + 2047) / 2048, most = (1 << 16) / (groups + 1);

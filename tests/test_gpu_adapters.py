@@ -94,6 +94,16 @@ def test_groups_of_any_size(ends):
     _check(x, down, up, y, scales, torch.tensor(ends, dtype=torch.int32), slots, BF16)
 
 
+def test_tokens_without_an_adapter_keep_y():
+    """Bit for bit: -0 and NaN among them."""
+    for m, n in ((5, 128), (700, 300)):
+        x, down, up, y, scales, _, slots = _make(m, 64, n, 8, 2, BF16)
+        y[:, 0], y[:, 1] = -0.0, float("nan")
+        ends = torch.zeros(2, dtype=torch.int32)
+        got = H.adapt_rows(*_cuda(x, down, up), *_cuda(ends, slots), y=y.cuda())
+        assert torch.equal(got.view(torch.int16).cpu(), y.view(torch.int16))
+
+
 def test_no_tokens_groups_or_columns():
     x, down, up, y, scales, ends, slots = _cuda(*_make(10, 64, 48, 8, 2, BF16))
     none = torch.zeros(0, dtype=torch.int32, device="cuda")

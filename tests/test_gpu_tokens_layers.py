@@ -62,7 +62,7 @@ def test_mixture(tokens, experts, n, k, choices, renormalize, padded, dtype):
     assert torch.equal(routes.experts.cpu(), chosen)
     ((out.float() * dy.cuda()).sum() + 0.1 * routes.loss).backward()
     assert _rel(out, want.detach()) <= REL
-    assert abs(float(routes.loss) - float(want_loss)) <= 1e-5 * float(want_loss)
+    assert abs(float(routes.loss.detach()) - float(want_loss.detach())) <= 1e-5 * float(want_loss.detach())
     for name, leaf, ref in zip(("x", "logits", "w"), leaves, want_grads):
         if float(ref.norm()) > 0:
             assert leaf.grad.dtype == leaf.dtype and _rel(leaf.grad, ref) <= REL, name

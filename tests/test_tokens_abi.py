@@ -143,6 +143,9 @@ ADAPT = dict(x=X, x_stride=512, down=A, down_stride=512, down_batch=40 * 512, up
     (dict(workspace=0), "WORKSPACE"), (dict(bytes=100), "WORKSPACE"), (dict(workspace=W + 4), "MISALIGNED"),
     (dict(out=X), "OVERLAP"), (dict(out=B + 4), "OVERLAP"), (dict(out=F + 1200), "OVERLAP"),
     (dict(out=F, out_stride=304), "OVERLAP"), (dict(hidden=G), "OVERLAP"), (dict(workspace=F), "OVERLAP"),
+    (dict(m=(1 << 27) - 1, n=1 << 15, x=1 << 50, down=1 << 58, up=1 << 59, y=1 << 51, out=1 << 52, workspace=1 << 53,
+          scales=1 << 54, ends=1 << 55, slots=1 << 56, up_stride=1 << 15, up_batch=40 << 15, y_stride=1 << 15, out_stride=1 << 15,
+          x_stride=512, bytes=1 << 50), "TOO_LARGE"),
     (dict(m=0, x=0, out=0), "SUCCESS")])
 def test_adapters_refusals(change, status):
     assert _status(H.hadacore_adapters, ADAPT, **change) == status

@@ -50,7 +50,8 @@ def _combine_gradient(dout, y, rows, ends, weights=None, want_dy=True):
 
 
 def _adapt_rows(x, down, up, ends=None, slots=None, y=None, scales=None, dtype=None, hidden=False):
-    out, _, h, _ = R.adapt(x, down.view(-1, *down.shape[-2:]), up.view(-1, *up.shape[-2:]), ends, slots, y, scales, 0, 0)
+    down, up = (t if t.dim() == 3 else t[None] for t in (down, up))
+    out, _, h, _ = R.adapt(x, down, up, ends, slots, y, scales, 0, 0)
     return (out, h) if hidden else out
 
 
