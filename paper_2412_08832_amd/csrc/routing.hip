@@ -8,7 +8,8 @@
 //
 // All of it moves few bytes (or each byte once): what bounds the large calls is HBM, and the small
 // ones their launches, so every call is one launch where a workgroup can do it and two otherwise.
-// No result depends on the order of atomics: the only ones count, in LDS.
+// No result depends on the order of atomics: they count in LDS, or find the last of the workgroups
+// that join the balance loss, which adds up the others' parts in their order.
 
 #include <hip/hip_runtime.h>
 
