@@ -111,6 +111,39 @@ __device__ __forceinline__ u4 load8(const uint16_t *p, int64_t valid) {
   return u4{w[0], w[1], w[2], w[3]};
 }
 
+// The words moved down by `by` of them, zeros behind; of more than N, any of them.
+template <int N>
+__device__ __forceinline__ void move_words(uint32_t (&w)[N], int by) {
+#pragma unroll
+  for (int step = N / 2; step > 0; step /= 2)
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = (by & step) != 0 ? (i + step < N ? w[i + step < N ? i + step : 0] : 0) : w[i];
+}
+// The same for 16-bit values, two a word.
+template <int N>
+__device__ __forceinline__ void move_values(uint32_t (&w)[N], int by) {
+  move_words<N>(w, by / 2);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    w[i] = (by & 1) != 0 ? (w[i] >> 16) | (i + 1 < N ? w[i + 1 < N ? i + 1 : 0] << 16 : 0) : w[i];
+}
+
+// Eight values moved down by any number of them, zeros behind.
+__device__ __forceinline__ u4 moved(u4 v, int by) {
+  uint32_t w[4] = {v[0], v[1], v[2], v[3]};
+  move_values<4>(w, by);
+  return by < 8 ? u4{w[0], w[1], w[2], w[3]} : u4{0, 0, 0, 0};
+}
+
+// How far before its own place a lane loads N values, `valid` of which are there, so that they end
+// with the row: in a row of N and more they are inside it, and no load stands in a branch, where a
+// wave would wait for each by itself.  move_values() then brings them to their places.  (up_kernel,
+// 3525 x 997, rank 95: 20 us instead of 55; gradient_any_kernel, 1957 x 5597, rank 9: 18 instead of 35.)
+template <int N>
+__device__ __forceinline__ int ahead_of(int64_t valid) {
+  return valid >= N ? 0 : N - (int)valid;
+}
+
 // Eight rows of 8 (or 4) consecutive columns, turned: column i's eight values in `col[i]`.
 template <int CT>
 __device__ __forceinline__ void turn(const uint32_t (&row)[8][CT / 2], u4 (&col)[CT]) {
@@ -251,10 +284,26 @@ __global__ __launch_bounds__(W *kWave) void down_kernel(AdapterArgs p) {
   const int left = (to - from) % U + (share == shares - 1 && p.k % kStep != 0);
   for (int s = 0; s < left; ++s) {
     const int valid = (from + turns * U + s < to ? kStep : p.k % kStep) - quarter * 8;
+    if (p.k >= 8) {
+      const int by = ahead_of<8>(valid);
 #pragma unroll
-    for (int t = 0; t < TT; ++t) xv[0][0][t] = load8(xp[t] + s * kStep, valid);
+      for (int t = 0; t < TT; ++t)
+        xv[0][0][t] = *reinterpret_cast<const u4_any *>(xp[t] + s * kStep - by);
 #pragma unroll
-    for (int r = 0; r < RT; ++r) wv[0][0][r] = load8(wp[r] + s * kStep, valid);
+      for (int r = 0; r < RT; ++r)
+        wv[0][0][r] = *reinterpret_cast<const u4_any *>(wp[r] + s * kStep - by);
+      if (by > 0) {
+#pragma unroll
+        for (int t = 0; t < TT; ++t) xv[0][0][t] = moved(xv[0][0][t], by);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) wv[0][0][r] = moved(wv[0][0][r], by);
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < TT; ++t) xv[0][0][t] = load8(xp[t] + s * kStep, valid);
+#pragma unroll
+      for (int r = 0; r < RT; ++r) wv[0][0][r] = load8(wp[r] + s * kStep, valid);
+    }
 #pragma unroll
     for (int t = 0; t < TT; ++t)
 #pragma unroll
@@ -350,6 +399,12 @@ struct OutRow {
         w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(p)[i] << (16 * (i % 2));
     }
   }
+  __device__ __forceinline__ void move(int by) {
+    if constexpr (OUT == HADACORE_FP32)
+      move_words<kWords>(w, by);
+    else
+      move_values<kWords>(w, by);
+  }
   __device__ __forceinline__ void store(uint8_t *p) const {
     if constexpr (kWords == 2) {
       stream_out<NT, u2_any>(p, u2{w[0], w[1]});
@@ -397,6 +452,8 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
   const int64_t valid = EVEN ? CT : (int64_t)p.n - col;
   // a wave behind the last column loads the first ones in their place
   const bool behind = (chunk * 4 + wave) * (kTile * CT) >= p.n;
+  const bool wide = !EVEN && p.n >= CT;
+  const int by = wide ? ahead_of<CT>(valid) : 0;
   uint32_t raw[RB][8][CT / 2];
   if (!bare) {
 #pragma unroll
@@ -405,9 +462,12 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
       for (int j = 0; j < 8; ++j) {
         const int row = b * kStep + quarter * 8 + j;
         // ranks that are not there: any values, cleared below
-        load_columns<CT>(p.up + piece.group * p.up_batch + (row < p.rank ? row : 0) * p.up_stride +
-                             (EVEN && behind ? c * CT : col),
-                         valid, raw[b][j]);
+        const uint16_t *at = p.up + piece.group * p.up_batch + (row < p.rank ? row : 0) * p.up_stride +
+                             (EVEN && behind ? c * CT : col);
+        if (wide)
+          load_columns<CT>(at - by, CT, raw[b][j]);
+        else
+          load_columns<CT>(at, valid, raw[b][j]);
       }
   }
   const uint8_t *y = static_cast<const uint8_t *>(p.y);
@@ -493,6 +553,10 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
           for (int i = 0; i < CT / 2; ++i)
             raw[b][j][i] = b * kStep + quarter * 8 + j < p.rank ? raw[b][j][i] : 0;
       }
+      if (by > 0) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) move_values<CT / 2>(raw[b][j], by);
+      }
       turn<CT>(raw[b], w[b]);
     }
   }
@@ -538,13 +602,28 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
       }
     }
   }
+  // the rest; rows held a tile ahead, as above, cost a wave of four on a SIMD (7028 x 4304, rank 8: 24
+  // us instead of 21)
+  const bool early = y != nullptr && (EVEN || wide);
   for (int t0 = fast; t0 < count; t0 += kTile) {
     Row rest[4];
+    if (early) {
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      const int t = t0 + 4 * quarter + v;
-      rest[v].clear();
-      if (y != nullptr && t < count) rest[v].load(y + (tokens[t] * p.y_stride + col) * kSize, valid);
+      for (int v = 0; v < 4; ++v) {
+        const int t = t0 + 4 * quarter + v < count ? t0 + 4 * quarter + v : count - 1;
+        rest[v].load(y + (tokens[t] * p.y_stride + col - by) * kSize);
+      }
+      if (by > 0) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) rest[v].move(by);
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int t = t0 + 4 * quarter + v;
+        rest[v].clear();
+        if (y != nullptr && t < count) rest[v].load(y + (tokens[t] * p.y_stride + col) * kSize, valid);
+      }
     }
     f4 acc[CT] = {};
     multiply(t0, acc);
@@ -601,13 +680,17 @@ __global__ __launch_bounds__(kFewWaves *kWave) void few_tokens_kernel(AdapterArg
   f4 acc[CT] = {};
   if (!bare) {
     uint32_t raw[8][CT / 2];
+    const int by = !EVEN && p.n >= CT ? ahead_of<CT>(valid) : 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int row = quarter * 8 + j;
       // ranks and columns that are not there: any values, cleared below or not stored
-      load_columns<CT>(p.up + piece.group * p.up_batch + (row < p.rank ? row : 0) * p.up_stride +
-                           (EVEN && valid == 0 ? 0 : col),
-                       EVEN ? CT : valid, raw[j]);
+      const uint16_t *at = p.up + piece.group * p.up_batch + (row < p.rank ? row : 0) * p.up_stride +
+                           (EVEN && valid == 0 ? 0 : col);
+      if (EVEN || p.n >= CT)
+        load_columns<CT>(at - by, CT, raw[j]);
+      else
+        load_columns<CT>(at, valid, raw[j]);
     }
     const int64_t steps = p.k / kStep;
     const int from = (int)(steps * wave / kFewWaves), to = (int)(steps * (wave + 1) / kFewWaves);
@@ -644,7 +727,15 @@ __global__ __launch_bounds__(kFewWaves *kWave) void few_tokens_kernel(AdapterArg
 #pragma unroll 1
     for (; s < last; ++s) {
       const int there = (s < to ? kStep : p.k % kStep) - quarter * 8;
-      h = mfma<DT>(load8(wp + (int64_t)s * kStep, there), load8(xp + (int64_t)s * kStep, there), h);
+      const uint16_t *wa = wp + (int64_t)s * kStep, *xa = xp + (int64_t)s * kStep;
+      if (p.k >= 8) {
+        const int back_by = ahead_of<8>(there);
+        const u4 wl = *reinterpret_cast<const u4_any *>(wa - back_by);
+        const u4 xl = *reinterpret_cast<const u4_any *>(xa - back_by);
+        h = mfma<DT>(moved(wl, back_by), moved(xl, back_by), h);
+      } else {
+        h = mfma<DT>(load8(wa, there), load8(xa, there), h);
+      }
     }
     sums[wave][lane] = h;
     __syncthreads();
@@ -665,6 +756,10 @@ __global__ __launch_bounds__(kFewWaves *kWave) void few_tokens_kernel(AdapterArg
     for (int j = 0; j < 8; ++j)
 #pragma unroll
       for (int i = 0; i < CT / 2; ++i) raw[j][i] = quarter * 8 + j < p.rank ? raw[j][i] : 0;
+    if (by > 0) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) move_values<CT / 2>(raw[j], by);
+    }
     turn<CT>(raw, w);
     __syncthreads();
     if (tid < 256) {
@@ -948,6 +1043,8 @@ __global__ __launch_bounds__(kAnyWaves *kWave) void gradient_any_kernel(Gradient
   const int rank0 = blockIdx.z * (kTile * RT);
   const int col = blockIdx.x * kGradColumns + c * 8;
   const int64_t valid = (int64_t)p.width - col;
+  const bool wide = p.width >= 8;
+  const int by = wide ? ahead_of<8>(valid) : 0;
   const int low = p.ends != nullptr && g > 0 ? clamp_end(p.ends[g - 1], p.m) : 0;
   const int high = p.ends != nullptr ? clamp_end(p.ends[g], p.m) : p.m;
   f4 acc[RT][8] = {};
@@ -961,13 +1058,27 @@ __global__ __launch_bounds__(kAnyWaves *kWave) void gradient_any_kernel(Gradient
     for (int j = 0; j < 8; ++j) {
       const bool on = s + 8 * quarter + j < high;
       const int at = on ? (int)s + 8 * quarter + j : high - 1;
-      load_columns<8>(p.x + token_of(p.slots, at, p.m) * p.x_stride + col, on ? valid : 0, raw[j]);
+      const uint16_t *row_of = p.x + token_of(p.slots, at, p.m) * p.x_stride + col;
+      if (wide)
+        load_columns<8>(row_of - by, 8, raw[j]);
+      else
+        load_columns<8>(row_of, valid, raw[j]);
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         const int row = rank0 + r * kTile + c;
         const float v = p.h[at * p.h_stride + (row < p.rank ? row : p.rank - 1)];
         hv[r][j] = on ? v : 0.0f;
       }
+    }
+    if (by > 0) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) move_values<4>(raw[j], by);
+    }
+    if (s + kStep > high) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) raw[j][e] = s + 8 * quarter + j < high ? raw[j][e] : 0;
     }
     gradient_step<DT, RT, P>(raw, hv, shift, acc);
   }

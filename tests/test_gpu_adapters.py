@@ -233,6 +233,37 @@ def test_gradients_against_the_formula(dtype):
     assert torch.equal(wy, dout.double())
 
 
+WIDTHS = list(range(1, 18)) + [23, 31, 33, 127, 129, 509, 511, 513, 1023, 1025]
+
+
+def _between(t):
+    """The same values on the GPU in rows with NaN before, between and behind them, off 16 bytes."""
+    width = t.shape[-1]
+    room = torch.full((3 + t[..., 0].numel() * (width + 3) + 3,), float("nan"), dtype=t.dtype, device="cuda")
+    rows = room[3:-3].view(*t.shape[:-1], width + 3)
+    rows[..., :width] = t.cuda()
+    return rows[..., :width], room
+
+
+@pytest.mark.parametrize("dtype,out", [(F16, F16), (BF16, BF16), (F16, F32), (BF16, F32)])
+@pytest.mark.parametrize("m,rank,groups", [(9, 5, 1), (21, 16, 2), (300, 7, 2), (90, 70, 2), (150, 150, 1)])
+def test_every_width_of_the_last_columns(m, rank, groups, dtype, out):
+    """Rows narrower than a load, and whose last values a load takes from before their place: nothing
+    from outside a row gets in, and nothing outside is written."""
+    for i, width in enumerate(WIDTHS):
+        k, n = width, WIDTHS[(i * 7 + 3) % len(WIDTHS)]
+        x, down, up, y, scales, ends, slots = _make(m, k, n, rank, groups, dtype, out, idle=False)
+        (gx, _), (gd, _), (gu, _), (gy, room) = (_between(t) for t in (x, down, up, y))
+        gs, ge, gl = _cuda(scales, ends, slots)
+        got, h = _check(x, down, up, y, scales, ends, slots, out, (gx, gd, gu, gy, gs, ge, gl))
+        gap = torch.isnan(room).sum()
+        assert H.adapt_rows(gx, gd, gu, ends=ge, slots=gl, y=gy, scales=gs, out=gy) is gy
+        assert torch.equal(gy, got) and torch.isnan(room).sum() == gap
+        want, off = R.weight_gradient(h.cpu(), x, ends, slots, scales, dtype, F32)
+        grad = H.adapter_gradient(h, gx, ge, gl, scales=gs, dtype=F32)
+        R.check("gradient", grad, want, R.rounded(want, off, F32))
+
+
 def test_refusals():
     x, down, up, y, scales, ends, slots = _cuda(*_make(10, 64, 48, 8, 2, BF16))
     h = torch.zeros((10, 8), device="cuda")
