@@ -222,8 +222,7 @@ __device__ __forceinline__ Piece piece_of(const int32_t *ends, int groups, int m
 template <int DT, int TT, int RT, int U, int W>
 __global__ __launch_bounds__(W *kWave) void down_kernel(AdapterArgs p) {
   constexpr int kTiles = TT * RT;
-  constexpr int kHeld = kTiles * W > 64 ? kTiles / 2 : kTiles;  // tiles in LDS at a time
-  __shared__ f4 sums[W][kHeld][kWave];
+  __shared__ f4 sums[W][kTiles][kWave];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int c = lane % kTile, quarter = lane / kTile;
   const Piece piece = piece_of(p.ends, p.groups, p.m, kTile * TT, blockIdx.x, false);
@@ -310,23 +309,19 @@ __global__ __launch_bounds__(W *kWave) void down_kernel(AdapterArgs p) {
       for (int r = 0; r < RT; ++r) acc[t][r] = mfma<DT>(wv[0][0][r], xv[0][0][t], acc[t][r]);
   }
 #pragma unroll
-  for (int first = 0; first < kTiles; first += kHeld) {
-    if (first > 0) __syncthreads();
+  for (int i = 0; i < kTiles; ++i) sums[wave][i][lane] = acc[i / RT][i % RT];
+  __syncthreads();
+  for (int i = wave; i < kTiles; i += W) {
+    f4 v = sums[0][i][lane];
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) sums[wave][i][lane] = acc[(first + i) / RT][(first + i) % RT];
-    __syncthreads();
-    for (int i = wave; i < kHeld; i += W) {
-      f4 v = sums[0][i][lane];
+    for (int w = 1; w < W; ++w) v += sums[w][i][lane];
+    const int place = piece.low + i / RT * kTile + c;
+    const int rank = rank0 + i % RT * kTile + 4 * quarter;
 #pragma unroll
-      for (int w = 1; w < W; ++w) v += sums[w][i][lane];
-      const int place = piece.low + (first + i) / RT * kTile + c;
-      const int rank = rank0 + (first + i) % RT * kTile + 4 * quarter;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (rank + j >= p.rank) v[j] = 0.0f;
-      if (place < piece.high && rank < p.padded)
-        *reinterpret_cast<f4 *>(p.part + blockIdx.y * p.part_step + place * p.part_pitch + rank) = v;
-    }
+    for (int j = 0; j < 4; ++j)
+      if (rank + j >= p.rank) v[j] = 0.0f;
+    if (place < piece.high && rank < p.padded)
+      *reinterpret_cast<f4 *>(p.part + blockIdx.y * p.part_step + place * p.part_pitch + rank) = v;
   }
 }
 
@@ -1139,10 +1134,12 @@ struct Cut {
 
 Cut cut_of(int64_t m, int64_t k, int64_t n, int64_t rank, int64_t groups, int parts) {
   Cut cut{};
-  cut.ranks = rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8;
+  // 64 ranks at most: of more, another workgroup reads x again, but 128 in one leave no registers for
+  // loads ahead (16384 x 4096 x 4096, rank 128: 222 us a call instead of 261)
+  cut.ranks = rank <= 16 ? 1 : rank <= 32 ? 2 : 4;
   const int64_t live = groups < 1 || m < 1 ? 1 : groups < m ? groups : m;
   const bool few = m <= 32 * live;
-  cut.tiles = few ? 1 : cut.ranks == 8 ? 2 : 4;
+  cut.tiles = few ? 1 : 4;
   cut.splits = 1;
   cut.unit = kTile;
   cut.fused = few && rank <= kTile && k <= kFewDepth &&
@@ -1201,24 +1198,19 @@ void launch_down(const AdapterArgs &p, const Cut &cut, hipStream_t stream) {
   const integral_constant<int, 1> one{};
   const integral_constant<int, 2> two{};
   const integral_constant<int, 4> four{};
-  const integral_constant<int, 8> eight{};
   if (cut.tiles == 1) {
     if (cut.ranks == 1)
       go(one, one, four, four);
     else if (cut.ranks == 2)
       go(one, two, four, four);
-    else if (cut.ranks == 4)
-      go(one, four, two, four);
     else
-      go(one, eight, two, four);
+      go(one, four, two, four);
   } else if (cut.ranks == 1) {
     go(four, one, two, four);
   } else if (cut.ranks == 2) {
     go(four, two, two, four);
-  } else if (cut.ranks == 4) {
-    go(four, four, two, four);
   } else {
-    go(two, eight, one, four);
+    go(four, four, two, four);
   }
 }
 
