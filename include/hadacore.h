@@ -541,9 +541,8 @@ int64_t hadacore_adapters_workspace_size(int64_t m, int64_t k, int64_t n, int64_
  *               rank rounded up to 16): down[g] x[t] by place, zeros up to that width; places behind
  *               the last end are left as they were.  The gradient of the weights takes it
  * The gradients of x are the same call on dout with `down` and `up` exchanged and y = NULL.
- * Between the products h is fp32; the second takes it in parts of 16 bits that sum up to 16 bits of
- * it for 16-bit outputs (22 for fp16) and to 24 for fp32 (22 for fp16, of the row's largest).  Inf
- * may give NaN.
+ * Between the products h is fp32, and the second takes all of its 24 bits (for fp16 above 2^-36 of
+ * the row's largest).  Inf may give NaN.
  */
 hadacore_status hadacore_adapters(const void *x, int64_t x_row_stride, const void *down,
                                   int64_t down_row_stride, int64_t down_batch_stride,

@@ -15,11 +15,12 @@
 // that have tokens; 2 rank operations for each 2 bytes are far below what the matrix cores do.
 //
 // Sums are the matrix cores' fp32.  h stays in fp32 between the two products: the second takes it
-// in parts of 16 bits that add up to it.  Two parts of bf16 keep 16 bits of h, which a 16-bit
-// result cannot tell from all (2^-17 against 2^-9); for a 32-bit result three parts keep all 24.
-// fp16 parts are made of h times a power of two (largest value of the row near 2^10), so
-// that they keep 22 bits whatever h's size.  A value of h, a weight or an x that is Inf gives a NaN
-// where the sum without parts may give Inf: Inf times a part of 0 is NaN.
+// in three parts of 16 bits that add up to all 24 bits of it, for 16-bit results too, since the
+// adapter's part may cancel against y and leave any bit of h to be seen.  (Two parts, which keep 16
+// bits of it in bf16, save 0 to 4% of a call.)  fp16 parts are made of h times a power of two (largest
+// value of the row near 2^10): all bits of values down to 2^-11 of the row's largest, and of smaller
+// ones those above 2^-36 of it.  A value of h, a weight or an x that is Inf gives a NaN where the sum
+// without parts may give Inf: Inf times a part of 0 is NaN.
 
 #include <hip/hip_runtime.h>
 
@@ -76,19 +77,23 @@ __device__ __forceinline__ float widen(uint16_t h) {
     return __builtin_bit_cast(float, (uint32_t)h << 16);
 }
 
-// v as a sum of P values of 16 bits.  Parts of bf16 but the last are cut off, so that a NaN stays
-// one (what is left of it is a quiet NaN) and no part rounds up to Inf.
-template <int DT, int P>
-__device__ __forceinline__ void split(float v, uint16_t (&part)[P]) {
-#pragma unroll
-  for (int i = 0; i < P; ++i) {
-    if constexpr (DT == HADACORE_FP16) {
-      part[i] = narrow<DT>(v);
-    } else {
-      part[i] = i < P - 1 ? (uint16_t)(__builtin_bit_cast(uint32_t, v) >> 16) : narrow<DT>(v);
-    }
-    v -= widen<DT>(part[i]);
-  }
+constexpr int kParts = 3;
+
+// Takes part i off v, a sum of kParts values of 16 bits.  Parts of bf16 but the last are cut off, so that a
+// NaN stays one (what is left of it is a quiet NaN) and no part rounds up to Inf.
+template <int DT>
+__device__ __forceinline__ uint16_t take_part(float &v, int i) {
+  const uint16_t part = DT == HADACORE_FP16 || i == kParts - 1
+                            ? narrow<DT>(v)
+                            : (uint16_t)(__builtin_bit_cast(uint32_t, v) >> 16);
+  v -= widen<DT>(part);
+  return part;
+}
+// The same for two values, as a word.
+template <int DT>
+__device__ __forceinline__ uint32_t take_parts(float &low, float &high, int i) {
+  const uint32_t part = take_part<DT>(low, i);
+  return part | (uint32_t)take_part<DT>(high, i) << 16;
 }
 
 // The power of two that brings values of at most `most` to at most 2^11: exponent of its inverse.
@@ -427,12 +432,12 @@ struct OutRow {
 // registers so that the ranks lie along an operand.  A lane then has CT consecutive columns of each
 // of four tokens, which it loads and stores whole, the next four's y under the products of these.
 // h, joined and split, goes through LDS.  Tokens behind the last end get y.
-template <int DT, int OUT, int RB, int CT, int P, int D, bool EVEN>
+template <int DT, int OUT, int RB, int CT, int D, bool EVEN>
 __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
-  constexpr int kPitch = kStep * RB + 8;
+  constexpr int P = kParts, kPitch = kStep * RB + 8;
   constexpr int kSize = OUT == HADACORE_FP32 ? 4 : 2;
   extern __shared__ __attribute__((aligned(16))) uint8_t room[];
-  uint16_t *parts = reinterpret_cast<uint16_t *>(room);  // [P][unit][kPitch]
+  uint16_t *parts = reinterpret_cast<uint16_t *>(room);  // [unit][P][kPitch]
   float *back = reinterpret_cast<float *>(parts + P * p.unit * kPitch);
   int *tokens = reinterpret_cast<int *>(back + p.unit);
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
@@ -528,13 +533,15 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
     for (int i = 0; i < kEach; ++i) {
       const int r = i * 64 + q * 4;
       if (r >= kStep * RB) continue;
-      uint16_t v[4][P];
+      float v[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) split<DT, P>(h[i][j] * shift, v[j]);
+      for (int j = 0; j < 4; ++j) v[j] = h[i][j] * shift;
 #pragma unroll
-      for (int k = 0; k < P; ++k)
-        *reinterpret_cast<u2 *>(parts + (k * p.unit + t) * kPitch + r) =
-            u2{v[0][k] | (uint32_t)v[1][k] << 16, v[2][k] | (uint32_t)v[3][k] << 16};
+      for (int k = 0; k < P; ++k) {
+        const uint32_t low = take_parts<DT>(v[0], v[1], k);
+        *reinterpret_cast<u2 *>(parts + (t * P + k) * kPitch + r) =
+            u2{low, take_parts<DT>(v[2], v[3], k)};
+      }
     }
   }
   u4 w[RB][CT];
@@ -565,7 +572,7 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
 #pragma unroll
       for (int k = P - 1; k >= 0; --k) {
         const u4 a = *reinterpret_cast<const u4 *>(
-            parts + (k * p.unit + t0 + c) * kPitch + b * kStep + quarter * 8);
+            parts + ((t0 + c) * P + k) * kPitch + b * kStep + quarter * 8);
 #pragma unroll
         for (int i = 0; i < CT; ++i) acc[i] = mfma<DT>(a, w[b][i], acc[i]);
       }
@@ -641,9 +648,9 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
 // 256 tokens of 64 adapters gain nothing, rank 64 takes 20 instead of 9.
 constexpr int kFewWaves = 8;
 
-template <int DT, int OUT, int P, bool EVEN>
+template <int DT, int OUT, bool EVEN>
 __global__ __launch_bounds__(kFewWaves *kWave) void few_tokens_kernel(AdapterArgs p) {
-  constexpr int CT = 8, U = 4, kPitch = kStep + 8;
+  constexpr int CT = 8, U = 4, P = kParts, kPitch = kStep + 8;
   constexpr int kSize = OUT == HADACORE_FP32 ? 4 : 2;
   __shared__ f4 sums[kFewWaves][kWave];
   __shared__ __attribute__((aligned(16))) float hs[kTile][kTile + 4];
@@ -774,13 +781,14 @@ __global__ __launch_bounds__(kFewWaves *kWave) void few_tokens_kernel(AdapterArg
         if (q == 0) back[t] = power_of_two(e);
       }
       if (r < kStep) {
-        uint16_t part[4][P];
+        float rest[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) split<DT, P>(v[j] * shift, part[j]);
+        for (int j = 0; j < 4; ++j) rest[j] = v[j] * shift;
 #pragma unroll
-        for (int k = 0; k < P; ++k)
-          *reinterpret_cast<u2 *>(&parts[k][t][r]) =
-              u2{part[0][k] | (uint32_t)part[1][k] << 16, part[2][k] | (uint32_t)part[3][k] << 16};
+        for (int k = 0; k < P; ++k) {
+          const uint32_t low = take_parts<DT>(rest[0], rest[1], k);
+          *reinterpret_cast<u2 *>(&parts[k][t][r]) = u2{low, take_parts<DT>(rest[2], rest[3], k)};
+        }
       }
     }
     __syncthreads();
@@ -832,9 +840,10 @@ constexpr int kGradColumns = kTile * 8;
 
 // A step of 32 tokens of dW[g]: their h (hv: rank c of 16 and tokens 8 quarter + j) times their x
 // (raw: the same tokens, 8 columns).  fp16: h is taken times 2^-shift, and `shift` grows with h.
-template <int DT, int RT, int P>
+template <int DT, int RT>
 __device__ __forceinline__ void gradient_step(const uint32_t (&raw)[8][4], const float (&hv)[RT][8],
                                               int &shift, f4 (&acc)[RT][8]) {
+  constexpr int P = kParts;
   float scale = 1.0f;
   if constexpr (DT == HADACORE_FP16) {
     float most = 0.0f;
@@ -857,17 +866,18 @@ __device__ __forceinline__ void gradient_step(const uint32_t (&raw)[8][4], const
   turn<8>(raw, xc);
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    uint16_t v[8][P];
+    float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) split<DT, P>(hv[r][j] * scale, v[j]);
+    for (int j = 0; j < 8; ++j) v[j] = hv[r][j] * scale;
+    u4 a[P];
 #pragma unroll
-    for (int k = P - 1; k >= 0; --k) {
-      u4 a;
+    for (int k = 0; k < P; ++k)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) a[j] = v[2 * j][k] | (uint32_t)v[2 * j + 1][k] << 16;
+      for (int j = 0; j < 4; ++j) a[k][j] = take_parts<DT>(v[2 * j], v[2 * j + 1], k);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[r][i] = mfma<DT>(a, xc[i], acc[r][i]);
-    }
+    for (int k = P - 1; k >= 0; --k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[r][i] = mfma<DT>(a[k], xc[i], acc[r][i]);
   }
 }
 
@@ -912,7 +922,7 @@ __device__ __forceinline__ void store_gradient(const GradientArgs &p, int g, int
 // (8191 x 4096, four adapters of rank 16: 27 us; with the loads in registers, a step ahead, 31).
 constexpr int kGradWaves = 2;
 
-template <int DT, int OUT, int RT, int P>
+template <int DT, int OUT, int RT>
 __global__ __launch_bounds__(kGradWaves *kWave) void gradient_kernel(GradientArgs p) {
   constexpr int D = RT == 4 ? 2 : 3;  // stages of the ring: two workgroups to a CU
   constexpr int kX = kStep * kGradColumns * 2, kH = RT * kStep * kTile * 4;
@@ -1019,7 +1029,7 @@ __global__ __launch_bounds__(kGradWaves *kWave) void gradient_kernel(GradientArg
         for (int r = 0; r < RT; ++r) hv[r][j] = on ? hv[r][j] : 0.0f;
       }
     }
-    gradient_step<DT, RT, P>(raw, hv, shift, acc);
+    gradient_step<DT, RT>(raw, hv, shift, acc);
   }
   store_gradient<DT, OUT, RT, kGradWaves>(p, g, rank0, shift, acc,
                                           reinterpret_cast<f4(*)[8][kWave + 1]>(room));
@@ -1029,7 +1039,7 @@ __global__ __launch_bounds__(kGradWaves *kWave) void gradient_kernel(GradientArg
 // is loaded ahead.
 constexpr int kAnyWaves = 8;
 
-template <int DT, int OUT, int RT, int P>
+template <int DT, int OUT, int RT>
 __global__ __launch_bounds__(kAnyWaves *kWave) void gradient_any_kernel(GradientArgs p) {
   __shared__ f4 sums[kAnyWaves][8][kWave + 1];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
@@ -1075,7 +1085,7 @@ __global__ __launch_bounds__(kAnyWaves *kWave) void gradient_any_kernel(Gradient
 #pragma unroll
         for (int e = 0; e < 4; ++e) raw[j][e] = s + 8 * quarter + j < high ? raw[j][e] : 0;
     }
-    gradient_step<DT, RT, P>(raw, hv, shift, acc);
+    gradient_step<DT, RT>(raw, hv, shift, acc);
   }
   store_gradient<DT, OUT, RT, kAnyWaves>(p, g, rank0, shift, acc, sums);
 }
@@ -1132,7 +1142,7 @@ struct Cut {
   int unit;    // tokens of a workgroup of up_kernel
 };
 
-Cut cut_of(int64_t m, int64_t k, int64_t n, int64_t rank, int64_t groups, int parts) {
+Cut cut_of(int64_t m, int64_t k, int64_t n, int64_t rank, int64_t groups) {
   Cut cut{};
   // 64 ranks at most: of more, another workgroup reads x again, but 128 in one leave no registers for
   // loads ahead (16384 x 4096 x 4096, rank 128: 222 us a call instead of 261)
@@ -1154,7 +1164,7 @@ Cut cut_of(int64_t m, int64_t k, int64_t n, int64_t rank, int64_t groups, int pa
   cut.splits = (int)(splits < 1 ? 1 : splits > 16 ? 16 : splits);
   const int64_t depth = round_up(rank, kStep), columns = divide_up(n, rank > 128 ? 256 : 512);
   cut.unit = 16;
-  while (cut.unit < 128 && !few && 2 * cut.unit * (depth + 8) * 2 * parts <= 48 * 1024 &&
+  while (cut.unit < 128 && !few && 2 * cut.unit * (depth + 8) * 2 * kParts <= 48 * 1024 &&
          m / (2 * cut.unit) * columns >= (rank > 64 ? 1 : 2) * kBlocksWanted)
     cut.unit *= 2;
   return cut;
@@ -1177,11 +1187,6 @@ void for_type(hadacore_dtype dtype, F f) {
     f(std::integral_constant<int, HADACORE_FP16>{});
   else
     f(std::integral_constant<int, HADACORE_BF16>{});
-}
-
-// Parts of h: see the top of the file.
-constexpr int parts_of(int dtype, int out) {
-  return dtype == HADACORE_BF16 && out == HADACORE_FP32 ? 3 : 2;
 }
 
 template <int DT>
@@ -1216,7 +1221,6 @@ void launch_down(const AdapterArgs &p, const Cut &cut, hipStream_t stream) {
 
 template <int DT, int OUT>
 void launch_up(AdapterArgs p, hipStream_t stream) {
-  constexpr int P = parts_of(DT, OUT);
   const int64_t pieces = most_pieces(p.m, p.groups, p.unit);
   // EVEN: columns in whole tiles, and rows of y and out from the start of a line
   constexpr int64_t kLine = 128 / (OUT == HADACORE_FP32 ? 4 : 2);
@@ -1225,15 +1229,15 @@ void launch_up(AdapterArgs p, hipStream_t stream) {
   constexpr int kAhead = 2;
   const auto go = [&](auto rb, auto ct) {
     constexpr int RB = decltype(rb)::value, CT = decltype(ct)::value;
-    const size_t lds = (size_t)p.unit * (P * (kStep * RB + 8) * 2 + 8);
+    const size_t lds = (size_t)p.unit * (kParts * (kStep * RB + 8) * 2 + 8);
     // the columns of a token's row run together: whole rows of y and out, and with as many chunks as
     // XCDs (or a multiple) each of them meets only its own columns of the weights
     p.chunks = p.n > 0 ? (int)divide_up(p.n, 4 * 16 * CT) : 1;  // without columns h is joined
     const dim3 grid((uint32_t)(pieces * p.chunks));
     if (p.n > 0 && p.n % (16 * CT) == 0 && lines)
-      hipLaunchKernelGGL((up_kernel<DT, OUT, RB, CT, P, kAhead, true>), grid, dim3(256), lds, stream, p);
+      hipLaunchKernelGGL((up_kernel<DT, OUT, RB, CT, kAhead, true>), grid, dim3(256), lds, stream, p);
     else
-      hipLaunchKernelGGL((up_kernel<DT, OUT, RB, CT, P, kAhead, false>), grid, dim3(256), lds, stream, p);
+      hipLaunchKernelGGL((up_kernel<DT, OUT, RB, CT, kAhead, false>), grid, dim3(256), lds, stream, p);
   };
   using std::integral_constant;
   const integral_constant<int, 8> eight{};
@@ -1249,28 +1253,26 @@ void launch_up(AdapterArgs p, hipStream_t stream) {
 
 template <int DT, int OUT>
 void launch_few(AdapterArgs p, hipStream_t stream) {
-  constexpr int P = parts_of(DT, OUT);
   p.chunks = p.n > 0 ? (int)divide_up(p.n, kFewWaves * 128) : 1;
   const dim3 grid((uint32_t)(most_pieces(p.m, p.groups, kTile) * p.chunks));
   if (p.n > 0 && p.n % 128 == 0)
-    hipLaunchKernelGGL((few_tokens_kernel<DT, OUT, P, true>), grid, dim3(kFewWaves * kWave), 0, stream, p);
+    hipLaunchKernelGGL((few_tokens_kernel<DT, OUT, true>), grid, dim3(kFewWaves * kWave), 0, stream, p);
   else
-    hipLaunchKernelGGL((few_tokens_kernel<DT, OUT, P, false>), grid, dim3(kFewWaves * kWave), 0, stream, p);
+    hipLaunchKernelGGL((few_tokens_kernel<DT, OUT, false>), grid, dim3(kFewWaves * kWave), 0, stream, p);
 }
 
 template <int DT, int OUT>
 void launch_gradient(const GradientArgs &p, hipStream_t stream) {
-  constexpr int P = parts_of(DT, OUT);
   const int ranks = p.rank <= 16 ? 1 : p.rank <= 32 ? 2 : 4;
   const dim3 grid((uint32_t)divide_up(p.width, kGradColumns), (uint32_t)(p.groups * p.splits),
                   (uint32_t)divide_up(p.rank, 16 * ranks));
   const bool streams = aligned_to(p.x, 16) && p.x_stride % 8 == 0 && p.width % 8 == 0;
   const auto go = [&](auto rt) {
     if (streams)
-      hipLaunchKernelGGL((gradient_kernel<DT, OUT, decltype(rt)::value, P>), grid,
+      hipLaunchKernelGGL((gradient_kernel<DT, OUT, decltype(rt)::value>), grid,
                          dim3(kGradWaves * kWave), 0, stream, p);
     else
-      hipLaunchKernelGGL((gradient_any_kernel<DT, OUT, decltype(rt)::value, P>), grid,
+      hipLaunchKernelGGL((gradient_any_kernel<DT, OUT, decltype(rt)::value>), grid,
                          dim3(kAnyWaves * kWave), 0, stream, p);
   };
   using std::integral_constant;
@@ -1352,7 +1354,7 @@ using namespace hadacore;
 extern "C" int64_t hadacore_adapters_workspace_size(int64_t m, int64_t k, int64_t n, int64_t rank,
                                                     int64_t groups) {
   if (check_sizes(m, k, n, rank, groups) != HADACORE_SUCCESS) return 0;
-  const Cut cut = cut_of(m, k, n, rank, groups, 2);
+  const Cut cut = cut_of(m, k, n, rank, groups);
   return cut.fused ? 0 : cut.splits * m * round_up(rank, 16) * 4;
 }
 
@@ -1405,7 +1407,7 @@ extern "C" hadacore_status hadacore_adapters(
       spans_overlap(sy, sh) || spans_overlap(sy, sw) ||
       (spans_overlap(so, sy) && !(out == y && (out_row_stride == y_row_stride || m == 1))))
     return HADACORE_ERROR_OVERLAP;
-  const Cut cut = cut_of(m, k, n, rank, groups, parts_of(dtype, out_dtype));
+  const Cut cut = cut_of(m, k, n, rank, groups);
   // up_kernel's launch, the largest
   if (!cut.fused && most_pieces(m, groups, cut.unit) * divide_up(n, rank > 128 ? 256 : 512) * 256 >=
                         (int64_t(1) << 32))
