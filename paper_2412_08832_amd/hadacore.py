@@ -20,6 +20,11 @@ ROCm device, and so are, for codes with a scale per block of 128, ``transform_fp
 ``grouped_weight_gradient_fp8``; for tokens and weights of their own ``route_tokens``,
 ``route_tokens_gradient``, ``group_tokens``, ``dispatch_rows``, ``combine_rows``,
 ``combine_rows_gradient``, ``adapt_rows`` and ``adapter_gradient``.
+
+Wrappers work on torch's current stream, or on ``stream`` (a torch stream or its handle) as if it were the
+current one: outputs that they create, and workspaces, are of its memory.  As with torch's own streams, the
+caller has ``stream`` wait for the inputs and keeps them until its work is done, and waits for it
+before using the outputs elsewhere.
 """
 from __future__ import annotations
 
@@ -505,6 +510,39 @@ def _call(name: str, device: int, *args) -> None:
         raise HadacoreError(status, name)
 
 
+class _Entered:
+    """A stream given to a wrapper, which is torch's current one now."""
+    __slots__ = ("stream", "cuda_stream")
+
+    def __init__(self, stream):
+        self.stream, self.cuda_stream = stream, stream.cuda_stream
+
+
+def _on_stream(stream, x, call):
+    """``call`` with ``stream`` (a torch stream or a handle; 0 is the default one), made torch's current one
+    for the time: new outputs and workspaces are of its memory, which is handed out in its order.  Of
+    torch's current stream they could be in use by work that is still to run there, or be handed out
+    again before ``stream`` is done.  Outputs are marked as used on the caller's stream, too."""
+    device = x.get_device()
+    if device < 0:
+        return call(None)  # which refuses such a tensor
+    here = _torch.cuda.current_stream(device)
+    handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
+    if handle == here.cuda_stream:
+        return call(_Entered(here))
+    if not isinstance(stream, _torch.cuda.Stream):
+        stream = (_torch.cuda.ExternalStream(handle, device=device) if handle
+                  else _torch.cuda.default_stream(device))
+    elif stream.device_index != device:
+        raise ValueError(f"the stream is of device {stream.device_index}, the tensors of {device}")
+    with _torch.cuda.stream(stream):
+        result = call(_Entered(stream))
+    for t in result if isinstance(result, tuple) else (result,):
+        if isinstance(t, _torch.Tensor):
+            t.record_stream(here)
+    return result
+
+
 def transform(x, out=None, scale: float | None = None, n: int | None = None, stream=None,
               workspace=None):
     """out = scale * x @ H_n over the first ``n`` columns of each row of a 2-D tensor.
@@ -518,6 +556,8 @@ def transform(x, out=None, scale: float | None = None, n: int | None = None, str
     """
     if _torch is None:
         _init_torch()
+    if stream is not None and type(stream) is not _Entered:
+        return _on_stream(stream, x, lambda s: transform(x, out, scale, n, s, workspace))
     if x.dim() != 2 or not x.is_cuda:
         raise ValueError("expected a 2-D tensor on a ROCm device")
     in_stride, column = x.stride()
@@ -537,10 +577,7 @@ def transform(x, out=None, scale: float | None = None, n: int | None = None, str
     if scale is None:
         scale = _default_scale(n)
     device = x.get_device()
-    if stream is None:
-        stream = _raw_stream(device)
-    elif hasattr(stream, "cuda_stream"):
-        stream = stream.cuda_stream
+    stream = _raw_stream(device) if stream is None else stream.cuda_stream
     # a single row's stride is never used to address anything; report n
     if m > 1:
         out_stride = out.stride(0)
@@ -562,6 +599,9 @@ def transform(x, out=None, scale: float | None = None, n: int | None = None, str
 def _transform_quantized(x, codes, scales, scale, stream, entry, int8):
     if _torch is None:
         _init_torch()
+    if stream is not None and type(stream) is not _Entered:
+        return _on_stream(stream, x, lambda s: _transform_quantized(x, codes, scales, scale, s, entry,
+                                                                    int8))
     codes_dtype = _torch.int8 if int8 else _torch.uint8
     if x.dim() != 2 or not x.is_cuda or x.stride(1) != 1:
         raise ValueError("expected a 2-D ROCm tensor with contiguous rows")
@@ -579,10 +619,7 @@ def _transform_quantized(x, codes, scales, scale, stream, entry, int8):
     if scale is None:
         scale = _default_scale(n)
     device = x.get_device()
-    if stream is None:
-        stream = _raw_stream(device)
-    elif hasattr(stream, "cuda_stream"):
-        stream = stream.cuda_stream
+    stream = _raw_stream(device) if stream is None else stream.cuda_stream
     in_stride = x.stride(0) if m > 1 else n
     codes_stride = codes.stride(0) if m > 1 else ((n + 15) // 16) * 16
     _call(entry, device, x.data_ptr(), in_stride, codes.data_ptr(), codes_stride,
@@ -612,9 +649,7 @@ def transform_int8(x, codes=None, scales=None, scale: float | None = None, strea
 
 
 def _stream_of(stream, device: int):
-    if stream is None:
-        return _raw_stream(device)
-    return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
+    return _raw_stream(device) if stream is None else stream.cuda_stream
 
 
 # The wrappers below allocate with empty_strided, a few tenths of a microsecond faster
@@ -701,6 +736,8 @@ def transform_fp8_blocks(x, n: int | None = None, codes=None, scales=None,
     """
     if _torch is None:
         _init_torch()
+    if stream is not None and type(stream) is not _Entered:
+        return _on_stream(stream, x, lambda s: transform_fp8_blocks(x, n, codes, scales, scale, s))
     device = x.get_device()
     if device < 0 or x.dim() != 2:
         raise ValueError("expected a 2-D tensor on a ROCm device")
@@ -739,6 +776,8 @@ def quantize_fp8_columns(x, ends=None, codes=None, scales=None, stream=None):
     """
     if _torch is None:
         _init_torch()
+    if stream is not None and type(stream) is not _Entered:
+        return _on_stream(stream, x, lambda s: quantize_fp8_columns(x, ends, codes, scales, s))
     device = x.get_device()
     if device < 0 or x.dim() != 2:
         raise ValueError("expected a 2-D tensor on a ROCm device")
@@ -771,6 +810,8 @@ def quantize_fp8_tiles(w, transposed: bool = False, stream=None):
     """
     if _torch is None:
         _init_torch()
+    if stream is not None and type(stream) is not _Entered:
+        return _on_stream(stream, w, lambda s: quantize_fp8_tiles(w, transposed, s))
     device = w.get_device()
     lead = w.shape[:-2]
     if device < 0 or len(lead) != w.dim() - 2 or len(lead) > 1:
@@ -831,6 +872,8 @@ def matmul_fp8(a, a_scales, b, b_scales, out=None, dtype=None, stream=None):
     """
     if _torch is None:
         _init_torch()
+    if stream is not None and type(stream) is not _Entered:
+        return _on_stream(stream, a, lambda s: matmul_fp8(a, a_scales, b, b_scales, out, dtype, s))
     device = a.get_device()
     if device < 0 or a.dim() != 2 or b.dim() != 2:
         raise ValueError("expected 2-D tensors on a ROCm device")
@@ -858,6 +901,9 @@ def grouped_matmul_fp8(a, a_scales, b, b_scales, ends, out=None, dtype=None, str
     """
     if _torch is None:
         _init_torch()
+    if stream is not None and type(stream) is not _Entered:
+        return _on_stream(stream, a, lambda s: grouped_matmul_fp8(a, a_scales, b, b_scales, ends,
+                                                                  out, dtype, s))
     device = a.get_device()
     if device < 0 or a.dim() != 2 or b.dim() != 3:
         raise ValueError("expected a 2-D and a 3-D tensor on a ROCm device")
@@ -889,6 +935,10 @@ def grouped_weight_gradient_fp8(dy, dy_scales, x, x_scales, ends=None, out=None,
     """
     if _torch is None:
         _init_torch()
+    if stream is not None and type(stream) is not _Entered:
+        return _on_stream(stream, dy, lambda s: grouped_weight_gradient_fp8(dy, dy_scales, x,
+                                                                            x_scales, ends, out,
+                                                                            dtype, s))
     device = dy.get_device()
     if device < 0 or dy.dim() != 2 or x.dim() != 2:
         raise ValueError("expected 2-D tensors on a ROCm device")
@@ -947,16 +997,13 @@ def _words(n: int, device, dtype=None):
 
 
 def _scratch(nbytes: int, device, stream):
-    """A workspace of the current stream's memory (None for no bytes) for work on ``stream``: given as
-    an argument, that may be another one, and the memory is not to be reused before it is done."""
+    """A workspace (None for no bytes) of the current stream's memory, which a stream given to the wrapper
+    has become; marked as that stream's, so that it is not reused before its work is done."""
     if not nbytes:
         return None, None
     t = _words(nbytes >> 2, device)
     if stream is not None:
-        if not hasattr(stream, "cuda_stream"):
-            stream = (_torch.cuda.ExternalStream(stream, device=device) if stream
-                      else _torch.cuda.default_stream(device))
-        t.record_stream(stream)
+        t.record_stream(stream.stream)
     return t, t.data_ptr()
 
 
@@ -1013,6 +1060,8 @@ def route_tokens(logits, k: int, renormalize: bool = True, valid=None, stream=No
     """
     if _torch is None:
         _init_torch()
+    if stream is not None and type(stream) is not _Entered:
+        return _on_stream(stream, logits, lambda s: route_tokens(logits, k, renormalize, valid, s))
     device = logits.get_device()
     stride = _matrix("logits", logits, device)
     code = _value_code("logits", logits)
@@ -1039,6 +1088,9 @@ def route_tokens_gradient(logits, routes: Routes, dweights=None, dloss=None, out
     ``routes.loss`` (a scalar tensor); None is no gradient."""
     if _torch is None:
         _init_torch()
+    if stream is not None and type(stream) is not _Entered:
+        return _on_stream(stream, logits, lambda s: route_tokens_gradient(logits, routes,
+                                                                          dweights, dloss, out, s))
     device = logits.get_device()
     stride = _matrix("logits", logits, device)
     code = _value_code("logits", logits)
@@ -1069,6 +1121,8 @@ def group_tokens(ids, groups: int, stream=None) -> Groups:
     """
     if _torch is None:
         _init_torch()
+    if stream is not None and type(stream) is not _Entered:
+        return _on_stream(stream, ids, lambda s: group_tokens(ids, groups, s))
     device = ids.get_device()
     if device < 0 or ids.dim() not in (1, 2) or ids.dtype is not _torch.int32 or not ids.is_contiguous():
         raise ValueError("ids must be a contiguous 1-D or 2-D int32 tensor on a ROCm device")
@@ -1098,6 +1152,8 @@ def dispatch_rows(x, rows, ends, out=None, stream=None):
     and ``ends`` are ``group_tokens``'.  Its gradient is ``combine_rows`` without weights."""
     if _torch is None:
         _init_torch()
+    if stream is not None and type(stream) is not _Entered:
+        return _on_stream(stream, x, lambda s: dispatch_rows(x, rows, ends, out, s))
     device = x.get_device()
     stride = _matrix("x", x, device)
     m, k, rows_ptr = _slots_of(rows, device)
@@ -1126,6 +1182,8 @@ def combine_rows(y, rows, weights=None, out=None, stream=None):
     without a row (-1) adds nothing; ``weights`` is float32 of rows' shape, or None for the sum."""
     if _torch is None:
         _init_torch()
+    if stream is not None and type(stream) is not _Entered:
+        return _on_stream(stream, y, lambda s: combine_rows(y, rows, weights, out, s))
     device = y.get_device()
     stride = _matrix("y", y, device)
     code = _value_code("y", y)
@@ -1144,6 +1202,9 @@ def combine_rows_gradient(dout, y, rows, ends, weights=None, want_dy: bool = Tru
     dweights out, ``want_dy=False`` dy: None in their places."""
     if _torch is None:
         _init_torch()
+    if stream is not None and type(stream) is not _Entered:
+        return _on_stream(stream, dout, lambda s: combine_rows_gradient(dout, y, rows, ends,
+                                                                        weights, want_dy, s))
     device = dout.get_device()
     stride = _matrix("dout", dout, device)
     code = _value_code("dout", dout)
@@ -1199,6 +1260,9 @@ def adapt_rows(x, down, up, ends=None, slots=None, y=None, scales=None, out=None
     """
     if _torch is None:
         _init_torch()
+    if stream is not None and type(stream) is not _Entered:
+        return _on_stream(stream, x, lambda s: adapt_rows(x, down, up, ends, slots, y, scales,
+                                                          out, dtype, hidden, s))
     device = x.get_device()
     x_stride = _matrix("x", x, device)
     code = _dtype_code(x)
@@ -1252,6 +1316,9 @@ def adapter_gradient(h, x, ends=None, slots=None, scales=None, out=None, dtype=N
     """
     if _torch is None:
         _init_torch()
+    if stream is not None and type(stream) is not _Entered:
+        return _on_stream(stream, x, lambda s: adapter_gradient(h, x, ends, slots, scales, out,
+                                                                dtype, s))
     device = x.get_device()
     x_stride, h_stride = _matrix("x", x, device), _matrix("h", h, device)
     code = _dtype_code(x)
