@@ -563,7 +563,9 @@ int64_t hadacore_adapter_gradient_workspace_size(int64_t m, int64_t width, int64
  * hadacore_adapter_gradient -- out[g] (rank x width) = scales[g] * sum over the places p of g of
  * hidden[p] x[token of p]^T: the gradient of `up` from hidden and dout, and that of `down` from the
  * hidden of the gradient's call (dout, roles exchanged) and x.  A group without tokens gets
- * zeros.  out_dtype is `dtype` or HADACORE_FP32; other arguments as for hadacore_adapters.
+ * zeros.  All 24 bits of hidden are taken (for fp16 above 2^-36 of the rank's largest value in the
+ * group), and a rank's values show in its own row only, Inf and NaN too.  out_dtype is `dtype` or
+ * HADACORE_FP32; other arguments as for hadacore_adapters.
  */
 hadacore_status hadacore_adapter_gradient(const float *hidden, int64_t hidden_row_stride,
                                           const void *x, int64_t x_row_stride,

@@ -839,33 +839,45 @@ __device__ __forceinline__ void store_value(void *out, int64_t at, float v) {
 constexpr int kGradColumns = kTile * 8;
 
 // A step of 32 tokens of dW[g]: their h (hv: rank c of 16 and tokens 8 quarter + j) times their x
-// (raw: the same tokens, 8 columns).  fp16: h is taken times 2^-shift, and `shift` grows with h.
+// (raw: the same tokens, 8 columns).  fp16: h is taken times 2^-shift, a power of its own for each rank
+// that grows with its values: what is large in one rank, or Inf, takes no bits of the others.
 template <int DT, int RT>
 __device__ __forceinline__ void gradient_step(const uint32_t (&raw)[8][4], const float (&hv)[RT][8],
-                                              int &shift, f4 (&acc)[RT][8]) {
+                                              int (&shift)[RT], f4 (&acc)[RT][8]) {
   constexpr int P = kParts;
-  float scale = 1.0f;
   if constexpr (DT == HADACORE_FP16) {
-    float most = 0.0f;
+    int next[RT];
+    bool grows = false;
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
+    for (int r = 0; r < RT; ++r) {
+      float most = 0.0f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(hv[r][j]));
-    const int e = scale_exponent(max_lanes(most, kWave));
-    if (e > shift) {
-      const float less = shift - e < -126 ? 0.0f : power_of_two(shift - e);
-#pragma unroll
-      for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) acc[r][i] *= less;
-      shift = e;
+      most = fmaxf(most, __shfl_xor(most, kTile));
+      const int e = scale_exponent(fmaxf(most, __shfl_xor(most, 2 * kTile)));
+      next[r] = e > shift[r] ? e : shift[r];
+      grows |= e > shift[r];
     }
-    scale = power_of_two(-shift);
+    if (__any(grows)) {
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const float less = shift[r] - next[r] < -126 ? 0.0f : power_of_two(shift[r] - next[r]);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          // the sums of rank 4 quarter + v
+          const float by = __shfl(less, 4 * (threadIdx.x % kWave / kTile) + v);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[r][i][v] *= by;
+        }
+        shift[r] = next[r];
+      }
+    }
   }
   u4 xc[8];
   turn<8>(raw, xc);
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
+    const float scale = DT == HADACORE_FP16 ? power_of_two(-shift[r]) : 1.0f;
     float v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = hv[r][j] * scale;
@@ -883,13 +895,18 @@ __device__ __forceinline__ void gradient_step(const uint32_t (&raw)[8][4], const
 
 // Adds up the W waves' sums and stores them, or leaves them in the workspace.
 template <int DT, int OUT, int RT, int W>
-__device__ __forceinline__ void store_gradient(const GradientArgs &p, int g, int rank0, int shift,
-                                               const f4 (&acc)[RT][8], f4 (*sums)[8][kWave + 1]) {
+__device__ __forceinline__ void store_gradient(const GradientArgs &p, int g, int rank0,
+                                               const int (&shift)[RT], const f4 (&acc)[RT][8],
+                                               f4 (*sums)[8][kWave + 1]) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const float unshift = DT == HADACORE_FP16 ? power_of_two(shift) : 1.0f;
   const float factor = p.scales != nullptr ? p.scales[g] : 1.0f;
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
+    f4 unshift = f4{1, 1, 1, 1};
+    if constexpr (DT == HADACORE_FP16) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) unshift[v] = power_of_two(__shfl(shift[r], 4 * (lane / kTile) + v));
+    }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 8; ++i) sums[wave][i][lane] = acc[r][i] * unshift;
@@ -981,7 +998,9 @@ __global__ __launch_bounds__(kGradWaves *kWave) void gradient_kernel(GradientArg
     }
   };
   f4 acc[RT][8] = {};
-  int shift = -100, stage = 1;
+  int shift[RT], stage = 1;
+#pragma unroll
+  for (int r = 0; r < RT; ++r) shift[r] = -100;
   // Turn i loads the tokens of step i + D and the rows of step i + D - 1, and multiplies step i.
   // In flight before its wait, in order (D = 3): the rows of step i, the tokens of i + 2, the rows of
   // i + 1, the tokens of i + 3; all but the last two have to be there.  (D = 2: the tokens of
@@ -1053,7 +1072,9 @@ __global__ __launch_bounds__(kAnyWaves *kWave) void gradient_any_kernel(Gradient
   const int low = p.ends != nullptr && g > 0 ? clamp_end(p.ends[g - 1], p.m) : 0;
   const int high = p.ends != nullptr ? clamp_end(p.ends[g], p.m) : p.m;
   f4 acc[RT][8] = {};
-  int shift = -100;
+  int shift[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) shift[r] = -100;
   const int stride = kStep * kAnyWaves * p.splits;
 #pragma unroll 1
   for (int64_t s = low + (int64_t)(share * kAnyWaves + wave) * kStep; s < high; s += stride) {
