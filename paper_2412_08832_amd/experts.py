@@ -234,10 +234,17 @@ def combine(y: torch.Tensor, groups: hadacore.Groups, weights: torch.Tensor | No
     return _Combine.apply(y.contiguous(), weights, groups.rows, groups.ends)
 
 
+def _check_router(logits: torch.Tensor, experts: int) -> None:
+    """A choice past the last expert would be a slot of no group, whose share of its token is lost."""
+    if logits.dim() != 2 or logits.shape[1] != experts:
+        raise ValueError(f"logits of {tuple(logits.shape)} for {experts} experts: expected a column for each")
+
+
 def mixture(x: torch.Tensor, logits: torch.Tensor, w: torch.Tensor, k: int, renormalize: bool = True,
             valid: torch.Tensor | None = None, rotate: int | None = None):
     """(out, routes): each token's ``k`` experts of ``w`` (experts x n x k) by ``logits`` (tokens x
     experts), joined by their weights; with gradients of x, logits (also for ``routes.loss``) and w."""
+    _check_router(logits, w.shape[0])
     routes = route(logits, k, renormalize, valid)
     groups = hadacore.group_tokens(routes.experts, w.shape[0])
     return combine(train_linear(dispatch(x, groups), w, groups.ends, rotate), groups, routes.weights), routes
@@ -247,6 +254,7 @@ def serve_mixture(x: torch.Tensor, logits: torch.Tensor, weights: Weights, k: in
                   valid: torch.Tensor | None = None) -> torch.Tensor:
     """``mixture`` for quantized weights, without gradients: tokens are rotated and quantized once, and
     their codes dispatched."""
+    _check_router(logits, weights.codes.shape[0])
     routes = hadacore.route_tokens(logits, k, renormalize, valid)
     groups = hadacore.group_tokens(routes.experts, weights.codes.shape[0])
     a, a_scales = hadacore.transform_fp8_blocks(x, n=weights.rotate)
