@@ -13,8 +13,8 @@ get zero rows.
     y = experts.linear(x, weights)                         # FP8, or any projection
     y = adapters.adapt(y, x, down, up, groups, scales)
 
-``adapt`` has gradients of y, x, down and up (first derivatives only); without any to make it is one
-call of ``hadacore.adapt_rows``, and ``adapt_rows(..., out=y)`` adds in place.
+``adapt`` has gradients of y, x, down and up (first derivatives only, no forward mode); without any to
+make it is one call of ``hadacore.adapt_rows``, and ``adapt_rows(..., out=y)`` adds in place.
 
 ``python -m paper_2412_08832_amd.adapters`` runs a projection in FP8 with the adapters of a batch of
 requests forward and backward on the GPU and prints its errors against 32 bits.
@@ -22,6 +22,7 @@ requests forward and backward on the GPU and prints its errors against 32 bits.
 from __future__ import annotations
 
 import torch
+from torch.autograd import forward_ad
 
 from . import hadacore
 from .experts import _NoSecondDerivative
@@ -71,7 +72,8 @@ def adapt(y: torch.Tensor, x: torch.Tensor, down: torch.Tensor, up: torch.Tensor
     ends, slots = (None, None) if groups is None else (groups.ends, groups.slots)
     if scales is not None and scales.requires_grad:
         raise ValueError("the adapters' scales have no gradient")
-    if torch.is_grad_enabled() and any(t.requires_grad for t in (y, x, down, up)):
+    # where forward mode is on, too: the function refuses tensors with tangents, which a call would drop
+    if forward_ad._current_level >= 0 or torch.is_grad_enabled() and any(t.requires_grad for t in (y, x, down, up)):
         return _Adapt.apply(y, x.contiguous(), down, up, ends, slots, scales)
     return hadacore.adapt_rows(x, down, up, ends, slots, y=y, scales=scales)
 
