@@ -70,7 +70,7 @@ def adapt(y: torch.Tensor, x: torch.Tensor, down: torch.Tensor, up: torch.Tensor
     (x's, or float32).  ``groups`` is ``hadacore.group_tokens``' of one id a token; None: one
     adapter for all.  ``scales`` (float32, one for each adapter) has no gradient."""
     ends, slots = (None, None) if groups is None else (groups.ends, groups.slots)
-    if scales is not None and scales.requires_grad:
+    if scales is not None and scales.requires_grad and torch.is_grad_enabled():
         raise ValueError("the adapters' scales have no gradient")
     # where forward mode is on, too: the function refuses tensors with tangents, which a call would drop
     if forward_ad._current_level >= 0 or torch.is_grad_enabled() and any(t.requires_grad for t in (y, x, down, up)):

@@ -40,3 +40,12 @@ def test_without_tangents_the_level_changes_nothing():
     want = A.adapt(**values)
     with forward_ad.dual_level():
         assert torch.equal(A.adapt(**values), want)
+
+
+def test_scales_of_a_module_without_gradients():
+    """Scales kept as a parameter serve where no gradient is made; where one would be, they are refused."""
+    values, scales = _values(), torch.nn.Parameter(torch.full((1,), 2.0, dtype=torch.float64))
+    with torch.no_grad():
+        assert torch.equal(A.adapt(**values, scales=scales), A.adapt(**values, scales=scales.detach()))
+    with pytest.raises(ValueError, match="scales"):
+        A.adapt(**values, scales=scales)
