@@ -29,6 +29,7 @@
 
 #include <type_traits>
 
+#include "adapters_cut.h"
 #include "groups.h"
 #include "hadacore.h"
 #include "internal.h"
@@ -45,9 +46,6 @@ typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef u4 u4_any __attribute__((aligned(2)));
 typedef u2 u2_any __attribute__((aligned(2)));
 typedef u4 u4_words __attribute__((aligned(4)));
-
-constexpr int kTile = 16;   // rows and columns of a matrix product
-constexpr int kStep = 32;   // its depth
 
 // D (16 x 16) += A B: lane l holds A[l % 16][8 (l / 16) + j], B[8 (l / 16) + j][l % 16] and
 // D[4 (l / 16) + v][l % 16].
@@ -76,8 +74,6 @@ __device__ __forceinline__ float widen(uint16_t h) {
   else
     return __builtin_bit_cast(float, (uint32_t)h << 16);
 }
-
-constexpr int kParts = 3;
 
 // Takes part i off v, a sum of kParts values of 16 bits.  Parts of bf16 but the last are cut off, so that a
 // NaN stays one (what is left of it is a quiet NaN) and no part rounds up to Inf.
@@ -646,8 +642,6 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
 // instead of 13, and 64 tokens of 32 adapters 10.8 instead of 13; inside a graph, where a launch
 // costs little, 8.5 instead of 7.3 and 11.0 instead of 9.3.  For ranks up to 16 and few workgroups:
 // 256 tokens of 64 adapters gain nothing, rank 64 takes 20 instead of 9.
-constexpr int kFewWaves = 8;
-
 template <int DT, int OUT, bool EVEN>
 __global__ __launch_bounds__(kFewWaves *kWave) void few_tokens_kernel(AdapterArgs p) {
   constexpr int CT = 8, U = 4, P = kParts, kPitch = kStep + 8;
@@ -836,8 +830,6 @@ __device__ __forceinline__ void store_value(void *out, int64_t at, float v) {
     static_cast<uint16_t *>(out)[at] = narrow<OUT>(v);
 }
 
-constexpr int kGradColumns = kTile * 8;
-
 // A step of 32 tokens of dW[g]: their h (hv: rank c of 16 and tokens 8 quarter + j) times their x
 // (raw: the same tokens, 8 columns).  fp16: h is taken times 2^-shift, a power of its own for each rank
 // that grows with its values: what is large in one rank, or Inf, takes no bits of the others.
@@ -937,8 +929,6 @@ __device__ __forceinline__ void store_gradient(const GradientArgs &p, int g, int
 // is split.  Each wave streams its own rows of x and h into a ring in LDS, two steps ahead, and
 // their tokens three: no barriers, and few instructions, which are loaded anew by every call
 // (8191 x 4096, four adapters of rank 16: 27 us; with the loads in registers, a step ahead, 31).
-constexpr int kGradWaves = 2;
-
 template <int DT, int OUT, int RT>
 __global__ __launch_bounds__(kGradWaves *kWave) void gradient_kernel(GradientArgs p) {
   constexpr int D = RT == 4 ? 2 : 3;  // stages of the ring: two workgroups to a CU
@@ -1140,68 +1130,6 @@ bool aligned_to(const void *p, uintptr_t bytes) {
   return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0;
 }
 
-// ---- how a call is cut ---------------------------------------------------------------
-
-constexpr int64_t kBlocksWanted = 512;  // two workgroups to a CU of a whole card
-
-int64_t round_up(int64_t v, int64_t unit) { return (v + unit - 1) / unit * unit; }
-int64_t divide_up(int64_t v, int64_t by) { return (v + by - 1) / by; }
-
-// Pieces of `unit` rows that `groups` groups of m rows can have at most.
-int64_t most_pieces(int64_t m, int64_t groups, int64_t unit) {
-  return m / unit + (groups < m ? groups : m) + 1;
-}
-
-// Workgroups of few_tokens_kernel at most, and the longest k of which each makes its own h.
-constexpr int64_t kFewBlocks = 192, kFewDepth = 8192;
-
-struct Cut {
-  bool fused;  // few_tokens_kernel
-  int ranks;   // tiles of ranks in a workgroup of down_kernel
-  int tiles;   // tiles of tokens there
-  int splits;  // shares of k
-  int unit;    // tokens of a workgroup of up_kernel
-};
-
-Cut cut_of(int64_t m, int64_t k, int64_t n, int64_t rank, int64_t groups) {
-  Cut cut{};
-  // 64 ranks at most: of more, another workgroup reads x again, but 128 in one leave no registers for
-  // loads ahead (16384 x 4096 x 4096, rank 128: 222 us a call instead of 261)
-  cut.ranks = rank <= 16 ? 1 : rank <= 32 ? 2 : 4;
-  const int64_t live = groups < 1 || m < 1 ? 1 : groups < m ? groups : m;
-  const bool few = m <= 32 * live;
-  cut.tiles = few ? 1 : 4;
-  cut.splits = 1;
-  cut.unit = kTile;
-  cut.fused = few && rank <= kTile && k <= kFewDepth &&
-              most_pieces(m, groups, kTile) * divide_up(n, kFewWaves * 128) <= kFewBlocks;
-  if (cut.fused) return cut;
-  const int64_t blocks =
-      (divide_up(m, 16 * cut.tiles) + live - 1) * divide_up(rank, 16 * cut.ranks);
-  // with four tiles of ranks a wave takes a whole SIMD: a workgroup to a CU
-  int64_t splits = divide_up(cut.ranks == 4 ? kBlocksWanted / 2 : kBlocksWanted, blocks < 1 ? 1 : blocks);
-  const int64_t most = k / 512;  // four steps of k for a wave at least
-  splits = splits > most ? most : splits;
-  cut.splits = (int)(splits < 1 ? 1 : splits > 16 ? 16 : splits);
-  const int64_t depth = round_up(rank, kStep), columns = divide_up(n, rank > 128 ? 256 : 512);
-  cut.unit = 16;
-  while (cut.unit < 128 && !few && 2 * cut.unit * (depth + 8) * 2 * kParts <= 48 * 1024 &&
-         m / (2 * cut.unit) * columns >= (rank > 64 ? 1 : 2) * kBlocksWanted)
-    cut.unit *= 2;
-  return cut;
-}
-
-int64_t gradient_splits(int64_t m, int64_t width, int64_t rank, int64_t groups) {
-  if (groups < 1 || width < 1) return 1;
-  const int64_t blocks = divide_up(width, kGradColumns) * groups * divide_up(rank, 64);
-  // all at once, two to a CU; of one tile of ranks twice as many do as well or better
-  int64_t splits = divide_up(rank <= kTile ? 2 * kBlocksWanted : kBlocksWanted, blocks);
-  // a workgroup goes through 64 tokens in a turn; a share has two turns at least
-  const int64_t most = m / groups / (2 * kStep * kGradWaves);
-  splits = splits > most ? most : splits;
-  return splits < 1 ? 1 : splits > 16 ? 16 : splits;
-}
-
 template <class F>
 void for_type(hadacore_dtype dtype, F f) {
   if (dtype == HADACORE_FP16)
@@ -1250,7 +1178,8 @@ void launch_up(AdapterArgs p, hipStream_t stream) {
   constexpr int kAhead = 2;
   const auto go = [&](auto rb, auto ct) {
     constexpr int RB = decltype(rb)::value, CT = decltype(ct)::value;
-    const size_t lds = (size_t)p.unit * (kParts * (kStep * RB + 8) * 2 + 8);
+    static_assert(CT == 8 || RB == 8, "columns of a workgroup: up_columns");
+    const size_t lds = (size_t)up_room(p.unit, p.rank);
     // the columns of a token's row run together: whole rows of y and out, and with as many chunks as
     // XCDs (or a multiple) each of them meets only its own columns of the weights
     p.chunks = p.n > 0 ? (int)divide_up(p.n, 4 * 16 * CT) : 1;  // without columns h is joined
@@ -1262,11 +1191,12 @@ void launch_up(AdapterArgs p, hipStream_t stream) {
   };
   using std::integral_constant;
   const integral_constant<int, 8> eight{};
-  if (p.rank <= 32)
+  const int64_t steps = up_steps(p.rank);
+  if (steps == 1)
     go(integral_constant<int, 1>{}, eight);
-  else if (p.rank <= 64)
+  else if (steps == 2)
     go(integral_constant<int, 2>{}, eight);
-  else if (p.rank <= 128)
+  else if (steps == 4)
     go(integral_constant<int, 4>{}, eight);
   else
     go(eight, integral_constant<int, 4>{});
@@ -1430,7 +1360,7 @@ extern "C" hadacore_status hadacore_adapters(
     return HADACORE_ERROR_OVERLAP;
   const Cut cut = cut_of(m, k, n, rank, groups);
   // up_kernel's launch, the largest
-  if (!cut.fused && most_pieces(m, groups, cut.unit) * divide_up(n, rank > 128 ? 256 : 512) * 256 >=
+  if (!cut.fused && most_pieces(m, groups, cut.unit) * divide_up(n, up_columns(rank)) * 256 >=
                         (int64_t(1) << 32))
     return HADACORE_ERROR_TOO_LARGE;
   st = check_device();
