@@ -541,7 +541,7 @@ int64_t hadacore_adapters_workspace_size(int64_t m, int64_t k, int64_t n, int64_
  *               rank rounded up to 16): down[g] x[t] by place, zeros up to that width; places behind
  *               the last end are left as they were.  The gradient of the weights takes it
  * The gradients of x are the same call on dout with `down` and `up` exchanged and y = NULL.
- * Between the products h is fp32, and the second takes all of its 24 bits (for fp16 above 2^-36 of
+ * Between the products h is fp32, and the second takes all of its 24 bits (for fp16 above 2^-35 of
  * the row's largest).  Inf may give NaN.
  */
 hadacore_status hadacore_adapters(const void *x, int64_t x_row_stride, const void *down,
@@ -563,7 +563,7 @@ int64_t hadacore_adapter_gradient_workspace_size(int64_t m, int64_t width, int64
  * hadacore_adapter_gradient -- out[g] (rank x width) = scales[g] * sum over the places p of g of
  * hidden[p] x[token of p]^T: the gradient of `up` from hidden and dout, and that of `down` from the
  * hidden of the gradient's call (dout, roles exchanged) and x.  A group without tokens gets
- * zeros.  All 24 bits of hidden are taken (for fp16 above 2^-36 of the rank's largest value in the
+ * zeros.  All 24 bits of hidden are taken (for fp16 above 2^-35 of the rank's largest value in the
  * group), and a rank's values show in its own row only, Inf and NaN too.  out_dtype is `dtype` or
  * HADACORE_FP32; other arguments as for hadacore_adapters.
  */

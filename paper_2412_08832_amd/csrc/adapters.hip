@@ -19,7 +19,7 @@
 // adapter's part may cancel against y and leave any bit of h to be seen.  (Two parts, which keep 16
 // bits of it in bf16, save 0 to 4% of a call.)  fp16 parts are made of h times a power of two (largest
 // value of the row near 2^10): all bits of values down to 2^-11 of the row's largest, and of smaller
-// ones those above 2^-36 of it.  A value of h, a weight or an x that is Inf gives a NaN where the sum
+// ones those above 2^-35 of it.  A value of h, a weight or an x that is Inf gives a NaN where the sum
 // without parts may give Inf: Inf times a part of 0 is NaN.
 
 #include <hip/hip_runtime.h>
