@@ -540,7 +540,8 @@ int64_t hadacore_adapters_workspace_size(int64_t m, int64_t k, int64_t n, int64_
  *   hidden      NULL, or m rows of fp32 (16-byte aligned, a stride of a multiple of 4 and at least
  *               rank rounded up to 16): down[g] x[t] by place, zeros up to that width; places behind
  *               the last end are left as they were.  The gradient of the weights takes it
- * The gradients of x are the same call on dout with `down` and `up` exchanged and y = NULL.
+ * The gradients of x are the same call on dout with `down` and `up` exchanged and y = NULL; dout, as x, is
+ * of `dtype`, also where the output was of 32 bits.
  * Between the products h is fp32, and the second takes all of its 24 bits (for fp16 above 2^-35 of
  * the row's largest).  Inf may give NaN.
  */

@@ -50,7 +50,8 @@ class _Adapt(torch.autograd.Function):
         x, down, up, ends, slots, scales, h = ctx.saved_tensors
         need_x, need_down, need_up = ctx.needs_input_grad[1:4]
         dx = d_down = d_up = None
-        # of a projection in 32 bits: in x's type, as the products take it
+        # of a projection in 32 bits: rounded to x's type, which the products take; the gradients are
+        # rounded to it themselves
         dout = dout.to(x.dtype).contiguous()
         if need_down:
             # without x's gradient only the first of the two products is made
@@ -68,7 +69,11 @@ def adapt(y: torch.Tensor, x: torch.Tensor, down: torch.Tensor, up: torch.Tensor
           groups: hadacore.Groups | None = None, scales: torch.Tensor | None = None) -> torch.Tensor:
     """y + scales[g] * (x down[g]^T) up[g] for the tokens of each adapter g; a new tensor of y's type
     (x's, or float32).  ``groups`` is ``hadacore.group_tokens``' of one id a token; None: one
-    adapter for all.  ``scales`` (float32, one for each adapter) has no gradient."""
+    adapter for all.  ``scales`` (float32, one for each adapter) has no gradient.
+
+    The gradient of a float32 output is y's as it is; for those of x, down and up it is rounded to x's
+    type first, as by a cast of the adapters' part before it is added: half a step of that type for
+    each value, and float16 has its range (scale the loss as for a float16 layer)."""
     ends, slots = (None, None) if groups is None else (groups.ends, groups.slots)
     if scales is not None and scales.requires_grad and torch.is_grad_enabled():
         raise ValueError("the adapters' scales have no gradient")
