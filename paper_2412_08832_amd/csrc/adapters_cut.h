@@ -65,7 +65,10 @@ inline Cut cut_of(int64_t m, int64_t k, int64_t n, int64_t rank, int64_t groups)
   if (cut.fused) return cut;
   const int64_t blocks =
       (divide_up(m, 16 * cut.tiles) + live - 1) * divide_up(rank, 16 * cut.ranks);
-  // with four tiles of ranks a wave takes a whole SIMD: a workgroup to a CU
+  // Half of the workgroups with four tiles of ranks, though two of these fit a CU as well: more shares cost
+  // more of h to write and join.  With all of them 1024 x 8192 -> 4096, rank 128, takes 51 us instead of 44,
+  // 4096 x 4096 -> 4096 and 12000 x 4096 -> 4096, ranks 64 and 48, 49 and 89 instead of 46 and 85; others
+  // gain: 8192 x 4096 -> 4096, ranks 64 and 80, 72 and 121 instead of 76 and 128.
   int64_t splits = divide_up(cut.ranks == 4 ? kBlocksWanted / 2 : kBlocksWanted, blocks < 1 ? 1 : blocks);
   const int64_t most = k / 512;  // four steps of k for a wave at least
   splits = splits > most ? most : splits;
