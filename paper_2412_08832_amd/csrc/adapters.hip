@@ -45,7 +45,6 @@ typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef u4 u4_any __attribute__((aligned(2)));
 typedef u2 u2_any __attribute__((aligned(2)));
-typedef u4 u4_words __attribute__((aligned(4)));
 
 // D (16 x 16) += A B: lane l holds A[l % 16][8 (l / 16) + j], B[8 (l / 16) + j][l % 16] and
 // D[4 (l / 16) + v][l % 16].
@@ -181,7 +180,7 @@ __device__ __forceinline__ void load_columns(const uint16_t *p, int64_t valid, u
   }
 }
 
-// Sum, or maximum, over the lanes of a wave in steps of xor.
+// Maximum over groups of `lanes` lanes of a wave, in steps of xor.
 __device__ __forceinline__ float max_lanes(float x, int lanes) {
   for (int step = 1; step < lanes; step *= 2) x = fmaxf(x, __shfl_xor(x, step));
   return x;

@@ -27,8 +27,6 @@ namespace {
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
-typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 
 constexpr int kMaxChoices = HADACORE_MAX_CHOICES;
 constexpr int kMaxExperts = HADACORE_MAX_EXPERTS;
