@@ -137,8 +137,9 @@ __device__ __forceinline__ u4 moved(u4 v, int by) {
 
 // How far before its own place a lane loads N values, `valid` of which are there, so that they end
 // with the row: in a row of N and more they are inside it, and no load stands in a branch, where a
-// wave would wait for each by itself.  move_values() then brings them to their places.  (up_kernel,
-// 3525 x 997, rank 95: 20 us instead of 55; gradient_any_kernel, 1957 x 5597, rank 9: 18 instead of 35.)
+// wave would wait for each by itself.  move_values() then brings them to their places.  (When it came in:
+// up_kernel, 3525 x 997, rank 95: 20 us instead of 55; gradient_any_kernel, 1957 x 5597, rank 9: 18
+// instead of 35.)
 template <int N>
 __device__ __forceinline__ int ahead_of(int64_t valid) {
   return valid >= N ? 0 : N - (int)valid;
@@ -326,8 +327,8 @@ __global__ __launch_bounds__(W *kWave) void down_kernel(AdapterArgs p) {
 }
 
 // Values that are read or written once: where rows are whole lines, the streaming policy (NT)
-// keeps them from pushing the weights and h out of the L2 (16384 x 8192: up_kernel 118 us instead of
-// 150).  Rows that share lines are slower with it (1733 x 5003 in 32 bits: 28 instead of 23).
+// keeps them from pushing the weights and h out of the L2 (16384 x 8192: up_kernel 122 us instead of
+// 133, a call 158 instead of 168).  Rows that share lines are slower with it (1733 x 5003 in 32 bits: 28 instead of 23).
 template <bool NT, class V>
 __device__ __forceinline__ V stream_in(const void *p) {
   if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const V *>(p));
@@ -637,9 +638,9 @@ __global__ __launch_bounds__(256) void up_kernel(AdapterArgs p) {
 // Both products in one launch, for up to 16 tokens of a group and 1024 columns: every workgroup makes
 // h itself, which costs it the group's `down` again (from the L2) but saves a launch and the
 // way of h through memory.  Eight waves share k and add up; then each has its 128 columns, whose weights
-// and y were loaded at the start.  Called one by one 1 token of rank 16, 4096 x 4096 takes 9.5 us
-// instead of 13, and 64 tokens of 32 adapters 10.8 instead of 13; inside a graph, where a launch
-// costs little, 8.5 instead of 7.3 and 11.0 instead of 9.3.  For ranks up to 16 and few workgroups:
+// and y were loaded at the start.  Called one by one 1 token of rank 16, 4096 x 4096 takes 11.5 us
+// instead of 15.0, and 64 tokens of 32 adapters 11.6 instead of 15.1; inside a graph, where a launch
+// costs little, 8.6 instead of 7.4 and 11.5 instead of 8.9.  For ranks up to 16 and few workgroups:
 // 256 tokens of 64 adapters gain nothing, rank 64 takes 20 instead of 9.
 template <int DT, int OUT, bool EVEN>
 __global__ __launch_bounds__(kFewWaves *kWave) void few_tokens_kernel(AdapterArgs p) {
@@ -927,7 +928,8 @@ __device__ __forceinline__ void store_gradient(const GradientArgs &p, int g, int
 // two waves in turn.  Both operands have the tokens along their depth: x is turned in registers, h
 // is split.  Each wave streams its own rows of x and h into a ring in LDS, two steps ahead, and
 // their tokens three: no barriers, and few instructions, which are loaded anew by every call
-// (8191 x 4096, four adapters of rank 16: 27 us; with the loads in registers, a step ahead, 31).
+// (8191 x 4096, four adapters of rank 16: 27 us; when it came in, 31 with the loads in registers, a step
+// ahead).
 template <int DT, int OUT, int RT>
 __global__ __launch_bounds__(kGradWaves *kWave) void gradient_kernel(GradientArgs p) {
   constexpr int D = RT == 4 ? 2 : 3;  // stages of the ring: two workgroups to a CU

@@ -34,9 +34,9 @@ inline int64_t up_steps(int64_t rank) { return rank <= 32 ? 1 : rank <= 64 ? 2 :
 inline int64_t up_columns(int64_t rank) { return rank > 128 ? 4 * 16 * 4 : 4 * 16 * 8; }
 
 // Its LDS for `unit` tokens: the parts of h, a power of two and the token's row.  At most a third of a
-// CU's: units of 128, 64, 64 and 32 tokens for its four versions.  (16384 x 4096 x 8192, rank 64: 188 us a
-// call, with units of 128 199; 16384 x 4096 x 4096, rank 128: 230, with units of 32 277; 8192 x 4096 x 4096,
-// ranks 160 and 256: 181 and 221, with units of 64 206 and 245.)
+// CU's: units of 128, 64, 64 and 32 tokens for its four versions.  (16384 x 4096 -> 8192, rank 64: 188 us a
+// call, with units of 128 199; 16384 x 4096 -> 4096, rank 128: 230, with units of 32 277; 8192 x 4096 -> 4096,
+// rank 160, and rank 256 in 32 bits: 181 and 221, with units of 64 206 and 245.)
 constexpr int64_t kUpRoom = 53 * 1024;
 inline int64_t up_room(int64_t unit, int64_t rank) {
   return unit * (kParts * (kStep * up_steps(rank) + 8) * 2 + 8);
@@ -53,7 +53,7 @@ struct Cut {
 inline Cut cut_of(int64_t m, int64_t k, int64_t n, int64_t rank, int64_t groups) {
   Cut cut{};
   // 64 ranks at most: of more, another workgroup reads x again, but 128 in one leave no registers for
-  // loads ahead (16384 x 4096 x 4096, rank 128: 222 us a call instead of 261)
+  // loads ahead (16384 x 4096 -> 4096, rank 128, when it came in: 222 us a call instead of 261)
   cut.ranks = rank <= 16 ? 1 : rank <= 32 ? 2 : 4;
   const int64_t live = groups < 1 || m < 1 ? 1 : groups < m ? groups : m;
   const bool few = m <= 32 * live;
